@@ -467,8 +467,8 @@ def exact(c, seed):
         out = {"rstd": rstd[:, 0], "y": n * weight + (s["bias"].double() if c["bias"] else 0.0)}
         if not c["rms"]:
             out["mean"] = mean[:, 0]
-        if c["kept"]:
-            out["kept"] = _nearest_kept(n)
+        if c["kept"]:  # what 8 bits stand for: which of two neighbours they take is no matter of the definition where n
+            out["kept"] = n  # lies between them to within the 32 bits of its sums
         return out
     dy, rstd = s["dy"].double(), s["rstd"].double()[:, None]
     if c["kept"]:
