@@ -438,6 +438,133 @@ uint64_t lc_record_bytes(const lc_ctx *c, uint32_t layer);
 /* Synchronises the stream and frees the context (NULL is a no-op). */
 lc_status lc_destroy(lc_ctx *c);
 
+/* ---- Training operators -----------------------------------------------------
+ * What a training step computes around the weights of a layout: the embedding
+ * and its gradient, layer norm and RMS norm with their gradients, activations
+ * kept in 8 bits, and a linear layer's weight gradient from them.  Their
+ * gradients are what lc_adamw_step_score and lc_sgd_step_score take, in the
+ * same types (LC_DT_BF16, LC_DT_F32).
+ *
+ * These calls need no context.  Every array is device memory of the caller's;
+ * a call writes the arrays that it returns and the workspace it is given, and
+ * keeps nothing.  All work is enqueued on `stream` (a hipStream_t of the
+ * current device, NULL = null stream) and the calls return without waiting;
+ * they allocate nothing, so they may be captured into a HIP graph.  Arguments
+ * are checked first (LC_ERR_INVALID_ARG, nothing enqueued): sizes, types,
+ * alignment, and that no array that is written overlaps another one (columns
+ * of one buffer beside each other are fine).  As with the gradients of the
+ * optimizer steps, addresses are checked for NULL and alignment and not
+ * looked up: a wrong one faults on the GPU.  A workspace is 16-byte aligned
+ * and at least as large as the _workspace call says for the same sizes
+ * (LC_ERR_CAPACITY if smaller; the _workspace calls give 0 for sizes beyond
+ * the limits, and where no workspace is needed); its contents need not be
+ * kept between calls.  Sums are fp32 or wider and their order is fixed, so a
+ * call gives the same bits every time. */
+
+/* Rows of elements in device memory: element (r, c) at data + (r * stride + c)
+ * elements.  At most 2^31 rows of 2^30 columns; data is aligned to its element
+ * (any element may be the first). */
+typedef struct {
+  void *data;       /* device; may be NULL with 0 rows           */
+  uint64_t rows;
+  uint64_t cols;    /* >= 1                                      */
+  uint64_t stride;  /* elements from row to row, >= cols (not
+                       looked at with fewer than two rows)        */
+  int32_t dtype;    /* lc_dtype                                   */
+  int32_t reserved; /* must be 0                                  */
+} lc_matrix;
+
+typedef enum { LC_IT_I32 = 1, LC_IT_I64 = 2 } lc_token_dtype;
+
+/* out[t] = scale * weight[token[t] - first_token], rounded to out's dtype from
+ * fp32; a row of zeros where that is no row of `weight` (a padding id, or a
+ * row that another rank of a vocabulary split holds: the ranks' results add up
+ * to the whole).  weight: vocabulary rows x dim, out: n_tokens x dim, either
+ * of both dtypes. */
+lc_status lc_embedding_forward(const lc_matrix *weight, const void *tokens, int32_t token_dtype, uint64_t n_tokens,
+                               int64_t first_token, double scale, const lc_matrix *out, void *stream);
+
+/* dweight[v] = scale * sum of dout[t] over the t whose token is v + first_token
+ * (accumulate 1: added to what dweight holds; 0: dweight is written in full,
+ * zeros in rows that no token has).  The tokens are sorted, a row's sum runs
+ * in the order of its positions in fp32 and is rounded once.  Tokens outside
+ * the rows of dweight add nothing.  dout: n_tokens x dim, dweight: vocabulary
+ * rows x dim, either of both dtypes. */
+uint64_t lc_embedding_backward_workspace(uint64_t n_tokens, uint64_t cols);
+lc_status lc_embedding_backward(const lc_matrix *dout, const void *tokens, int32_t token_dtype, uint64_t n_tokens,
+                                int64_t first_token, double scale, int32_t accumulate, const lc_matrix *dweight,
+                                void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* An activation kept in 8 bits: rows x cols codes and, for every 32 columns of
+ * a row, the exponent of a power of two.  A code is a sign, 4 exponent and 3
+ * mantissa bits (bias 7; the largest value is 448, 0x7F and 0xFF are NaN,
+ * there are no infinities), a scale byte s stands for 2^(s - 127) (255: NaN).
+ * Kept is code * 2^(s - 127) with the smallest power that brings the largest
+ * finite element of the 32 to 448 or less, and codes to nearest, halves to
+ * even: an element keeps 4 significant bits (an error of at most 2^-4 of
+ * itself, or 2^-17 of the block's largest where that is more), none
+ * saturates (but what lies beyond 1.875 * 2^127 is kept as that, so that what
+ * is finite stays so), and its value is exact in bf16 (down to 2^-126).  An
+ * element that is infinite or NaN is kept as NaN and leaves its neighbours
+ * alone. */
+typedef struct {
+  void *codes;           /* device, any alignment                              */
+  void *scales;          /* device, any alignment                              */
+  uint64_t rows;
+  uint64_t cols;         /* >= 1                                               */
+  uint64_t code_stride;  /* bytes from row to row, >= cols                     */
+  uint64_t scale_stride; /* bytes from row to row, >= ceil(cols / 32)          */
+} lc_saved_act;
+
+/* x into its 8-bit form, and back: out's dtype is either. */
+lc_status lc_act_save(const lc_matrix *x, const lc_saved_act *saved, void *stream);
+lc_status lc_act_load(const lc_saved_act *saved, const lc_matrix *out, void *stream);
+
+typedef enum { LC_NORM_LAYER = 0, LC_NORM_RMS = 1 } lc_norm_kind;
+
+typedef struct {
+  int32_t kind;        /* lc_norm_kind                                          */
+  int32_t param_dtype; /* lc_dtype of weight and bias                           */
+  const void *weight;  /* device [cols]; NULL: ones                             */
+  const void *bias;    /* device [cols]; NULL: zeros; NULL for LC_NORM_RMS      */
+  double eps;          /* finite and >= 0                                       */
+} lc_norm_params;
+
+/* For every row, n = (x - mean) * rstd and y = n * weight + bias, with
+ * rstd = 1 / sqrt(mean((x - mean)^2) + eps); LC_NORM_RMS has no mean (0) and
+ * no bias.  y has x's shape and dtype.  mean (LC_NORM_LAYER only) and rstd
+ * receive one float a row, for the backward pass; either may be NULL.  With
+ * `saved` the normalised rows n are kept there in 8 bits from their fp32
+ * values; the backward pass then needs neither x nor mean, and lc_linear_wgrad
+ * takes the same rows for the layer that follows (its col_scale and col_shift
+ * are weight and bias), so neither x nor y has to be kept. */
+lc_status lc_norm_forward(const lc_norm_params *params, const lc_matrix *x, const lc_matrix *y, float *mean,
+                          float *rstd, const lc_saved_act *saved, void *stream);
+
+/* With g = dy * weight, and n from x, mean and rstd, or from `saved` (exactly
+ * one of x and saved is given; mean goes with x and LC_NORM_LAYER):
+ *   dx = rstd * (g - mean(g) - n * mean(g * n))     (LC_NORM_RMS: without mean(g))
+ *   dweight (+)= sum over rows of dy * n,  dbias (+)= sum over rows of dy
+ * dx (dy's shape and dtype), dweight and dbias ([cols] of grad_dtype) may each
+ * be NULL; accumulate applies to the latter two.  The workspace is needed for
+ * dweight or dbias. */
+uint64_t lc_norm_backward_workspace(uint64_t rows, uint64_t cols);
+lc_status lc_norm_backward(const lc_norm_params *params, const lc_matrix *dy, const lc_matrix *x, const float *mean,
+                           const float *rstd, const lc_saved_act *saved, const lc_matrix *dx, void *dweight,
+                           void *dbias, int32_t grad_dtype, int32_t accumulate, void *workspace,
+                           uint64_t workspace_bytes, void *stream);
+
+/* The weight gradient of y = X W^T + bias, with X kept in 8 bits:
+ *   dweight[n][k] (+)= sum over rows t of dy[t][n] * (X[t][k] * col_scale[k] + col_shift[k])
+ *   dbias[n] (+)= sum over rows t of dy[t][n]
+ * dy: rows x n, saved: rows x k, dweight: n x k, dbias: [n] of dweight's dtype
+ * or NULL; col_scale and col_shift: [k] of param_dtype, each may be NULL (1, 0).
+ * Products are exact (an fp32 dy enters with all its 24 bits), sums fp32. */
+uint64_t lc_linear_wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k);
+lc_status lc_linear_wgrad(const lc_matrix *dy, const lc_saved_act *saved, const void *col_scale,
+                          const void *col_shift, int32_t param_dtype, const lc_matrix *dweight, void *dbias,
+                          int32_t accumulate, void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* Message for the last failing call on this thread ("" if none). */
 const char *lc_last_error(void);
 

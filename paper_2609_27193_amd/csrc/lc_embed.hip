@@ -1,0 +1,516 @@
+// Rows of a table by token, scaled, and the table's gradient.
+//
+//   out[t] = scale * W[token[t] - first]            (zeros for a token outside the table)
+//   dW[v] (+)= scale * sum over t with token[t] - first = v of dout[t]
+//
+// Both are bound by memory.  The gradient sorts the tokens, so that every row
+// of the table is written once, and sums a row's tokens in the order of their
+// positions, in fp32: the result does not depend on how blocks are scheduled.
+#include "lc_ops_device.h"
+
+namespace lc {
+namespace {
+
+// Row of the table for token i, or `vocab` for a token outside it.
+__device__ __forceinline__ uint32_t token_row(uint64_t tokens, int token64, uint64_t i, int64_t first, uint64_t vocab) {
+  typedef const __attribute__((address_space(1))) int64_t gc_i64;
+  typedef const __attribute__((address_space(1))) int32_t gc_i32;
+  const int64_t t = token64 ? *(gc_i64*)(tokens + 8 * i) : *(gc_i32*)(tokens + 4 * i);
+  const uint64_t r = static_cast<uint64_t>(t) - static_cast<uint64_t>(first);  // wraps below `first`: beyond the table
+  return t >= first && r < vocab ? static_cast<uint32_t>(r) : static_cast<uint32_t>(vocab);
+}
+
+constexpr uint32_t kEmbedThreads = 256;
+constexpr int kEmbedVecs = 4;  // groups of eight that a thread has in flight
+
+// `lanes` threads (a power of two) take one token's row, 8 elements each at a time.
+template <int WDT, int ODT>
+__global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, uint32_t lanes_log2) {
+  const uint32_t lanes = 1u << lanes_log2, per_block = kEmbedThreads >> lanes_log2;
+  const uint32_t groups = (a.dim + 7) / 8, lane = threadIdx.x & (lanes - 1);
+  const uint64_t items = (a.n + per_block - 1) / per_block;
+  for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const uint64_t t = it * per_block + (threadIdx.x >> lanes_log2);
+    if (t >= a.n) continue;
+    const uint32_t row = token_row(a.tokens, a.token64, t, a.first, a.vocab);
+    const bool held = row < a.vocab;
+    const uint64_t src = a.w.data + static_cast<uint64_t>(row) * a.w.stride * kEsz<WDT>;
+    const uint64_t dst = a.out.data + t * a.out.stride * kEsz<ODT>;
+    for (uint32_t g0 = lane; g0 < groups; g0 += lanes * kEmbedVecs) {
+      Raw8<WDT> r[kEmbedVecs];
+#pragma unroll
+      for (int i = 0; i < kEmbedVecs; ++i) {
+        const uint32_t g = g0 + i * lanes;
+        for (auto& q : r[i].v) q = u32x4{0, 0, 0, 0};
+        if (held && g < groups) r[i] = load8_raw<WDT>(src + 8ull * kEsz<WDT> * g, in_group(a.dim, g));
+      }
+#pragma unroll
+      for (int i = 0; i < kEmbedVecs; ++i) {
+        const uint32_t g = g0 + i * lanes;
+        if (g >= groups) break;
+        float f[8];
+        unpack8<WDT>(r[i], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = held ? f[e] * a.scale : 0.0f;
+        store8<ODT>(dst + 8ull * kEsz<ODT> * g, f, in_group(a.dim, g));
+      }
+    }
+  }
+}
+
+// ---- sorting the tokens ------------------------------------------------------------
+// Up to kRankTokens one launch counts, for every token, the tokens that come
+// before it (a smaller row, or the same row at an earlier position); beyond
+// that a radix sort of kDigitBits a pass, two launches a pass.
+constexpr uint32_t kRankTokens = 8192;
+constexpr uint32_t kRankThreads = 256;
+constexpr uint32_t kRankOwn = 32;  // tokens of a block; its 8 slices of threads share the others
+constexpr uint32_t kDigitBits = 9, kDigits = 1u << kDigitBits;
+constexpr uint32_t kSortThreads = 512;
+constexpr uint32_t kSortWaves = kSortThreads / 64;
+static_assert(kSortThreads == kDigits, "one thread a digit");
+
+__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedBwd a, uint32_t* keys, uint32_t* pos) {
+  __shared__ __align__(16) uint32_t all[kRankTokens];
+  __shared__ uint32_t count[kRankThreads / kRankOwn][kRankOwn];
+  const uint32_t n = static_cast<uint32_t>(a.n);
+  const uint32_t padded = (n + kRankOwn - 1) / kRankOwn * kRankOwn;
+  for (uint32_t i = threadIdx.x; i < padded; i += kRankThreads)
+    all[i] = i < n ? token_row(a.tokens, a.token64, i, a.first, a.vocab) : 0xFFFFFFFFu;
+  __syncthreads();
+  const uint32_t own = threadIdx.x % kRankOwn, slice = threadIdx.x / kRankOwn;
+  for (uint32_t base = blockIdx.x * kRankOwn; base < n; base += gridDim.x * kRankOwn) {
+    const uint32_t i = base + own, key = all[i];
+    uint32_t before = 0;
+    // groups of kRankOwn tokens, dealt out to the slices
+    for (uint32_t g = slice * kRankOwn; g < padded; g += kRankThreads) {
+      if (g == base) {
+        for (uint32_t j = 0; j < kRankOwn; ++j) {
+          const uint32_t k = all[g + j];
+          before += k < key || (k == key && j < own);
+        }
+      } else {
+        // an equal row counts where it stands before: k < key + 1 there.  key
+        // is at most 2^31 for a token; the padding's own rank is not used.
+        const uint32_t limit = g < base ? key + 1 : key;
+#pragma unroll
+        for (uint32_t j = 0; j < kRankOwn; j += 4) {
+          const u32x4 k = *reinterpret_cast<const u32x4*>(&all[g + j]);
+          before += (k[0] < limit) + (k[1] < limit) + (k[2] < limit) + (k[3] < limit);
+        }
+      }
+    }
+    count[slice][own] = before;
+    __syncthreads();
+    if (slice == 0 && i < n) {
+      uint32_t r = 0;
+#pragma unroll
+      for (uint32_t s = 0; s < kRankThreads / kRankOwn; ++s) r += count[s][own];
+      keys[r] = key;
+      pos[r] = i;
+    }
+    __syncthreads();
+  }
+}
+
+// The tile of a radix pass: a multiple of kSortThreads that leaves at most kSortTiles of them.
+constexpr uint32_t kSortTiles = 512;
+__host__ __device__ inline uint32_t sort_tile(uint64_t n) {
+  const uint64_t per = (n + kSortTiles - 1) / kSortTiles;
+  const uint64_t t = (per + kSortThreads - 1) / kSortThreads * kSortThreads;
+  return static_cast<uint32_t>(t < 4 * kSortThreads ? 4 * kSortThreads : t);
+}
+
+// keys null: the tokens themselves, at position i.
+__device__ __forceinline__ uint32_t sort_key(const EmbedBwd& a, const uint32_t* keys, uint64_t i) {
+  return keys ? keys[i] : token_row(a.tokens, a.token64, i, a.first, a.vocab);
+}
+
+__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(EmbedBwd a, const uint32_t* keys, uint32_t shift,
+                                                                   uint32_t tile, uint32_t* hist) {
+  __shared__ uint32_t bins[kDigits];
+  const uint64_t tiles = (a.n + tile - 1) / tile;
+  for (uint64_t b = blockIdx.x; b < tiles; b += gridDim.x) {
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    const uint64_t end = b * tile + tile < a.n ? b * tile + tile : a.n;
+    for (uint64_t i = b * tile + threadIdx.x; i < end; i += kSortThreads)
+      atomicAdd(&bins[(sort_key(a, keys, i) >> shift) % kDigits], 1u);  // whole numbers: any order gives the same
+    __syncthreads();
+    hist[b * kDigits + threadIdx.x] = bins[threadIdx.x];
+    __syncthreads();
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a, const uint32_t* keys,
+                                                                     const uint32_t* pos, uint32_t shift, uint32_t tile,
+                                                                     const uint32_t* hist, uint32_t* keys_out,
+                                                                     uint32_t* pos_out) {
+  __shared__ uint32_t next[kDigits];              // where a digit's next key goes
+  __shared__ uint32_t wave_count[kSortWaves][kDigits];
+  __shared__ uint32_t wave_total[kSortWaves];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint64_t tiles = (a.n + tile - 1) / tile;
+  for (uint64_t b = blockIdx.x; b < tiles; b += gridDim.x) {
+    uint32_t total = 0, before = 0;
+    for (uint64_t j = 0; j < tiles; ++j) {
+      const uint32_t h = hist[j * kDigits + tid];
+      total += h;
+      before += j < b ? h : 0;
+    }
+    // exclusive sum of `total` over the digits
+    uint32_t scan = total;
+#pragma unroll
+    for (uint32_t d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(scan, d, 64);
+      if (lane >= d) scan += o;
+    }
+    if (lane == 63) wave_total[wave] = scan;
+    __syncthreads();
+    uint32_t base = scan - total;
+    for (uint32_t w = 0; w < wave; ++w) base += wave_total[w];
+    next[tid] = base + before;
+#pragma unroll
+    for (uint32_t w = 0; w < kSortWaves; ++w) wave_count[w][tid] = 0;
+    __syncthreads();
+    for (uint32_t r = 0; r < tile; r += kSortThreads) {
+      const uint64_t i = b * tile + r + tid;
+      const bool on = i < a.n;
+      const uint32_t key = on ? sort_key(a, keys, i) : 0;
+      const uint32_t digit = (key >> shift) % kDigits;
+      uint64_t same = __ballot(on);  // lanes of this wave with the same digit
+#pragma unroll
+      for (uint32_t bit = 0; bit < kDigitBits; ++bit) {
+        const bool one = digit >> bit & 1;
+        const uint64_t ones = __ballot(one);
+        same &= one ? ones : ~ones;
+      }
+      const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
+      if (on && rank == 0) wave_count[wave][digit] = __popcll(same);
+      __syncthreads();
+      uint32_t at = next[tid];
+#pragma unroll
+      for (uint32_t w = 0; w < kSortWaves; ++w) {  // thread tid owns digit tid
+        const uint32_t c = wave_count[w][tid];
+        wave_count[w][tid] = at;
+        at += c;
+      }
+      next[tid] = at;
+      __syncthreads();
+      if (on) {
+        const uint32_t to = wave_count[wave][digit] + rank;
+        keys_out[to] = key;
+        pos_out[to] = pos ? pos[i] : static_cast<uint32_t>(i);
+      }
+      __syncthreads();
+#pragma unroll
+      for (uint32_t w = 0; w < kSortWaves; ++w) wave_count[w][tid] = 0;
+      __syncthreads();
+    }
+  }
+}
+
+// ---- sums of the sorted tokens ---------------------------------------------------------
+// A wave takes `run` sorted positions and 512 columns.  A row whose tokens all
+// lie in the tile is written at once; one that crosses into the next tile
+// leaves fp32 partial sums: [tile][0] of the row that came in from the tile
+// before, [tile][1] of one that begins here and goes on.  The join kernel adds
+// those in the order of the tiles.  So a token that fills the batch is spread
+// over the chip like any others.
+constexpr uint32_t kSumThreads = 256;
+constexpr uint32_t kSumCols = 512;
+constexpr uint32_t kFillRows = 64;  // rows of the table that one block clears, where no token has them
+
+__host__ __device__ inline uint32_t sum_run(uint64_t n) {  // sorted positions of a tile: at most 2048 tiles up to n = 2^31
+  uint64_t r = 16;
+  while (r * 2048 < n) r *= 2;
+  return static_cast<uint32_t>(r);
+}
+
+struct SumArgs {
+  Rows dout, dw;
+  const uint32_t* keys;
+  const uint32_t* pos;
+  float* part;       // [tiles][2][dim]
+  uint64_t n, vocab;
+  uint32_t dim, run, tiles, chunks;
+  float scale;
+  int accumulate;
+};
+
+__device__ __forceinline__ float* sum_part(const SumArgs& a, uint64_t tile, int which) {
+  return a.part + (tile * 2 + which) * static_cast<uint64_t>(a.dim);
+}
+
+template <int GDT>
+__device__ __forceinline__ void sum_write(const SumArgs& a, uint32_t row, uint32_t g, const float (&acc)[8], int n) {
+  const uint64_t p = a.dw.data + (static_cast<uint64_t>(row) * a.dw.stride + 8ull * g) * kEsz<GDT>;
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = acc[e] * a.scale;
+  if (a.accumulate) {
+    float old[8];
+    unpack8<GDT>(load8_raw<GDT>(p, n), old);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] += old[e];
+  }
+  store8<GDT>(p, f, n);
+}
+
+__device__ __forceinline__ void part_write(float* p, uint32_t g, const float (&acc)[8], int n) {
+  store8<kF32>(reinterpret_cast<uint64_t>(p) + 32ull * g, acc, n);
+}
+
+template <int DDT, int GDT>
+__device__ void sum_tile(const SumArgs& a, uint64_t item) {
+  constexpr int U = 8;  // rows in flight
+  const uint32_t lane = threadIdx.x & 63;
+  const uint32_t tile = static_cast<uint32_t>(item / a.chunks), chunk = static_cast<uint32_t>(item % a.chunks);
+  const uint32_t g = chunk * (kSumCols / 8) + lane;
+  const int in = in_group(a.dim, g);
+  const uint64_t b0 = static_cast<uint64_t>(tile) * a.run;
+  const uint64_t b1 = b0 + a.run < a.n ? b0 + a.run : a.n;
+  const uint32_t none = static_cast<uint32_t>(a.vocab);
+  const uint32_t left = b0 ? a.keys[b0 - 1] : none;   // `none` sorts last and is never summed
+  const uint32_t right = b1 < a.n ? a.keys[b1] : none;
+  float acc[8] = {};
+  uint32_t cur = none;
+  bool open_left = false;
+  auto flush = [&](bool open_right) {
+    if (cur == none || in <= 0) return;
+    if (open_left) part_write(sum_part(a, tile, 0), g, acc, in);
+    else if (open_right) part_write(sum_part(a, tile, 1), g, acc, in);
+    else sum_write<GDT>(a, cur, g, acc, in);
+  };
+  for (uint64_t c0 = b0; c0 < b1; c0 += 64) {
+    const uint32_t m = static_cast<uint32_t>(b1 - c0 < 64 ? b1 - c0 : 64);
+    const uint32_t key = lane < m ? a.keys[c0 + lane] : none;
+    const uint32_t at = lane < m ? a.pos[c0 + lane] : 0;
+    for (uint32_t u0 = 0; u0 < m; u0 += U) {
+      Raw8<DDT> r[U];
+      uint32_t k[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        k[u] = u0 + u < m ? __builtin_amdgcn_readlane(key, u0 + u) : none;
+        const uint32_t p = __builtin_amdgcn_readlane(at, (u0 + u) & 63);
+        if (k[u] != none && in > 0)
+          r[u] = load8_raw<DDT>(a.dout.data + (static_cast<uint64_t>(p) * a.dout.stride + 8ull * g) * kEsz<DDT>, in);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k[u] == none) continue;  // behind the last token, or outside the table
+        if (k[u] != cur) {
+          flush(false);
+          open_left = c0 == b0 && u0 + u == 0 && k[u] == left;
+          cur = k[u];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+        }
+        float f[8];
+        if (in > 0) {
+          unpack8<DDT>(r[u], f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] += f[e];
+        }
+      }
+    }
+  }
+  flush(cur == right);
+}
+
+// Zeros into the rows of the table that no token has.
+template <int GDT>
+__device__ void fill_rows(const SumArgs& a, uint64_t block) {
+  __shared__ uint64_t touched;
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t r0 = block * kFillRows;
+  if (wave == 0) {  // each lane looks for its row among the sorted tokens
+    uint64_t lo = 0, hi = a.n;
+    const uint64_t row = r0 + lane;
+    while (__ballot(lo < hi)) {
+      const uint64_t mid = (lo + hi) / 2;
+      const bool on = lo < hi;
+      const uint32_t k = on ? a.keys[mid] : 0;
+      if (on && k < row) lo = mid + 1;
+      else if (on) hi = mid;
+    }
+    const uint64_t found = __ballot(lo < a.n && a.keys[lo < a.n ? lo : 0] == row);
+    if (lane == 0) touched = found;
+  }
+  __syncthreads();
+  const uint64_t skip = touched;
+  __syncthreads();  // a block that takes another range writes it anew
+  const float zero[8] = {};
+  const uint32_t groups = (a.dim + 7) / 8;
+  for (uint32_t i = wave; i < kFillRows && r0 + i < a.vocab; i += kSumThreads / 64) {
+    if (skip >> i & 1) continue;
+    const uint64_t p = a.dw.data + (r0 + i) * a.dw.stride * kEsz<GDT>;
+    for (uint32_t g = lane; g < groups; g += 64) store8<GDT>(p + 8ull * kEsz<GDT> * g, zero, in_group(a.dim, g));
+  }
+}
+
+template <int DDT, int GDT>
+__global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(SumArgs a, uint64_t sum_blocks, uint64_t fill_blocks) {
+  for (uint64_t b = blockIdx.x; b < sum_blocks + fill_blocks; b += gridDim.x) {
+    if (b < sum_blocks) {
+      const uint64_t item = b * (kSumThreads / 64) + (threadIdx.x >> 6);
+      if (item < static_cast<uint64_t>(a.tiles) * a.chunks) sum_tile<DDT, GDT>(a, item);
+    } else {
+      fill_rows<GDT>(a, b - sum_blocks);
+    }
+  }
+}
+
+// The row that begins in `tile` and goes on behind it.  Its four waves add a
+// quarter of the tiles each, then the first adds the quarters in order.
+template <int GDT>
+__global__ __launch_bounds__(kSumThreads) void embed_join_kernel(SumArgs a) {
+  constexpr uint32_t W = kSumThreads / 64;
+  __shared__ float sums[W][kSumCols];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t items = static_cast<uint64_t>(a.tiles - 1) * a.chunks;  // the last tile has none
+  for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t tile = static_cast<uint32_t>(item / a.chunks), chunk = static_cast<uint32_t>(item % a.chunks);
+    const uint64_t b0 = static_cast<uint64_t>(tile) * a.run, b1 = b0 + a.run;  // b1 < n: not the last tile
+    const uint32_t key = a.keys[b1 - 1];
+    if (key == a.vocab || a.keys[b1] != key || (b0 && a.keys[b0 - 1] == key)) continue;
+    // the last tile that holds the row: tiles whose first position has it are consecutive
+    uint32_t lo = tile + 1, hi = a.tiles - 1;
+    while (lo < hi) {
+      const uint32_t mid = (lo + hi + 1) / 2;
+      if (a.keys[static_cast<uint64_t>(mid) * a.run] == key) lo = mid;
+      else hi = mid - 1;
+    }
+    const uint32_t count = lo - tile + 1;  // [tile][1], then [tile + 1][0] to [lo][0]
+    const uint32_t g = chunk * (kSumCols / 8) + lane;
+    const int in = in_group(a.dim, g);
+    float acc[8] = {};
+    const uint32_t j1 = static_cast<uint32_t>(static_cast<uint64_t>(count) * (wave + 1) / W);
+    for (uint32_t j = static_cast<uint32_t>(static_cast<uint64_t>(count) * wave / W); j < j1; ++j) {
+      if (in <= 0) break;
+      float f[8];
+      const float* p = j ? sum_part(a, tile + j, 0) : sum_part(a, tile, 1);
+      unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(p) + 32ull * g, in), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += f[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (wave == 0 && in > 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        for (uint32_t w = 1; w < W; ++w) acc[e] += sums[w][e * 64 + lane];
+      sum_write<GDT>(a, key, g, acc, in);
+    }
+    __syncthreads();
+  }
+}
+
+uint64_t pad256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+struct BwdRegions {
+  uint64_t keys[2], pos[2], hist, part, end;
+  uint32_t run, tiles;
+};
+BwdRegions bwd_regions(uint64_t n, uint64_t dim) {
+  BwdRegions r{};
+  r.run = sum_run(n);
+  r.tiles = static_cast<uint32_t>((n + r.run - 1) / r.run);
+  const bool radix = n > kRankTokens;
+  const uint64_t list = pad256(n * 4);
+  uint64_t at = 0;
+  for (int i = 0; i < (radix ? 2 : 1); ++i) {
+    r.keys[i] = at;
+    r.pos[i] = at + list;
+    at += 2 * list;
+  }
+  r.hist = at;
+  if (radix) at += pad256((n + sort_tile(n) - 1) / sort_tile(n) * kDigits * 4);
+  r.part = at;
+  if (r.tiles > 1) at += pad256(static_cast<uint64_t>(r.tiles) * 2 * dim * 4);
+  r.end = at;
+  return r;
+}
+
+template <int WDT>
+hipError_t embed_fwd_of(const EmbedFwd& a, hipStream_t st) {
+  const uint32_t groups = (a.dim + 7) / 8;
+  uint32_t lg = 0;
+  while ((1u << lg) < groups && (1u << lg) < kEmbedThreads) ++lg;
+  const uint64_t per_block = kEmbedThreads >> lg;
+  const uint32_t grid = grid_for((a.n + per_block - 1) / per_block, kEmbedThreads);
+  if (a.out_dtype == kBf16)
+    hipLaunchKernelGGL((embed_fwd_kernel<WDT, kBf16>), dim3(grid), dim3(kEmbedThreads), 0, st, a, lg);
+  else
+    hipLaunchKernelGGL((embed_fwd_kernel<WDT, kF32>), dim3(grid), dim3(kEmbedThreads), 0, st, a, lg);
+  return hipGetLastError();
+}
+
+template <int DDT, int GDT>
+hipError_t embed_sums(const SumArgs& s, hipStream_t st) {
+  const uint64_t items = static_cast<uint64_t>(s.tiles) * s.chunks;
+  const uint64_t sum_blocks = (items + kSumThreads / 64 - 1) / (kSumThreads / 64);
+  const uint64_t fill_blocks = s.accumulate ? 0 : (s.vocab + kFillRows - 1) / kFillRows;
+  if (sum_blocks + fill_blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL((embed_sum_kernel<DDT, GDT>), dim3(grid_for(sum_blocks + fill_blocks, kSumThreads)),
+                     dim3(kSumThreads), 0, st, s, sum_blocks, fill_blocks);
+  if (s.tiles > 1)
+    hipLaunchKernelGGL((embed_join_kernel<GDT>),
+                       dim3(grid_for(static_cast<uint64_t>(s.tiles - 1) * s.chunks, kSumThreads)), dim3(kSumThreads), 0,
+                       st, s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_embed_fwd(const EmbedFwd& a, hipStream_t st) {
+  return a.w_dtype == kBf16 ? embed_fwd_of<kBf16>(a, st) : embed_fwd_of<kF32>(a, st);
+}
+
+uint64_t embed_bwd_workspace(uint64_t n, uint64_t dim) { return bwd_regions(n, dim).end; }
+
+hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
+  const BwdRegions r = bwd_regions(a.n, a.dim);
+  uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(a.ws + r.keys[0]), reinterpret_cast<uint32_t*>(a.ws + r.keys[1])};
+  uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(a.ws + r.pos[0]), reinterpret_cast<uint32_t*>(a.ws + r.pos[1])};
+  int sorted = 0;
+  if (a.n > kRankTokens) {
+    uint32_t* hist = reinterpret_cast<uint32_t*>(a.ws + r.hist);
+    const uint32_t tile = sort_tile(a.n);
+    const uint32_t grid = grid_for((a.n + tile - 1) / tile, kSortThreads);
+    int from = -1;
+    for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += kDigitBits) {  // keys 0 to vocab
+      const int to = from == 0 ? 1 : 0;
+      const uint32_t* ki = from < 0 ? nullptr : keys[from];
+      const uint32_t* pi = from < 0 ? nullptr : pos[from];
+      hipLaunchKernelGGL(embed_count_kernel, dim3(grid), dim3(kSortThreads), 0, st, a, ki, shift, tile, hist);
+      hipLaunchKernelGGL(embed_scatter_kernel, dim3(grid), dim3(kSortThreads), 0, st, a, ki, pi, shift, tile,
+                         static_cast<const uint32_t*>(hist), keys[to], pos[to]);
+      from = to;
+    }
+    sorted = from;
+  } else if (a.n > 0) {
+    const uint32_t grid = grid_for((a.n + kRankOwn - 1) / kRankOwn, kRankThreads);
+    hipLaunchKernelGGL(embed_rank_kernel, dim3(grid), dim3(kRankThreads), 0, st, a, keys[0], pos[0]);
+  }
+  SumArgs s;
+  s.dout = a.dout;
+  s.dw = a.dw;
+  s.keys = keys[sorted];
+  s.pos = pos[sorted];
+  s.part = reinterpret_cast<float*>(a.ws + r.part);
+  s.n = a.n;
+  s.vocab = a.vocab;
+  s.dim = a.dim;
+  s.run = r.run;
+  s.tiles = r.tiles;
+  s.chunks = (a.dim + kSumCols - 1) / kSumCols;
+  s.scale = a.scale;
+  s.accumulate = a.accumulate;
+  if (a.dout_dtype == kBf16)
+    return a.dw_dtype == kBf16 ? embed_sums<kBf16, kBf16>(s, st) : embed_sums<kBf16, kF32>(s, st);
+  return a.dw_dtype == kBf16 ? embed_sums<kF32, kBf16>(s, st) : embed_sums<kF32, kF32>(s, st);
+}
+
+}  // namespace lc

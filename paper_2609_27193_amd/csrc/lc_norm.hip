@@ -1,0 +1,442 @@
+// Layer norm and RMS norm of rows, forward and backward.
+//
+//   n = (x - mean) * rstd,  rstd = 1 / sqrt(var + eps)     (RMS: mean 0, var = mean of x^2)
+//   y = n * w + b
+//   g = dy * w;  dx = rstd * (g - mean(g) - n * mean(g * n))     (RMS: without mean(g))
+//   dw = sum over rows of dy * n;  db = sum over rows of dy
+//
+// Bound by memory: a row is read once and stays in registers, the variance is
+// taken about the mean found before it, sums are fp32.  The forward pass may
+// keep n in 8 bits, and the backward pass take it from there instead of x.  The
+// sums over rows are split over blocks and joined in a fixed order.
+#include "lc_ops_device.h"
+
+namespace lc {
+namespace {
+
+// TPR threads a row, NV groups of eight elements a thread.
+template <int TPR>
+constexpr uint32_t kNormThreads = TPR < 256 ? 256 : TPR;
+
+// Sums of (a, b) over the TPR threads of a row, in each of them.  `red` holds
+// two sets of slots used in turn: a set is written again only behind the next
+// call's barrier.
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float2 (&red)[2][kNormThreads<TPR> / 64], uint32_t& turn) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (TPR > 64) {
+    constexpr uint32_t W = TPR / 64;
+    const uint32_t wave = threadIdx.x >> 6, w0 = wave / W * W;
+    if ((threadIdx.x & 63) == 0) red[turn][wave] = make_float2(a, b);
+    __syncthreads();
+    a = red[turn][w0].x;
+    b = red[turn][w0].y;
+#pragma unroll
+    for (uint32_t w = 1; w < W; ++w) {
+      a += red[turn][w0 + w].x;
+      b += red[turn][w0 + w].y;
+    }
+    turn ^= 1;
+  }
+}
+template <int TPR>
+__device__ __forceinline__ float row_sum(float a, float2 (&red)[2][kNormThreads<TPR> / 64], uint32_t& turn) {
+  float b = 0;
+  row_sum2<TPR>(a, b, red, turn);
+  return a;
+}
+
+__device__ __forceinline__ void load_params8(uint64_t p, int dtype, uint32_t g, int n, float other, float (&f)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = p && e < n ? load_param(p, 8ull * g + e, dtype) : other;
+}
+
+template <int DT, bool LAYER, int TPR, int NV>
+__global__ __launch_bounds__(kNormThreads<TPR>) void norm_fwd_kernel(NormFwd a) {
+  constexpr uint32_t RPB = kNormThreads<TPR> / TPR;
+  __shared__ float2 red[2][kNormThreads<TPR> / 64];
+  uint32_t turn = 0;
+  const uint32_t t = threadIdx.x % TPR;
+  const float inv_dim = 1.0f / static_cast<float>(a.dim);
+  float w[NV][8], b[LAYER ? NV : 1][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const uint32_t g = i * TPR + t;
+    load_params8(a.weight, a.param_dtype, g, in_group(a.dim, g), 1.0f, w[i]);
+    if constexpr (LAYER) load_params8(a.bias, a.param_dtype, g, in_group(a.dim, g), 0.0f, b[i]);
+  }
+  const uint64_t items = (a.rows + RPB - 1) / RPB;
+  for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const uint64_t row = it * RPB + threadIdx.x / TPR;
+    const bool on = row < a.rows;  // the others only take part in the barriers
+    float v[NV][8];
+    float sum = 0, unused = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t g = i * TPR + t;
+      const int n = on ? in_group(a.dim, g) : 0;
+      unpack8<DT>(load8_raw<DT>(a.x.data + (row * a.x.stride + 8ull * g) * kEsz<DT>, n), v[i]);
+      if constexpr (LAYER) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[i][e];
+      }
+    }
+    float mean = 0;
+    if constexpr (LAYER) mean = row_sum<TPR>(sum, red, turn) * inv_dim;
+    float sq = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int n = in_group(a.dim, i * TPR + t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (LAYER) v[i][e] = e < n ? v[i][e] - mean : 0.0f;
+        sq = __builtin_fmaf(v[i][e], v[i][e], sq);
+      }
+    }
+    row_sum2<TPR>(sq, unused, red, turn);
+    const float rstd = 1.0f / sqrtf(sq * inv_dim + a.eps);
+    if (!on) continue;
+    if (t == 0) {
+      if (LAYER && a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t g = i * TPR + t;
+      const int n = in_group(a.dim, g);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[i][e] *= rstd;
+        y[e] = v[i][e] * w[i][e];
+        if constexpr (LAYER) y[e] += b[i][e];
+      }
+      store8<DT>(a.y.data + (row * a.y.stride + 8ull * g) * kEsz<DT>, y, n);
+      if (a.kept.codes) {
+        if (n < 8) {  // what is no element must not set its block's power: a NaN row has one here, too
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[i][e] = e < n ? v[i][e] : 0.0f;
+        }
+        uint32_t code;
+        const u32x2 q = act_encode8(v[i], code);
+        store_kept8(a.kept, row, g, n, q, code);
+      }
+    }
+  }
+}
+
+// Rows of any length: read again for each of the three steps.
+constexpr uint32_t kLongThreads = 1024;
+template <int DT, bool LAYER>
+__global__ __launch_bounds__(kLongThreads) void norm_fwd_long_kernel(NormFwd a) {
+  __shared__ float2 red[2][kLongThreads / 64];
+  uint32_t turn = 0;
+  const float inv_dim = 1.0f / static_cast<float>(a.dim);
+  const uint32_t groups = (a.dim + 31) / 32 * 4;  // whole quads, so that a block's four lanes stay together
+  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const uint64_t src = a.x.data + row * a.x.stride * kEsz<DT>;
+    float mean = 0, sum = 0, unused = 0;
+    float v[8];
+    if constexpr (LAYER) {
+      for (uint32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+        unpack8<DT>(load8_raw<DT>(src + 8ull * g * kEsz<DT>, in_group(a.dim, g)), v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[e];
+      }
+      mean = row_sum<kLongThreads>(sum, red, turn) * inv_dim;
+    }
+    float sq = 0;
+    for (uint32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+      const int n = in_group(a.dim, g);
+      unpack8<DT>(load8_raw<DT>(src + 8ull * g * kEsz<DT>, n), v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = e < n ? v[e] - mean : 0.0f;
+        sq = __builtin_fmaf(d, d, sq);
+      }
+    }
+    row_sum2<kLongThreads>(sq, unused, red, turn);
+    const float rstd = 1.0f / sqrtf(sq * inv_dim + a.eps);
+    if (threadIdx.x == 0) {
+      if (LAYER && a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+    for (uint32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+      const int n = in_group(a.dim, g);
+      unpack8<DT>(load8_raw<DT>(src + 8ull * g * kEsz<DT>, n), v);
+      float w[8], b[8], y[8];
+      load_params8(a.weight, a.param_dtype, g, n, 1.0f, w);
+      load_params8(LAYER ? a.bias : 0, a.param_dtype, g, n, 0.0f, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = e < n ? (v[e] - mean) * rstd : 0.0f;
+        y[e] = v[e] * w[e] + b[e];
+      }
+      store8<DT>(a.y.data + (row * a.y.stride + 8ull * g) * kEsz<DT>, y, n);
+      if (a.kept.codes) {
+        uint32_t code;
+        const u32x2 q = act_encode8(v, code);
+        store_kept8(a.kept, row, g, n, q, code);
+      }
+    }
+  }
+}
+
+// ---- backward ------------------------------------------------------------------------
+// Partial sums of dw and db: `parts` rows of dim each, dw's first.
+constexpr uint32_t kNormBlocks = 512;
+struct NormParts {
+  uint32_t rpb;    // rows that a block takes at once
+  uint32_t parts;
+};
+
+template <int DT, bool KEPT>
+__device__ __forceinline__ void load_normed8(const NormBwd& a, uint64_t row, uint32_t g, int n, float mean, float rstd,
+                                             float (&f)[8]) {
+  if constexpr (KEPT) {
+    const float scale = n > 0 ? act_scale(load_kept_code(a.kept, row, g)) : 0.0f;
+    act_decode8(load_kept8(a.kept, row, g, n), scale, f);
+  } else {
+    unpack8<DT>(load8_raw<DT>(a.x.data + (row * a.x.stride + 8ull * g) * kEsz<DT>, n), f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (f[e] - mean) * rstd;
+  }
+  if (n < 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = e < n ? f[e] : 0.0f;
+  }
+}
+
+template <int DT, bool LAYER, bool KEPT, int TPR, int NV>
+__global__ __launch_bounds__(kNormThreads<TPR>) void norm_bwd_kernel(NormBwd a, uint32_t parts) {
+  constexpr uint32_t RPB = kNormThreads<TPR> / TPR;
+  __shared__ float2 red[2][kNormThreads<TPR> / 64];
+  uint32_t turn = 0;
+  const uint32_t t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const float inv_dim = 1.0f / static_cast<float>(a.dim);
+  float w[NV][8], dw[NV][8], db[LAYER ? NV : 1][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const uint32_t g = i * TPR + t;
+    load_params8(a.weight, a.param_dtype, g, in_group(a.dim, g), 1.0f, w[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dw[i][e] = 0;
+      if constexpr (LAYER) db[i][e] = 0;
+    }
+  }
+  const uint64_t items = (a.rows + RPB - 1) / RPB;
+  for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const uint64_t row = it * RPB + sub;
+    const bool on = row < a.rows;
+    const float rstd = on ? a.rstd[row] : 0.0f, mean = on && LAYER && !KEPT ? a.mean[row] : 0.0f;
+    float n[NV][8], d[NV][8];
+    float c1 = 0, c2 = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t g = i * TPR + t;
+      const int in = on ? in_group(a.dim, g) : 0;
+      unpack8<DT>(load8_raw<DT>(a.dy.data + (row * a.dy.stride + 8ull * g) * kEsz<DT>, in), d[i]);
+      load_normed8<DT, KEPT>(a, row, g, in, mean, rstd, n[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dw[i][e] = __builtin_fmaf(d[i][e], n[i][e], dw[i][e]);
+        if constexpr (LAYER) db[i][e] += d[i][e];
+        d[i][e] *= w[i][e];
+        if constexpr (LAYER) c1 += d[i][e];
+        c2 = __builtin_fmaf(d[i][e], n[i][e], c2);
+      }
+    }
+    if (!a.dx.data) continue;  // uniform: every thread of the grid goes on
+    row_sum2<TPR>(c1, c2, red, turn);
+    c1 *= inv_dim;
+    c2 *= inv_dim;
+    if (!on) continue;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t g = i * TPR + t;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[i][e] = rstd * (d[i][e] - c1 - n[i][e] * c2);
+      store8<DT>(a.dx.data + (row * a.dx.stride + 8ull * g) * kEsz<DT>, d[i], in_group(a.dim, g));
+    }
+  }
+  if (!a.part) return;
+  float* out = a.part + (blockIdx.x * RPB + sub) * static_cast<uint64_t>(a.dim);
+  const uint64_t db_off = static_cast<uint64_t>(parts) * a.dim;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const uint32_t g = i * TPR + t;
+    const int in = in_group(a.dim, g);
+    store8<kF32>(reinterpret_cast<uint64_t>(out) + 32ull * g, dw[i], in);
+    if constexpr (LAYER) store8<kF32>(reinterpret_cast<uint64_t>(out + db_off) + 32ull * g, db[i], in);
+  }
+}
+
+// Rows of any length: a block's partial sums stay in its part of the
+// workspace, each element with the thread that it belongs to.
+template <int DT, bool LAYER, bool KEPT>
+__global__ __launch_bounds__(kLongThreads) void norm_bwd_long_kernel(NormBwd a, uint32_t parts) {
+  __shared__ float2 red[2][kLongThreads / 64];
+  uint32_t turn = 0;
+  const float inv_dim = 1.0f / static_cast<float>(a.dim);
+  const uint32_t groups = (a.dim + 7) / 8;
+  float* out = a.part ? a.part + blockIdx.x * static_cast<uint64_t>(a.dim) : nullptr;
+  const uint64_t db_off = static_cast<uint64_t>(parts) * a.dim;
+  bool first = true;
+  for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float rstd = a.rstd[row], mean = LAYER && !KEPT ? a.mean[row] : 0.0f;
+    float c1 = 0, c2 = 0;
+    float n[8], d[8], w[8];
+    for (uint32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+      const int in = in_group(a.dim, g);
+      unpack8<DT>(load8_raw<DT>(a.dy.data + (row * a.dy.stride + 8ull * g) * kEsz<DT>, in), d);
+      load_normed8<DT, KEPT>(a, row, g, in, mean, rstd, n);
+      load_params8(a.weight, a.param_dtype, g, in, 1.0f, w);
+      if (out) {
+        const uint64_t pw = reinterpret_cast<uint64_t>(out) + 32ull * g;
+        const uint64_t pb = reinterpret_cast<uint64_t>(out + db_off) + 32ull * g;
+        float s[8] = {}, r[8] = {};
+        if (!first) {
+          unpack8<kF32>(load8_raw<kF32>(pw, in), s);
+          if constexpr (LAYER) unpack8<kF32>(load8_raw<kF32>(pb, in), r);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s[e] = __builtin_fmaf(d[e], n[e], s[e]);
+          r[e] += d[e];
+        }
+        store8<kF32>(pw, s, in);
+        if constexpr (LAYER) store8<kF32>(pb, r, in);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float gw = d[e] * w[e];
+        if constexpr (LAYER) c1 += gw;
+        c2 = __builtin_fmaf(gw, n[e], c2);
+      }
+    }
+    first = false;
+    if (!a.dx.data) continue;
+    row_sum2<kLongThreads>(c1, c2, red, turn);
+    c1 *= inv_dim;
+    c2 *= inv_dim;
+    for (uint32_t g = threadIdx.x; g < groups; g += kLongThreads) {
+      const int in = in_group(a.dim, g);
+      unpack8<DT>(load8_raw<DT>(a.dy.data + (row * a.dy.stride + 8ull * g) * kEsz<DT>, in), d);
+      load_normed8<DT, KEPT>(a, row, g, in, mean, rstd, n);
+      load_params8(a.weight, a.param_dtype, g, in, 1.0f, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = rstd * (d[e] * w[e] - c1 - n[e] * c2);
+      store8<DT>(a.dx.data + (row * a.dx.stride + 8ull * g) * kEsz<DT>, d, in);
+    }
+  }
+}
+
+// Column sums of the parts: 64 columns a block, 16 slices of the parts, joined
+// in order.  blockIdx.y: dw, db.
+constexpr uint32_t kJoinSlices = 16;
+__global__ __launch_bounds__(64 * kJoinSlices) void norm_join_kernel(NormBwd a, uint32_t parts) {
+  __shared__ float sums[kJoinSlices][64];
+  const uint32_t lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
+  const uint64_t dst = blockIdx.y ? a.dbias : a.dweight;
+  if (!dst) return;
+  const float* src = a.part + static_cast<uint64_t>(blockIdx.y) * parts * a.dim;
+  for (uint64_t c0 = blockIdx.x * 64ull; c0 < a.dim; c0 += gridDim.x * 64ull) {
+    const uint64_t c = c0 + lane;
+    float s = 0;
+    if (c < a.dim)
+      for (uint32_t p = slice; p < parts; p += kJoinSlices) s += src[p * static_cast<uint64_t>(a.dim) + c];
+    sums[slice][lane] = s;
+    __syncthreads();
+    if (slice == 0 && c < a.dim) {
+#pragma unroll
+      for (uint32_t i = 1; i < kJoinSlices; ++i) s += sums[i][lane];
+      if (a.accumulate) s += load_param(dst, c, a.grad_dtype);
+      store_param(dst, c, a.grad_dtype, s);
+    }
+    __syncthreads();
+  }
+}
+
+// The shapes of row kernels: the smallest that holds a row.
+constexpr uint32_t kNormLongest = 16384;
+uint32_t rows_per_block(uint64_t dim) { return dim <= 1024 ? 4 : dim <= 2048 ? 2 : 1; }
+
+NormParts norm_parts(uint64_t rows, uint64_t dim) {
+  NormParts p;
+  p.rpb = rows_per_block(dim);
+  const uint64_t items = (rows + p.rpb - 1) / p.rpb;
+  uint64_t blocks = items < kNormBlocks ? items : kNormBlocks;
+  if (LC_MAX_GRID_BLOCKS > 0 && blocks > LC_MAX_GRID_BLOCKS) blocks = LC_MAX_GRID_BLOCKS;
+  p.parts = static_cast<uint32_t>(blocks * p.rpb);
+  return p;
+}
+
+template <int DT, bool LAYER>
+hipError_t norm_fwd_of(const NormFwd& a, hipStream_t st) {
+  const uint32_t rpb = rows_per_block(a.dim);
+  const uint64_t items = (a.rows + rpb - 1) / rpb;
+#define LC_NORM_FWD(TPR, NV)                                                                                   \
+  hipLaunchKernelGGL((norm_fwd_kernel<DT, LAYER, TPR, NV>), dim3(grid_for(items, kNormThreads<TPR>)),          \
+                     dim3(kNormThreads<TPR>), 0, st, a)
+  if (a.dim <= 512) LC_NORM_FWD(64, 1);
+  else if (a.dim <= 1024) LC_NORM_FWD(64, 2);
+  else if (a.dim <= 2048) LC_NORM_FWD(128, 2);
+  else if (a.dim <= 4096) LC_NORM_FWD(256, 2);
+  else if (a.dim <= 6144) LC_NORM_FWD(256, 3);
+  else if (a.dim <= 8192) LC_NORM_FWD(512, 2);
+  else if (a.dim <= kNormLongest) LC_NORM_FWD(1024, 2);
+  else
+    hipLaunchKernelGGL((norm_fwd_long_kernel<DT, LAYER>), dim3(grid_for(a.rows, kLongThreads)), dim3(kLongThreads), 0,
+                       st, a);
+#undef LC_NORM_FWD
+  return hipGetLastError();
+}
+
+template <int DT, bool LAYER, bool KEPT>
+void norm_bwd_of(const NormBwd& a, const NormParts& p, hipStream_t st) {
+  const uint32_t grid = p.parts / p.rpb;
+#define LC_NORM_BWD(TPR, NV)                                                                                   \
+  hipLaunchKernelGGL((norm_bwd_kernel<DT, LAYER, KEPT, TPR, NV>), dim3(grid), dim3(kNormThreads<TPR>), 0, st, a, p.parts)
+  if (a.dim <= 512) LC_NORM_BWD(64, 1);
+  else if (a.dim <= 1024) LC_NORM_BWD(64, 2);
+  else if (a.dim <= 2048) LC_NORM_BWD(128, 2);
+  else if (a.dim <= 4096) LC_NORM_BWD(256, 2);
+  else if (a.dim <= 6144) LC_NORM_BWD(256, 3);
+  else if (a.dim <= 8192) LC_NORM_BWD(512, 2);
+  else if (a.dim <= kNormLongest) LC_NORM_BWD(1024, 2);
+  else
+    hipLaunchKernelGGL((norm_bwd_long_kernel<DT, LAYER, KEPT>), dim3(grid), dim3(kLongThreads), 0, st, a, p.parts);
+#undef LC_NORM_BWD
+}
+
+}  // namespace
+
+hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t st) {
+  if (a.rows == 0) return hipSuccess;
+  if (a.dtype == kBf16) return a.layer ? norm_fwd_of<kBf16, true>(a, st) : norm_fwd_of<kBf16, false>(a, st);
+  return a.layer ? norm_fwd_of<kF32, true>(a, st) : norm_fwd_of<kF32, false>(a, st);
+}
+
+uint64_t norm_bwd_workspace(uint64_t rows, uint64_t dim) { return norm_parts(rows, dim).parts * 2ull * dim * 4; }
+
+hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t st) {
+  const NormParts p = norm_parts(a.rows, a.dim);
+  if (a.rows > 0 && (a.part || a.dx.data)) {
+    const bool kept = a.kept.codes != 0;
+    if (a.dtype == kBf16) {
+      if (a.layer) kept ? norm_bwd_of<kBf16, true, true>(a, p, st) : norm_bwd_of<kBf16, true, false>(a, p, st);
+      else kept ? norm_bwd_of<kBf16, false, true>(a, p, st) : norm_bwd_of<kBf16, false, false>(a, p, st);
+    } else {
+      if (a.layer) kept ? norm_bwd_of<kF32, true, true>(a, p, st) : norm_bwd_of<kF32, true, false>(a, p, st);
+      else kept ? norm_bwd_of<kF32, false, true>(a, p, st) : norm_bwd_of<kF32, false, false>(a, p, st);
+    }
+  }
+  if (a.dweight || a.dbias)
+    hipLaunchKernelGGL(norm_join_kernel, dim3(grid_for((a.dim + 63) / 64, 64 * kJoinSlices), a.dbias ? 2 : 1),
+                       dim3(64 * kJoinSlices), 0, st, a, p.parts);
+  return hipGetLastError();
+}
+
+}  // namespace lc

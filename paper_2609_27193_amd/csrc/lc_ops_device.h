@@ -1,0 +1,233 @@
+// Device helpers shared by the training operators' kernels: rows in groups of
+// eight elements at any element address, sums over a wave and a block, and
+// the 8-bit form of a kept activation.
+#pragma once
+
+#include "lc_device.h"
+#include "lc_ops.h"
+
+namespace lc {
+namespace {
+
+constexpr int kBf16 = 1;
+constexpr int kF32 = 2;
+template <int DT>
+constexpr uint32_t kEsz = DT == kBf16 ? 2 : 4;
+
+// fp32 to bf16, to nearest, halves to even; a NaN stays one.
+__device__ __forceinline__ uint16_t to_bf16(float f) {
+  uint32_t u = __float_as_uint(f);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7FC0u;
+  u += 0x7FFFu + ((u >> 16) & 1u);
+  return static_cast<uint16_t>(u >> 16);
+}
+
+// The same for two at once, in the instruction that gfx950 has for it.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+typedef const __attribute__((address_space(1))) u32x4_any2 gc_u32x4_any2;
+typedef const __attribute__((address_space(1))) u32x4_any4 gc_u32x4_any4;
+typedef const __attribute__((address_space(1))) uint16_t gc_u16;
+typedef const __attribute__((address_space(1))) float gc_f32;
+
+template <int DT>
+__device__ __forceinline__ float load1(uint64_t p) {
+  if constexpr (DT == kBf16) return __uint_as_float(static_cast<uint32_t>(*(gc_u16*)p) << 16);
+  else return *(gc_f32*)p;
+}
+template <int DT>
+__device__ __forceinline__ void store1(uint64_t p, float v) {
+  if constexpr (DT == kBf16) *(g_u16*)p = to_bf16(v);
+  else *(g_f32*)p = v;
+}
+// One element of a small array whose type only the call knows.
+__device__ __forceinline__ float load_param(uint64_t p, uint64_t i, int dtype) {
+  return dtype == kBf16 ? load1<kBf16>(p + 2 * i) : load1<kF32>(p + 4 * i);
+}
+__device__ __forceinline__ void store_param(uint64_t p, uint64_t i, int dtype, float v) {
+  if (dtype == kBf16) store1<kBf16>(p + 2 * i, v);
+  else store1<kF32>(p + 4 * i, v);
+}
+
+// Eight elements as they lie in memory: 16 or 32 bytes, at any element.
+template <int DT>
+struct Raw8 {
+  u32x4 v[DT == kBf16 ? 1 : 2];
+};
+template <int DT>
+__device__ __forceinline__ Raw8<DT> load8_raw(uint64_t p) {
+  Raw8<DT> r;
+  if constexpr (DT == kBf16) {
+    r.v[0] = *(gc_u32x4_any2*)p;
+  } else {
+    r.v[0] = *(gc_u32x4_any4*)p;
+    r.v[1] = *(gc_u32x4_any4*)(p + 16);
+  }
+  return r;
+}
+// The first n of the eight, zeros behind them (a row's last group).
+template <int DT>
+__device__ __forceinline__ Raw8<DT> load8_raw(uint64_t p, int n) {
+  if (n >= 8) return load8_raw<DT>(p);
+  Raw8<DT> r;
+  for (auto& q : r.v) q = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 7; ++i) {
+    if (i >= n) break;
+    if constexpr (DT == kBf16)
+      r.v[0][i / 2] |= static_cast<uint32_t>(*(gc_u16*)(p + 2 * i)) << (16 * (i & 1));
+    else
+      r.v[i / 4][i % 4] = __float_as_uint(*(gc_f32*)(p + 4 * i));
+  }
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ void unpack8(const Raw8<DT>& r, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (DT == kBf16) f[i] = i & 1 ? bf_hi(r.v[0][i / 2]) : bf_lo(r.v[0][i / 2]);
+    else f[i] = __uint_as_float(r.v[i / 4][i % 4]);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store8(uint64_t p, const float (&f)[8], int n) {
+  if (n >= 8) {
+    if constexpr (DT == kBf16) {
+      const u32x4 v = {pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+      *(g_u32x4_any2*)p = v;
+    } else {
+      const u32x4 a = {__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+      const u32x4 b = {__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])};
+      *(g_u32x4_any4*)p = a;
+      *(g_u32x4_any4*)(p + 16) = b;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < n) store1<DT>(p + kEsz<DT> * i, f[i]);
+}
+// Elements of group g of a row of `dim` that exist (at most 0 when none does).
+__device__ __forceinline__ int in_group(uint32_t dim, uint32_t g) {
+  return static_cast<int>(dim) - static_cast<int>(g * 8u);
+}
+
+// ---- sums over a wave and a block, fixed order ---------------------------------
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ float dpp_f32(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xF, false));
+}
+// Sum over the 64 lanes, in every lane.
+__device__ __forceinline__ float wave_sum(float v) {
+  v += dpp_f32<0xB1>(v);        // lane ^ 1
+  v += dpp_f32<0x4E>(v);        // lane ^ 2
+  v += dpp_f32<0x141>(v);       // the other quad of each eight
+  v += dpp_f32<0x140>(v);       // the other half of each row
+  v += dpp_f32<0x142, 0xA>(v);  // row_bcast:15 into rows 1 and 3
+  v += dpp_f32<0x143, 0xC>(v);  // row_bcast:31 into rows 2 and 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// ---- the 8-bit form --------------------------------------------------------------
+// An element is a sign, 4 exponent and 3 mantissa bits (bias 7, largest value
+// 448, 0x7F not a number); the 32 elements of a block share the power of two
+// 2^(code - 127), the smallest that brings the largest finite one of them to
+// 448 or less.  A scaled element is rounded to nearest, halves to even: at
+// most 2^-4 of itself is lost, and no element saturates, except that under the
+// largest power that fp32 elements reach, 2^120, the codes end at 240, for
+// 256 * 2^120 would read back as an infinity.  An element that is not finite
+// becomes NaN and does not count for its block's power.
+constexpr uint32_t kActTopCode = 247;
+__device__ __forceinline__ uint32_t act_code(uint32_t top) {  // top: bits of the largest finite magnitude
+  const int c = static_cast<int>(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return static_cast<uint32_t>(c > 0 ? c : 0);
+}
+__device__ __forceinline__ float act_inverse(uint32_t code) { return __uint_as_float((254u - code) << 23); }
+__device__ __forceinline__ float act_scale(uint32_t code) {  // 2^-127 is below the normal range; 255 stands for NaN
+  return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7FC00000u : code << 23);
+}
+// Eight neighbours of a block whose four groups of eight lie in one quad of
+// lanes: the eight bytes, and the block's code in every lane of the quad.
+__device__ __forceinline__ u32x2 act_encode8(const float (&f)[8], uint32_t& code) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t a = __float_as_uint(f[i]) & 0x7fffffffu;
+    if (a < 0x7f800000u && a > top) top = a;
+  }
+  uint32_t o = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(top), 0xB1, 0xF, 0xF, false));
+  top = o > top ? o : top;
+  o = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(top), 0x4E, 0xF, 0xF, false));
+  top = o > top ? o : top;
+  code = act_code(top);
+  const float inv = act_inverse(code);
+  float q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    q[i] = (__float_as_uint(f[i]) & 0x7fffffffu) < 0x7f800000u ? f[i] * inv : __uint_as_float(0x7FC00000u);
+  if (code == kActTopCode) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = q[i] > 240.0f ? 240.0f : q[i] < -240.0f ? -240.0f : q[i];
+  }
+  int lo = 0, hi = 0;
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], hi, true);
+  return u32x2{static_cast<uint32_t>(lo), static_cast<uint32_t>(hi)};
+}
+__device__ __forceinline__ void act_decode8(u32x2 b, float scale, float (&f)[8]) {
+  const f32x2 p0 = __builtin_amdgcn_cvt_pk_f32_fp8(b[0], false), p1 = __builtin_amdgcn_cvt_pk_f32_fp8(b[0], true);
+  const f32x2 p2 = __builtin_amdgcn_cvt_pk_f32_fp8(b[1], false), p3 = __builtin_amdgcn_cvt_pk_f32_fp8(b[1], true);
+  f[0] = p0[0] * scale;
+  f[1] = p0[1] * scale;
+  f[2] = p1[0] * scale;
+  f[3] = p1[1] * scale;
+  f[4] = p2[0] * scale;
+  f[5] = p2[1] * scale;
+  f[6] = p3[0] * scale;
+  f[7] = p3[1] * scale;
+}
+
+typedef u32x2 __attribute__((aligned(1))) u32x2_any1;
+typedef __attribute__((address_space(1))) u32x2_any1 g_u32x2_any1;
+typedef const __attribute__((address_space(1))) u32x2_any1 gc_u32x2_any1;
+typedef __attribute__((address_space(1))) uint8_t g_u8;
+typedef const __attribute__((address_space(1))) uint8_t gc_u8;
+__device__ __forceinline__ u32x2 load_codes8(uint64_t p, int n) {
+  if (n >= 8) return *(gc_u32x2_any1*)p;
+  u32x2 r = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < n) r[i / 4] |= static_cast<uint32_t>(*(gc_u8*)(p + i)) << (8 * (i & 3));
+  return r;
+}
+__device__ __forceinline__ void store_codes8(uint64_t p, u32x2 b, int n) {
+  if (n >= 8) {
+    *(g_u32x2_any1*)p = b;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < n) *(g_u8*)(p + i) = static_cast<uint8_t>(b[i / 4] >> (8 * (i & 3)));
+}
+// Group g of row r of a kept activation, and its block's scale.
+__device__ __forceinline__ u32x2 load_kept8(const Kept& k, uint64_t row, uint32_t g, int n) {
+  return load_codes8(k.codes + row * k.code_stride + 8ull * g, n);
+}
+__device__ __forceinline__ uint32_t load_kept_code(const Kept& k, uint64_t row, uint32_t g) {
+  return *(gc_u8*)(k.scales + row * k.scale_stride + g / 4);
+}
+__device__ __forceinline__ void store_kept8(const Kept& k, uint64_t row, uint32_t g, int n, u32x2 b, uint32_t code) {
+  if (n <= 0) return;
+  store_codes8(k.codes + row * k.code_stride + 8ull * g, b, n);
+  if (g % 4 == 0) *(g_u8*)(k.scales + row * k.scale_stride + g / 4) = static_cast<uint8_t>(code);
+}
+
+}  // namespace
+}  // namespace lc

@@ -27,12 +27,17 @@ LC_OK, LC_ERR_INVALID_ARG, LC_ERR_BAD_STATE, LC_ERR_CAPACITY, LC_ERR_NO_VERSION,
     LC_ERR_IO = range(8)
 LC_DT_BF16, LC_DT_F32 = 1, 2
 LC_MODE_ACCUM, LC_MODE_SNAPSHOT = 0, 1
+LC_IT_I32, LC_IT_I64 = 1, 2
+LC_NORM_LAYER, LC_NORM_RMS = 0, 1
 
 EXPORTED = ("lc_query_build", "lc_query_layout", "lc_init_layout", "lc_score_layers", "lc_select", "lc_pack_selected",
             "lc_restore_composite", "lc_rebase", "lc_adamw_step_score", "lc_sgd_step_score", "lc_store_open",
             "lc_store_append", "lc_store_append_async", "lc_store_sync", "lc_store_count", "lc_store_entry",
             "lc_store_plan", "lc_store_restore", "lc_store_compact", "lc_store_discard_after", "lc_store_close",
-            "lc_read_state", "lc_record_bytes", "lc_destroy", "lc_last_error", "lc_score_layers_static")
+            "lc_read_state", "lc_record_bytes", "lc_destroy", "lc_last_error", "lc_score_layers_static",
+            "lc_embedding_forward", "lc_embedding_backward", "lc_embedding_backward_workspace", "lc_act_save",
+            "lc_act_load", "lc_norm_forward", "lc_norm_backward", "lc_norm_backward_workspace", "lc_linear_wgrad",
+            "lc_linear_wgrad_workspace")
 
 
 class lc_segment(C.Structure):
@@ -76,6 +81,21 @@ class lc_adamw_params(C.Structure):
 
 class lc_sgd_params(C.Structure):
     _fields_ = [("lr", C.c_double), ("weight_decay", C.c_double)]
+
+
+class lc_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64), ("stride", C.c_uint64),
+                ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class lc_saved_act(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
+                ("code_stride", C.c_uint64), ("scale_stride", C.c_uint64)]
+
+
+class lc_norm_params(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("param_dtype", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("eps", C.c_double)]
 
 
 class LCError(RuntimeError):
@@ -127,6 +147,22 @@ def load_library(path: str = LIB_PATH):
             "lc_record_bytes": (C.c_uint64, [C.c_void_p, C.c_uint32]),
             "lc_destroy": (C.c_int, [C.c_void_p]),
             "lc_last_error": (C.c_char_p, []),
+            "lc_embedding_forward": (C.c_int, [P(lc_matrix), C.c_void_p, C.c_int32, C.c_uint64, C.c_int64, C.c_double,
+                                               P(lc_matrix), C.c_void_p]),
+            "lc_embedding_backward_workspace": (C.c_uint64, [C.c_uint64, C.c_uint64]),
+            "lc_embedding_backward": (C.c_int, [P(lc_matrix), C.c_void_p, C.c_int32, C.c_uint64, C.c_int64, C.c_double,
+                                                C.c_int32, P(lc_matrix), C.c_void_p, C.c_uint64, C.c_void_p]),
+            "lc_act_save": (C.c_int, [P(lc_matrix), P(lc_saved_act), C.c_void_p]),
+            "lc_act_load": (C.c_int, [P(lc_saved_act), P(lc_matrix), C.c_void_p]),
+            "lc_norm_forward": (C.c_int, [P(lc_norm_params), P(lc_matrix), P(lc_matrix), C.c_void_p, C.c_void_p,
+                                          P(lc_saved_act), C.c_void_p]),
+            "lc_norm_backward_workspace": (C.c_uint64, [C.c_uint64, C.c_uint64]),
+            "lc_norm_backward": (C.c_int, [P(lc_norm_params), P(lc_matrix), P(lc_matrix), C.c_void_p, C.c_void_p,
+                                           P(lc_saved_act), P(lc_matrix), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                           C.c_void_p, C.c_uint64, C.c_void_p]),
+            "lc_linear_wgrad_workspace": (C.c_uint64, [C.c_uint64, C.c_uint64, C.c_uint64]),
+            "lc_linear_wgrad": (C.c_int, [P(lc_matrix), P(lc_saved_act), C.c_void_p, C.c_void_p, C.c_int32,
+                                          P(lc_matrix), C.c_void_p, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
         }
         for name, (res, args) in sig.items():
             f = getattr(lib, name)
@@ -382,6 +418,84 @@ def lc_read_state(ctx, n_layers: int):
                                         d.ctypes.data_as(C.POINTER(C.c_double)),
                                         t.ctypes.data_as(C.POINTER(C.c_int64))), "lc_read_state")
     return u, d, t
+
+
+# ---- training operators: embedding, norms, activations kept in 8 bits, linear weight gradient ----------------------------
+
+ACT_BLOCK = 32  # columns of a row that share a scale in a kept activation
+
+
+def matrix(data: int, rows: int, cols: int, dtype: int, stride: int = 0) -> lc_matrix:
+    """Rows of elements in device memory; ``stride`` elements from row to row (0: ``cols``)."""
+    return lc_matrix(data or None, rows, cols, stride or cols, dtype, 0)
+
+
+def saved_act(codes: int, scales: int, rows: int, cols: int, code_stride: int = 0, scale_stride: int = 0) -> lc_saved_act:
+    """An activation kept in 8 bits: rows x cols bytes of codes, rows x ceil(cols / 32) bytes of scales."""
+    return lc_saved_act(codes or None, scales or None, rows, cols, code_stride or cols,
+                        scale_stride or -(-cols // ACT_BLOCK))
+
+
+def norm_params(kind: int, weight: int, bias: int, param_dtype: int, eps: float) -> lc_norm_params:
+    return lc_norm_params(kind, param_dtype, weight or None, bias or None, eps)
+
+
+def lc_embedding_forward(weight: lc_matrix, tokens: int, token_dtype: int, n_tokens: int, out: lc_matrix,
+                         scale: float = 1.0, first_token: int = 0, stream: int = 0) -> None:
+    _check(load_library().lc_embedding_forward(weight, tokens or None, token_dtype, n_tokens, first_token, scale, out,
+                                               stream or None), "lc_embedding_forward")
+
+
+def lc_embedding_backward_workspace(n_tokens: int, cols: int) -> int:
+    return load_library().lc_embedding_backward_workspace(n_tokens, cols)
+
+
+def lc_embedding_backward(dout: lc_matrix, tokens: int, token_dtype: int, n_tokens: int, dweight: lc_matrix,
+                          workspace: int, workspace_bytes: int, scale: float = 1.0, first_token: int = 0,
+                          accumulate: bool = False, stream: int = 0) -> None:
+    _check(load_library().lc_embedding_backward(dout, tokens or None, token_dtype, n_tokens, first_token, scale,
+                                                int(accumulate), dweight, workspace or None, workspace_bytes,
+                                                stream or None), "lc_embedding_backward")
+
+
+def lc_act_save(x: lc_matrix, saved: lc_saved_act, stream: int = 0) -> None:
+    _check(load_library().lc_act_save(x, saved, stream or None), "lc_act_save")
+
+
+def lc_act_load(saved: lc_saved_act, out: lc_matrix, stream: int = 0) -> None:
+    _check(load_library().lc_act_load(saved, out, stream or None), "lc_act_load")
+
+
+def lc_norm_forward(params: lc_norm_params, x: lc_matrix, y: lc_matrix, mean: Optional[int] = None,
+                    rstd: Optional[int] = None, saved: Optional[lc_saved_act] = None, stream: int = 0) -> None:
+    _check(load_library().lc_norm_forward(params, x, y, mean or None, rstd or None, saved, stream or None),
+           "lc_norm_forward")
+
+
+def lc_norm_backward_workspace(rows: int, cols: int) -> int:
+    return load_library().lc_norm_backward_workspace(rows, cols)
+
+
+def lc_norm_backward(params: lc_norm_params, dy: lc_matrix, rstd: int, dx: Optional[lc_matrix], dweight: Optional[int],
+                     dbias: Optional[int], grad_dtype: int, workspace: int, workspace_bytes: int,
+                     x: Optional[lc_matrix] = None, mean: Optional[int] = None, saved: Optional[lc_saved_act] = None,
+                     accumulate: bool = False, stream: int = 0) -> None:
+    """The normalised rows come from ``x`` (with ``mean`` for LC_NORM_LAYER) or from ``saved``."""
+    _check(load_library().lc_norm_backward(params, dy, x, mean or None, rstd or None, saved, dx, dweight or None,
+                                           dbias or None, grad_dtype, int(accumulate), workspace or None,
+                                           workspace_bytes, stream or None), "lc_norm_backward")
+
+
+def lc_linear_wgrad_workspace(rows: int, n: int, k: int) -> int:
+    return load_library().lc_linear_wgrad_workspace(rows, n, k)
+
+
+def lc_linear_wgrad(dy: lc_matrix, saved: lc_saved_act, dweight: lc_matrix, workspace: int, workspace_bytes: int,
+                    col_scale: Optional[int] = None, col_shift: Optional[int] = None, param_dtype: int = LC_DT_F32,
+                    dbias: Optional[int] = None, accumulate: bool = False, stream: int = 0) -> None:
+    _check(load_library().lc_linear_wgrad(dy, saved, col_scale or None, col_shift or None, param_dtype, dweight,
+                                          dbias or None, int(accumulate), workspace or None, workspace_bytes,
+                                          stream or None), "lc_linear_wgrad")
 
 
 def lc_record_bytes(ctx, layer: int) -> int:

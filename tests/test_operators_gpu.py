@@ -1,0 +1,755 @@
+"""The training operators against plain implementations in 64 bits.
+
+Tolerances are bounds on the rounding of the kernels' own arithmetic, formed from the inputs: u32 = 2^-24 a rounding of an
+fp32 operation, u_out the rounding of the result's type (2^-24 or 2^-8), `depth` an upper bound on the additions that one
+addend of a sum passes through.  What involves no rounding (the 8-bit form, rows without a token, gaps between rows) has to
+be equal bit for bit."""
+import math
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_27193_amd import layercheck as LC
+from paper_2609_27193_amd.build_lib import GRID_CAPPED_LIB
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+DT = {"bf16": (torch.bfloat16, LC.LC_DT_BF16, 2.0 ** -8), "f32": (torch.float32, LC.LC_DT_F32, U32)}
+I64 = torch.int64
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+class Guarded:
+    """A rows x cols view at any element of a larger buffer with a known pattern around it and between its rows."""
+
+    def __init__(self, rows, cols, dtype, pad=0, off=0, value=None):
+        self.rows, self.cols, self.stride = rows, cols, cols + pad
+        pattern = 77 if dtype == torch.uint8 else -3.25
+        self.flat = torch.full((off + max(rows, 1) * self.stride + 64,), pattern, dtype=dtype, device="cuda")
+        self.view = self.flat[off:off + rows * self.stride].view(rows, self.stride)[:, :cols]
+        self.mask = torch.ones_like(self.flat, dtype=torch.bool)
+        self.mask[off:off + rows * self.stride].view(rows, self.stride)[:, :cols] = False
+        if value is not None:
+            self.view.copy_(value)
+        self.before = self.flat.clone()
+        self.addr = self.flat.data_ptr() + off * self.flat.element_size()
+
+    def matrix(self):
+        return LC.matrix(self.addr, self.rows, self.cols,
+                         LC.LC_DT_BF16 if self.flat.dtype == torch.bfloat16 else LC.LC_DT_F32, self.stride)
+
+    def intact(self):
+        same = self.flat.view(torch.uint8).view(-1, self.flat.element_size()) == \
+            self.before.view(torch.uint8).view(-1, self.flat.element_size())
+        return bool(same.all(1)[self.mask].all())
+
+
+def space(n):
+    t = torch.full((n + 16,), 0xA5, dtype=torch.uint8, device="cuda")  # what is left there must not matter
+    return t, t.data_ptr(), n
+
+
+def close(got, ref, tol):
+    got = got.double()
+    nan = torch.isnan(ref)
+    assert torch.equal(torch.isnan(got), nan)
+    inf = torch.isinf(ref)
+    assert torch.equal(got[inf], ref[inf])
+    fin = ~(nan | inf)
+    err = (got - ref).abs()[fin]
+    tol = tol.expand_as(ref)[fin] if isinstance(tol, torch.Tensor) else torch.full_like(err, tol)
+    worst = (err - tol).max().item() if err.numel() else 0.0
+    assert worst <= 0, f"off by {err.max().item():.3g}, {worst:.3g} beyond the bound"
+
+
+# ---- the 8-bit form, by its definition -------------------------------------------------------------------------------------
+
+
+def code_values():
+    v = np.arange(256)
+    s, e, m = np.where(v >= 128, -1.0, 1.0), v % 128 // 8, v % 8
+    t = s * np.where(e > 0, (1 + m / 8) * 2.0 ** (e - 7.0), m / 8 * 2.0 ** -6)
+    t[v % 128 == 127] = np.nan
+    return t
+
+
+def keep(x):
+    """(codes, scales) of x (a CPU tensor) by the definition, one candidate power and one code after the other."""
+    x = x.double().numpy()
+    rows, cols = x.shape
+    blocks = -(-cols // 32)
+    table = code_values()
+    pos = table[:127]  # ascending, the codes 0 to 126
+    codes, scales = np.zeros((rows, cols), np.uint8), np.zeros((rows, blocks), np.uint8)
+    for b in range(blocks):
+        part = x[:, 32 * b:32 * b + 32]
+        fin = np.where(np.isfinite(part), np.abs(part), 0)
+        top = fin.max(1)
+        k = np.full(rows, -127)
+        while True:
+            grow = top > 448 * 2.0 ** k.astype(float)
+            if not grow.any():
+                break
+            k = k + grow
+        scales[:, b] = k + 127
+        u = np.where(np.isfinite(part), np.abs(part) / 2.0 ** k.astype(float)[:, None], 0)
+        u = np.where(k[:, None] == 120, np.minimum(u, 240), u)  # 256 * 2^120 would read back as an fp32 infinity
+        hi = np.clip(np.searchsorted(pos, u), 0, 126)
+        lo = np.maximum(hi - 1, 0)
+        dl, dh = u - pos[lo], pos[hi] - u
+        c = np.where(dl < dh, lo, np.where(dh < dl, hi, np.where(lo % 2 == 0, lo, hi)))
+        c = np.where(u == pos[hi], hi, c) | np.where(np.signbit(part), 128, 0)
+        codes[:, 32 * b:32 * b + 32] = np.where(np.isfinite(part), c, 127)
+    return torch.from_numpy(codes), torch.from_numpy(scales)
+
+
+def stands_for(codes, scales):
+    """Values in 64 bits, on the GPU."""
+    t = torch.from_numpy(code_values()).cuda()
+    p = torch.ldexp(torch.ones((), dtype=torch.float64), torch.arange(256) - 127)  # on the CPU: exact
+    p[255] = math.nan
+    p = p.cuda()[scales.long()].repeat_interleave(32, 1)[:, :codes.shape[1]]
+    return t[codes.long()] * p
+
+
+class Kept:
+    def __init__(self, rows, cols, codes=None, scales=None, pad=0, off=0):
+        self.codes = Guarded(rows, cols, torch.uint8, pad, off, codes)
+        self.scales = Guarded(rows, -(-cols // 32), torch.uint8, pad, off, scales)
+        self.act = LC.saved_act(self.codes.addr, self.scales.addr, rows, cols, self.codes.stride, self.scales.stride)
+
+    def values(self):
+        return stands_for(self.codes.view, self.scales.view)
+
+    def intact(self):
+        return self.codes.intact() and self.scales.intact()
+
+
+def kept_normal(rows, cols, seed, pad=0, off=0):
+    g = gen(seed)
+    codes = torch.randint(0, 256, (rows, cols), generator=g, device="cuda")
+    codes[codes % 128 == 127] = 1  # no NaN
+    scales = torch.randint(117, 121, (rows, -(-cols // 32)), generator=g, device="cuda")
+    return Kept(rows, cols, codes.to(torch.uint8), scales.to(torch.uint8), pad, off)
+
+
+ACT_SIZES = [(1, 1), (3, 7), (2, 8), (5, 31), (4, 32), (3, 33), (2, 100), (7, 1024), (3, 1101), (2, 5000)]
+
+
+@pytest.mark.parametrize("rows,cols", ACT_SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,off", [(0, 0), (5, 3)])
+def test_act_is_kept_bit_for_bit(rows, cols, dtype, pad, off):
+    dt, _, _ = DT[dtype]
+    g = gen(rows * 7919 + cols)
+    x = torch.randn(rows, cols, generator=g, device="cuda") * torch.exp2(torch.randint(-30, 30, (rows, 1), generator=g, device="cuda").float())
+    src = Guarded(rows, cols, dt, pad, off, x)
+    k = Kept(rows, cols, pad=pad, off=off)
+    LC.lc_act_save(src.matrix(), k.act, stream())
+    codes, scales = keep(src.view.cpu())
+    assert torch.equal(k.scales.view.cpu(), scales)
+    assert torch.equal(k.codes.view.cpu(), codes)
+    assert k.intact()
+    for out_dt in (torch.bfloat16, torch.float32):
+        out = Guarded(rows, cols, out_dt, pad, off)
+        LC.lc_act_load(k.act, out.matrix(), stream())
+        assert torch.equal(out.view.double(), k.values())  # exact in either type
+        assert out.intact()
+
+
+def test_act_edges():
+    inf, nan, top = math.inf, math.nan, 3.3895e38
+    tiny = 2.0 ** -126
+    rows = [[0.0, -0.0, 448.0, -448.0], [449.0, 1.0, -1.0, 0.5], [inf, 1.0, 2.0, -3.0], [nan, -inf, 0.0, 1e-3],
+            [nan] * 4, [-inf] * 4, [top, -top, 1.0, 1e-30], [tiny, -tiny / 2, tiny / 128, 0.0], [1e-45, 0.0, 0.0, -1e-45],
+            [448.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -11], [17.0, 19.0, 21.0, 23.0], [464.0, 432.0, 1.0, 0.0]]
+    x = torch.tensor(rows, dtype=torch.float32)
+    x = torch.nn.functional.pad(x, (0, 40))  # a second block that stays zero, and a third that is cut off
+    k = Kept(len(rows), x.shape[1])
+    src = Guarded(len(rows), x.shape[1], torch.float32, value=x.cuda())
+    LC.lc_act_save(src.matrix(), k.act, stream())
+    codes, scales = keep(x)
+    assert torch.equal(k.scales.view.cpu(), scales)
+    got, want = k.codes.view.cpu(), codes
+    nans = want % 128 == 127
+    assert torch.equal(got % 128 == 127, nans) and torch.equal(got[~nans], want[~nans])
+    out = Guarded(len(rows), x.shape[1], torch.float32)
+    LC.lc_act_load(k.act, out.matrix(), stream())
+    ref = k.values()
+    normal = ref.abs() >= 2.0 ** -126  # below, the multiply may or may not round to the subnormals
+    assert torch.equal(torch.isnan(out.view), torch.isnan(ref))
+    assert torch.equal(out.view.double()[normal], ref[normal])
+    assert bool((out.view.double() - ref)[~normal & ~torch.isnan(ref)].abs().max() <= 2.0 ** -126)
+
+
+def test_act_scale_of_255_is_nan():
+    k = Kept(1, 64, torch.full((1, 64), 0x38, dtype=torch.uint8), torch.tensor([[255, 128]], dtype=torch.uint8))
+    out = Guarded(1, 64, torch.float32)
+    LC.lc_act_load(k.act, out.matrix(), stream())
+    assert bool(torch.isnan(out.view[:, :32]).all()) and bool((out.view[:, 32:] == 2).all())
+
+
+# ---- embedding ---------------------------------------------------------------------------------------------------------------
+
+
+def some_tokens(n, vocab, first, seed, kind):
+    g = gen(seed)
+    t = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    if kind == "one":
+        t[:] = vocab - 1
+    elif kind == "skewed":  # half of them one token
+        t[torch.rand(n, generator=g, device="cuda") < 0.5] = vocab // 2
+    elif kind == "none":
+        t[:] = -1 - first
+    t = t + first
+    if kind == "mixed" and n > 4:
+        t[1], t[2], t[n - 1] = first - 1, first + vocab, -100
+    return t
+
+
+EMBED = [(0, 5, 8, "mixed"), (1, 1, 1, "one"), (1, 10, 4096, "mixed"), (5, 3, 7, "mixed"), (37, 50, 33, "mixed"),
+         (64, 9, 513, "skewed"), (300, 1000, 256, "mixed"), (1000, 7, 1025, "skewed"), (777, 400, 96, "none"),
+         (4096, 30, 64, "one"), (8192, 5000, 40, "skewed"), (8193, 5000, 40, "skewed"), (20001, 300, 72, "skewed"),
+         (9000, 300000, 8, "mixed"), (33000, 11, 24, "one"), (50000, 600, 9, "none")]
+
+
+@pytest.mark.parametrize("n,vocab,dim,kind", EMBED)
+@pytest.mark.parametrize("w,o", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+def test_embedding(n, vocab, dim, kind, w, o):
+    first = 1000 if n % 2 else 0
+    tokens = some_tokens(n, vocab, first, n + dim, kind)
+    if n % 3 == 0:
+        tokens = tokens.int()
+    elif n > 8:
+        tokens[3], tokens[4] = 2 ** 63 - 1, -2 ** 63
+    tdt = LC.LC_IT_I32 if tokens.dtype == torch.int32 else LC.LC_IT_I64
+    at = tokens.long() - first
+    held = (tokens >= first) & (tokens < first + vocab)
+    g = gen(dim)
+    pad, off = (3, 1) if dim % 2 else (0, 0)
+    scale = 22.5 if dim % 4 else 1.0
+    # forward: one product, rounded to fp32 and then to the output's type
+    weight = Guarded(vocab, dim, DT[w][0], pad, off, torch.randn(vocab, dim, generator=g, device="cuda"))
+    out = Guarded(n, dim, DT[o][0], pad, off)
+    LC.lc_embedding_forward(weight.matrix(), tokens.data_ptr(), tdt, n, out.matrix(), scale=scale, first_token=first,
+                            stream=stream())
+    ref = torch.zeros(n, dim, dtype=torch.float64, device="cuda")
+    ref[held] = weight.view.double()[at[held]] * scale
+    close(out.view, ref, ref.abs() * (DT[o][2] + 2 * U32))
+    assert out.intact() and weight.intact()
+    # backward; w: dout's type, o: the gradient's
+    dout = Guarded(n, dim, DT[w][0], pad, off, torch.randn(n, dim, generator=g, device="cuda"))
+    need = LC.lc_embedding_backward_workspace(n, dim)
+    for accumulate in (False, True):
+        old = torch.randn(vocab, dim, generator=g, device="cuda")
+        dw = Guarded(vocab, dim, DT[o][0], pad, off, old if accumulate else torch.full_like(old, math.nan))
+        buf, ws, _ = space(need)
+        args = dict(scale=scale, first_token=first, accumulate=accumulate, stream=stream())
+        LC.lc_embedding_backward(dout.matrix(), tokens.data_ptr(), tdt, n, dw.matrix(), ws, need, **args)
+        assert bool((buf[need:] == 0xA5).all())
+        total = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at[held], dout.view.double()[held])
+        size = torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, at[held], dout.view.double()[held].abs())
+        count = torch.zeros(vocab, dtype=torch.float64, device="cuda").index_add_(0, at[held], torch.ones(int(held.sum()), dtype=torch.float64, device="cuda"))
+        start = dw.before[~dw.mask].view(vocab, dim).double() if accumulate else torch.zeros_like(total)
+        ref = total * scale + start
+        close(dw.view, ref, ref.abs() * (DT[o][2] + 2 * U32) + (count[:, None] + 2) * U32 * size * scale * (1 + DT[o][2]) + 2 * U32 * start.abs())
+        if not accumulate:
+            assert bool((dw.view[count == 0] == 0).all())
+        assert dw.intact() and dout.intact()
+        again = Guarded(vocab, dim, DT[o][0], pad, off, old if accumulate else torch.zeros_like(old))
+        LC.lc_embedding_backward(dout.matrix(), tokens.data_ptr(), tdt, n, again.matrix(), ws, need, **args)
+        assert torch.equal(again.view, dw.view)  # the same bits every time
+
+
+def test_embedding_gradient_against_differences():
+    """The table's gradient is that of sum(dout * out): out is linear in the table, so a difference is exact to rounding."""
+    n, vocab, dim, scale = 200, 30, 40, 3.0
+    g = gen(5)
+    tokens = some_tokens(n, vocab, 0, 3, "mixed")
+    held = (tokens >= 0) & (tokens < vocab)
+    dout = torch.randn(n, dim, generator=g, device="cuda")
+    dw = torch.empty(vocab, dim, device="cuda")
+    need = LC.lc_embedding_backward_workspace(n, dim)
+    buf, ws, _ = space(need)
+    LC.lc_embedding_backward(LC.matrix(dout.data_ptr(), n, dim, LC.LC_DT_F32), tokens.data_ptr(), LC.LC_IT_I64, n,
+                             LC.matrix(dw.data_ptr(), vocab, dim, LC.LC_DT_F32), ws, need, scale=scale, stream=stream())
+
+    def loss(w):
+        out = torch.zeros(n, dim, dtype=torch.float64, device="cuda")
+        out[held] = w[tokens[held]] * scale
+        return (out * dout.double()).sum()
+
+    w0 = torch.randn(vocab, dim, generator=g, device="cuda", dtype=torch.float64)
+    for _ in range(4):
+        v = torch.randn(vocab, dim, generator=g, device="cuda", dtype=torch.float64)
+        got, want = (dw.double() * v).sum(), (loss(w0 + v) - loss(w0 - v)) / 2
+        size = (torch.zeros(vocab, dim, dtype=torch.float64, device="cuda").index_add_(0, tokens[held], dout.double()[held].abs()) * v.abs()).sum() * scale
+        assert abs(got - want) <= n * U32 * size
+
+
+def test_a_row_that_no_token_reads_may_hold_anything():
+    w = torch.full((4, 64), math.nan, device="cuda")
+    w[2] = 1.5
+    t = torch.tensor([2, -1, 7, 2], device="cuda")
+    out = torch.full((4, 64), math.nan, device="cuda")
+    LC.lc_embedding_forward(LC.matrix(w.data_ptr(), 4, 64, LC.LC_DT_F32), t.data_ptr(), LC.LC_IT_I64, 4,
+                            LC.matrix(out.data_ptr(), 4, 64, LC.LC_DT_F32), scale=2.0, stream=stream())
+    assert torch.equal(out, torch.tensor([3.0, 0, 0, 3.0], device="cuda")[:, None].expand(4, 64))
+    dout = torch.full((4, 64), math.nan, device="cuda")  # a gradient at a padding id goes nowhere
+    dout[0], dout[3] = 1, 2
+    dw = torch.empty(4, 64, device="cuda")
+    need = LC.lc_embedding_backward_workspace(4, 64)
+    buf, ws, _ = space(need)
+    LC.lc_embedding_backward(LC.matrix(dout.data_ptr(), 4, 64, LC.LC_DT_F32), t.data_ptr(), LC.LC_IT_I64, 4,
+                             LC.matrix(dw.data_ptr(), 4, 64, LC.LC_DT_F32), ws, need, stream=stream())
+    assert torch.equal(dw, torch.tensor([0, 0, 3.0, 0], device="cuda")[:, None].expand(4, 64))
+
+
+def test_ranks_of_a_split_vocabulary_add_up():
+    n, vocab, dim = 500, 96, 128
+    g = gen(1)
+    w = torch.randn(vocab, dim, generator=g, device="cuda").bfloat16()
+    t = some_tokens(n, vocab, 0, 2, "skewed")
+    whole = torch.empty(n, dim, device="cuda")
+    parts = torch.zeros(n, dim, device="cuda")
+    LC.lc_embedding_forward(LC.matrix(w.data_ptr(), vocab, dim, LC.LC_DT_BF16), t.data_ptr(), LC.LC_IT_I64, n,
+                            LC.matrix(whole.data_ptr(), n, dim, LC.LC_DT_F32), stream=stream())
+    for first in range(0, vocab, 32):
+        one = torch.empty(n, dim, device="cuda")
+        LC.lc_embedding_forward(LC.matrix(w[first:first + 32].data_ptr(), 32, dim, LC.LC_DT_BF16), t.data_ptr(),
+                                LC.LC_IT_I64, n, LC.matrix(one.data_ptr(), n, dim, LC.LC_DT_F32), first_token=first,
+                                stream=stream())
+        parts += one
+    assert torch.equal(parts, whole) and torch.equal(whole, w[t].float())
+
+
+# ---- norms -------------------------------------------------------------------------------------------------------------------
+
+
+def norm_reference(x, w, b, rms, eps):
+    x = x.double()
+    mean = torch.zeros(x.shape[0], 1, dtype=torch.float64, device="cuda") if rms else x.mean(1, keepdim=True)
+    rstd = 1 / torch.sqrt(((x - mean) ** 2).mean(1, keepdim=True) + eps)
+    n = (x - mean) * rstd
+    return mean, rstd, n, n * w.double() + b.double()
+
+
+def norm_depth(dim):
+    # a thread's own elements (24 of them up to 6144 columns, 16 beyond; rows over 16384 in strides of 1024 threads), six
+    # steps within a wave, up to 16 waves, and a dozen roundings of the formula itself
+    return 24 + 8 * (dim // 8192) + 6 + 16 + 12
+
+
+NORM = [(0, 8), (1, 1), (3, 2), (5, 7), (4, 8), (9, 31), (2, 96), (7, 511), (6, 512), (5, 513), (3, 1024), (9, 1027),
+        (3, 2048), (4, 2050), (2, 4096), (3, 5120), (2, 6145), (3, 8192), (2, 8200), (2, 16384), (2, 16391), (1, 40003),
+        (700, 64), (1200, 160)]
+
+
+@pytest.mark.parametrize("rows,dim", NORM)
+@pytest.mark.parametrize("dtype,param", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_norm(rows, dim, dtype, param, kind):
+    rms, eps = kind == "rms", 1e-5
+    dt, _, u_out = DT[dtype]
+    pt, pcode, _ = DT[param]
+    g = gen(rows + 31 * dim)
+    pad, off = (5, 1) if dim % 2 else (0, 0)
+    x = Guarded(rows, dim, dt, pad, off, torch.randn(rows, dim, generator=g, device="cuda") * 3 + 0.5)
+    w = (1 + 0.3 * torch.randn(dim, generator=g, device="cuda")).to(pt)
+    b = None if rms else (0.3 * torch.randn(dim, generator=g, device="cuda")).to(pt)
+    b64 = torch.zeros(dim, device="cuda") if rms else b
+    y = Guarded(rows, dim, dt, pad, off)
+    mean, rstd = torch.empty(rows + 1, device="cuda"), torch.empty(rows + 1, device="cuda")
+    k = Kept(rows, dim, pad=pad, off=off)
+    prm = LC.norm_params(LC.LC_NORM_RMS if rms else LC.LC_NORM_LAYER, w.data_ptr(), 0 if rms else b.data_ptr(), pcode, eps)
+    LC.lc_norm_forward(prm, x.matrix(), y.matrix(), 0 if rms else mean.data_ptr(), rstd.data_ptr(), k.act, stream())
+    rm, rr, rn, ry = norm_reference(x.view, w, b64, rms, eps)
+    depth = norm_depth(dim)
+    if rows:
+        close(mean[:rows] if not rms else torch.zeros(rows, device="cuda"), rm[:, 0], depth * U32 * x.view.double().abs().mean(1))
+        # the mean's error is second order in rstd, but counts against a spread of zero (dim 1)
+        shift = depth * U32 * x.view.double().abs().mean(1, keepdim=True) * (0 if rms else 1)
+        close(rstd[:rows], rr[:, 0], (depth * U32 * rr + shift ** 2 * rr ** 3)[:, 0])
+        n_tol = depth * U32 * rn.abs() + shift * rr + 2 * U32 * rm.abs() * rr
+        close(y.view, ry, u_out * ry.abs() * 2 + n_tol * w.double().abs() + 4 * U32 * (ry.abs() + b64.double().abs()))
+        # what is kept lies next to n: half a step of its 4 bits, or of the block's smallest step, and n's own error
+        step = torch.ldexp(torch.ones_like(rn), (k.scales.view.long() - 127 - 10).repeat_interleave(32, 1)[:, :dim])
+        close(k.values(), rn, torch.maximum(rn.abs() / 16, step) * (1 + 1e-6) + 2 * n_tol)
+        # and is the 8-bit form of what the kernel normalised: its power fits the block
+        top = torch.nn.functional.pad(rn.abs(), (0, -dim % 32)).view(rows, -1, 32).amax(2)
+        power = torch.ldexp(torch.ones_like(top), k.scales.view.long() - 127)
+        assert bool((top <= 448 * power * (1 + 1e-4)).all())
+        assert bool(((top >= 224 * power * (1 - 1e-4)) | (k.scales.view == 0)).all())
+    assert y.intact() and k.intact() and x.intact()
+    # nothing kept, no statistics: the same y
+    y2 = Guarded(rows, dim, dt, pad, off)
+    LC.lc_norm_forward(prm, x.matrix(), y2.matrix(), stream=stream())
+    assert torch.equal(y2.view, y.view)
+
+
+def norm_sums_depth(rows):
+    # a block's rows (512 blocks take turns), the parts of up to 2048 rows in 16 slices, the join of the slices
+    return rows // 512 + 1 + 128 + 16 + 4
+
+
+@pytest.mark.parametrize("rows,dim", NORM)
+@pytest.mark.parametrize("dtype,grad", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("kind,source", [("rms", "x"), ("rms", "kept"), ("layer", "x"), ("layer", "kept")])
+def test_norm_gradient(rows, dim, dtype, grad, kind, source):
+    rms = kind == "rms"
+    dt, _, u_out = DT[dtype]
+    gt, gcode, u_grad = DT[grad]
+    g = gen(rows + 17 * dim)
+    pad, off = (5, 1) if dim % 2 else (0, 0)
+    dy = Guarded(rows, dim, dt, pad, off, torch.randn(rows, dim, generator=g, device="cuda"))
+    w = (1 + 0.3 * torch.randn(dim, generator=g, device="cuda")).to(dt)
+    rstd = torch.rand(rows + 1, generator=g, device="cuda") + 0.5
+    mean = torch.randn(rows + 1, generator=g, device="cuda")
+    x = k = None
+    if source == "x":
+        x = Guarded(rows, dim, dt, pad, off, torch.randn(rows, dim, generator=g, device="cuda"))
+        m64 = torch.zeros(rows, 1, dtype=torch.float64, device="cuda") if rms else mean[:rows, None].double()
+        n = (x.view.double() - m64) * rstd[:rows, None].double()
+        n_tol = 3 * U32 * (n.abs() + m64.abs() * rstd[:rows, None].double())
+    else:
+        k = kept_normal(rows, dim, dim, pad, off)
+        n = k.values()
+        n_tol = torch.zeros_like(n)
+    prm = LC.norm_params(LC.LC_NORM_RMS if rms else LC.LC_NORM_LAYER, w.data_ptr(), 0, DT[dtype][1], 1e-5)
+    need = LC.lc_norm_backward_workspace(rows, dim)
+    d64 = dy.view.double()
+    gw = d64 * w.double()
+    c1 = torch.zeros(rows, 1, dtype=torch.float64, device="cuda") if rms or not rows else gw.mean(1, keepdim=True)
+    c2 = (gw * n).mean(1, keepdim=True)
+    rs = rstd[:rows, None].double()
+    rdx = rs * (gw - c1 - n * c2)
+    depth = norm_depth(dim)
+    c1_tol = depth * U32 * gw.abs().mean(1, keepdim=True) * (0 if rms else 1)
+    c2_tol = depth * U32 * (gw * n).abs().mean(1, keepdim=True) + (gw.abs() * n_tol).mean(1, keepdim=True)
+    dx_tol = rs * (4 * U32 * (gw.abs() + c1.abs() + (n * c2).abs()) + c1_tol + n.abs() * c2_tol + n_tol * c2.abs())
+    rw, rb = (d64 * n).sum(0), d64.sum(0)
+    for accumulate in (False, True):
+        dx = Guarded(rows, dim, dt, pad, off)
+        old_w, old_b = (torch.randn(1, dim, generator=g, device="cuda") for _ in "wb")
+        dw = Guarded(1, dim, gt, 0, off, old_w if accumulate else torch.full_like(old_w, math.nan))
+        db = Guarded(1, dim, gt, 0, off, old_b if accumulate else torch.full_like(old_b, math.nan))
+        buf, ws, _ = space(need)
+        args = dict(x=x.matrix() if x else None, mean=mean.data_ptr() if x and not rms else 0, saved=k.act if k else None,
+                    stream=stream())
+        LC.lc_norm_backward(prm, dy.matrix(), rstd.data_ptr(), dx.matrix(), dw.addr, 0 if rms else db.addr, gcode, ws, need,
+                            accumulate=accumulate, **args)
+        assert bool((buf[need:] == 0xA5).all())
+        if rows and dim:
+            close(dx.view, rdx, u_out * rdx.abs() * 2 + dx_tol)
+        sd = norm_sums_depth(rows)
+        for got, want, size, old in ((dw, rw, (d64 * n).abs().sum(0) + (d64.abs() * n_tol).sum(0) / (sd * U32), old_w),
+                                     (db, rb, d64.abs().sum(0), old_b)):
+            if got is db and rms:
+                continue
+            base = old.to(gt).double()[0] if accumulate else torch.zeros_like(want)
+            close(got.view[0], want + base, 2 * u_grad * (want + base).abs() + sd * U32 * size * (1 + u_grad) + 2 * U32 * base.abs())
+        assert dx.intact() and dw.intact() and (rms or db.intact())
+    # parts of it: the same bits
+    dx2 = Guarded(rows, dim, dt, pad, off)
+    LC.lc_norm_backward(prm, dy.matrix(), rstd.data_ptr(), dx2.matrix(), 0, 0, gcode, 0, 0, **args)
+    assert torch.equal(dx2.view, dx.view)
+    dw2 = Guarded(1, dim, gt, 0, off, old_w)
+    LC.lc_norm_backward(prm, dy.matrix(), rstd.data_ptr(), None, dw2.addr, 0, gcode, ws, need, accumulate=True, **args)
+    assert torch.equal(dw2.view, dw.view)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_norm_gradient_against_differences(kind):
+    rms, rows, dim, eps = kind == "rms", 6, 200, 1e-3
+    g = gen(11)
+    x, dy = (torch.randn(rows, dim, generator=g, device="cuda") for _ in "xd")
+    w = 1 + 0.3 * torch.randn(dim, generator=g, device="cuda")
+    b = torch.randn(dim, generator=g, device="cuda")
+    prm = LC.norm_params(LC.LC_NORM_RMS if rms else LC.LC_NORM_LAYER, w.data_ptr(), 0 if rms else b.data_ptr(), LC.LC_DT_F32, eps)
+    m = lambda t: LC.matrix(t.data_ptr(), rows, dim, LC.LC_DT_F32)  # noqa: E731
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, dw, db = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(dim, device="cuda"), torch.empty(dim, device="cuda")
+    LC.lc_norm_forward(prm, m(x), m(y), 0 if rms else mean.data_ptr(), rstd.data_ptr(), stream=stream())
+    need = LC.lc_norm_backward_workspace(rows, dim)
+    buf, ws, _ = space(need)
+    LC.lc_norm_backward(prm, m(dy), rstd.data_ptr(), m(dx), dw.data_ptr(), 0 if rms else db.data_ptr(), LC.LC_DT_F32, ws, need,
+                        x=m(x), mean=0 if rms else mean.data_ptr(), stream=stream())
+
+    def loss(x, w, b):
+        return (norm_reference(x, w, b, rms, eps)[3] * dy.double()).sum()
+
+    b = torch.zeros_like(b) if rms else b
+    h = 1e-4  # the differences' own error is h^2 times third derivatives of order one, summed over `rows * dim` terms
+    for what, grad in (("x", dx), ("w", dw)) + ((("b", db),) if not rms else ()):
+        args = {"x": x.double(), "w": w.double(), "b": b.double()}
+        v = torch.randn(args[what].shape, generator=g, device="cuda", dtype=torch.float64)
+        up, down = dict(args), dict(args)
+        up[what], down[what] = args[what] + h * v, args[what] - h * v
+        want = (loss(**up) - loss(**down)) / (2 * h)
+        got = (grad.double() * v).sum()
+        scale = dy.double().abs().sum() * 4
+        assert abs(got - want) <= scale * (100 * U32 + h * h), (what, got.item(), want.item())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 1500, 9000])
+def test_norm_edges(dtype, dim):
+    """A row that is constant, zero, or holds an infinity or a NaN changes no other row."""
+    dt, code, u = DT[dtype]
+    g = gen(3)
+    x = torch.randn(6, dim, generator=g, device="cuda")
+    x[1], x[2], x[3, dim // 2], x[4, 0] = 2.5, 0.0, math.inf, math.nan
+    x = x.to(dt)
+    for rms in (False, True):
+        for eps in (1e-5, 0.0):
+            prm = LC.norm_params(LC.LC_NORM_RMS if rms else LC.LC_NORM_LAYER, 0, 0, code, eps)
+            y = torch.empty_like(x)
+            k = Kept(6, dim)
+            LC.lc_norm_forward(prm, LC.matrix(x.data_ptr(), 6, dim, code), LC.matrix(y.data_ptr(), 6, dim, code), saved=k.act,
+                               stream=stream())
+            ref = norm_reference(x, torch.ones(dim, device="cuda"), torch.zeros(dim, device="cuda"), rms, eps)[3]
+            for r in (0, 5):
+                close(y[r], ref[r], 2 * u * ref[r].abs() + 100 * U32)
+            # the constant and the zero row: zeros, or 0 * inf with an eps of 0.  2.5 times the number of columns is a
+            # sum of equal terms, whose mean comes out as 2.5 where every partial sum is exact
+            want1, want2 = ref[1], ref[2]
+            if rms:
+                close(y[1], want1, 2 * u * want1.abs() + 100 * U32)
+            elif eps:
+                assert bool((y[1].abs() <= 100 * U32 * 2.5 / math.sqrt(eps)).all())
+            assert torch.equal(torch.isnan(y[2]), torch.isnan(want2)) and (eps == 0 or bool((y[2] == 0).all()))
+            assert bool(torch.isnan(y[4]).all())
+            assert bool(torch.isnan(y[3, dim // 2]))  # inf - inf, or inf * 0
+            kept = k.values()
+            assert bool(torch.isnan(kept[4]).all()) and not bool(torch.isnan(kept[[0, 5]]).any())
+
+
+# ---- the linear layer's weight gradient ------------------------------------------------------------------------------------
+
+
+WGRAD = [(0, 5, 9), (1, 1, 1), (3, 7, 5), (31, 16, 33), (32, 128, 128), (33, 130, 129), (100, 64, 300), (257, 129, 31),
+         (513, 300, 260), (1000, 40, 1030), (4100, 70, 50), (300, 2100, 2050), (96, 4112, 520)]
+
+
+@pytest.mark.parametrize("rows,n,k", WGRAD)
+@pytest.mark.parametrize("dtype,out,affine", [("bf16", "bf16", 0), ("bf16", "f32", 2), ("f32", "f32", 1), ("f32", "bf16", 2)])
+def test_linear_wgrad(rows, n, k, dtype, out, affine):
+    dt, _, _ = DT[dtype]
+    ot, _, u_out = DT[out]
+    pt, pcode, _ = DT["bf16" if affine == 1 else "f32"]
+    g = gen(rows + n + k)
+    pad, off = (3, 1) if (n + k) % 2 else (0, 0)
+    dy = Guarded(rows, n, dt, pad, off, torch.randn(rows, n, generator=g, device="cuda"))
+    kept = kept_normal(rows, k, n, pad, off)
+    scale = (1 + 0.3 * torch.randn(k, generator=g, device="cuda")).to(pt) if affine else None
+    shift = torch.randn(k, generator=g, device="cuda").to(pt) if affine == 2 else None
+    s64 = scale.double() if affine else torch.ones(k, dtype=torch.float64, device="cuda")
+    b64 = shift.double() if affine == 2 else torch.zeros(k, dtype=torch.float64, device="cuda")
+    x = kept.values()
+    d64 = dy.view.double()
+    total, size = d64.t() @ x, d64.abs().t() @ x.abs()
+    sums, sum_size = d64.sum(0)[:, None], d64.abs().sum(0)[:, None]
+    need = LC.lc_linear_wgrad_workspace(rows, n, k)
+    depth = 3 * rows + 80  # every token's product once (three parts of an fp32 dy), the splits, the formula
+    for accumulate in (False, True):
+        for bias in (False, True):
+            old, old_b = torch.randn(n, k, generator=g, device="cuda"), torch.randn(1, n, generator=g, device="cuda")
+            dw = Guarded(n, k, ot, pad, off, old if accumulate else torch.full_like(old, math.nan))
+            db = Guarded(1, n, ot, 0, off, old_b if accumulate else torch.full_like(old_b, math.nan))
+            buf, ws, _ = space(need)
+            args = dict(col_scale=scale.data_ptr() if affine else 0, col_shift=shift.data_ptr() if affine == 2 else 0,
+                        param_dtype=pcode, dbias=db.addr if bias else 0, accumulate=accumulate, stream=stream())
+            LC.lc_linear_wgrad(dy.matrix(), kept.act, dw.matrix(), ws, need, **args)
+            assert bool((buf[need:] == 0xA5).all())
+            base = old.to(ot).double() if accumulate else torch.zeros_like(total)
+            ref = total * s64 + sums * b64 + base
+            close(dw.view, ref, 2 * u_out * ref.abs() + depth * U32 * (size * s64.abs() + sum_size * b64.abs() + base.abs()))
+            if bias:
+                base = old_b.to(ot).double() if accumulate else torch.zeros_like(old_b).double()
+                ref = sums.t() + base
+                close(db.view, ref, 2 * u_out * ref.abs() + depth * U32 * (sum_size.t() + base.abs()))
+            assert dw.intact() and db.intact() and dy.intact() and kept.intact()
+            again = Guarded(n, k, ot, pad, off, old if accumulate else torch.zeros_like(old))
+            if bias:
+                db.view.copy_(old_b)
+            LC.lc_linear_wgrad(dy.matrix(), kept.act, again.matrix(), ws, need, **args)
+            assert torch.equal(again.view, dw.view)
+
+
+def test_wgrad_takes_all_bits_of_a_32_bit_gradient():
+    """One token and a kept 1.0: the gradient is dy itself, to the last bit, from the largest to the smallest normal."""
+    g = gen(9)
+    n = 256
+    bits = torch.randint(0, 1 << 23, (1, n), generator=g, device="cuda") | (torch.randint(24, 255, (1, n), generator=g, device="cuda") << 23)
+    dy = bits.int().view(torch.float32)
+    dy[0, ::2] *= -1
+    kept = Kept(1, 32, torch.full((1, 32), 0x38, dtype=torch.uint8), torch.full((1, 1), 127, dtype=torch.uint8))
+    dw = torch.empty(n, 32, device="cuda")
+    need = LC.lc_linear_wgrad_workspace(1, n, 32)
+    buf, ws, _ = space(need)
+    LC.lc_linear_wgrad(LC.matrix(dy.data_ptr(), 1, n, LC.LC_DT_F32), kept.act, LC.matrix(dw.data_ptr(), n, 32, LC.LC_DT_F32),
+                       ws, need, stream=stream())
+    assert torch.equal(dw, dy.t().expand(n, 32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wgrad_edges(dtype):
+    """An infinity or NaN in one output's gradient, or one input's column, stays in its row, or column."""
+    dt, code, _ = DT[dtype]
+    rows, n, k = 40, 130, 140
+    g = gen(4)
+    dy = torch.randn(rows, n, generator=g, device="cuda")
+    dy[5, 7], dy[6, 100], dy[39, 129] = math.inf, math.nan, -math.inf
+    dy = dy.to(dt)
+    kept = kept_normal(rows, k, 8)
+    kept.codes.view[kept.codes.view % 128 == 0] = 1  # no zeros: an infinity times one is NaN
+    kept.codes.view[3, 9] = 127
+    dw = torch.empty(n, k, device="cuda")
+    need = LC.lc_linear_wgrad_workspace(rows, n, k)
+    buf, ws, _ = space(need)
+    LC.lc_linear_wgrad(LC.matrix(dy.data_ptr(), rows, n, code), kept.act, LC.matrix(dw.data_ptr(), n, k, LC.LC_DT_F32), ws, need,
+                       stream=stream())
+    ref = dy.double().t() @ kept.values()
+    assert bool(torch.isnan(dw[:, 9]).all()) and bool(torch.isnan(dw[100]).all())
+    cols = torch.arange(k, device="cuda") != 9
+    for r in (7, 129):
+        assert torch.equal(dw[r][cols].double(), ref[r][cols])
+    good = torch.ones(n, dtype=torch.bool, device="cuda")
+    good[[7, 100, 129]] = False
+    assert bool(torch.isfinite(dw[good][:, cols]).all())
+
+
+# ---- the calls as a program makes them ---------------------------------------------------------------------------------------
+
+
+def a_step(n_tok, vocab, dim, out, seed):
+    """Buffers and calls of one step through all the operators: (enqueue, results)."""
+    g = gen(seed)
+    bf, f32 = torch.bfloat16, torch.float32
+    E = lambda *s, dtype=bf: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    B, F = LC.LC_DT_BF16, LC.LC_DT_F32
+    M = lambda t: LC.matrix(t.data_ptr(), t.shape[0], t.shape[1], B if t.dtype == bf else F)  # noqa: E731
+    tokens = some_tokens(n_tok, vocab, 0, seed, "skewed")
+    table, w = torch.randn(vocab, dim, generator=g, device="cuda").to(bf), torch.rand(dim, generator=g, device="cuda").to(bf)
+    dz, dy = (torch.randn(n_tok, s, generator=g, device="cuda").to(bf) for s in (out, dim))
+    h, y, dx, back = E(n_tok, dim), E(n_tok, dim), E(n_tok, dim), E(n_tok, dim)
+    rstd, codes, scales = E(n_tok, dtype=f32), E(n_tok, dim, dtype=torch.uint8), E(n_tok, -(-dim // 32), dtype=torch.uint8)
+    dtable, dw, dlin = E(vocab, dim), E(dim, dtype=f32), E(out, dim)
+    sizes = [LC.lc_embedding_backward_workspace(n_tok, dim), LC.lc_norm_backward_workspace(n_tok, dim),
+             LC.lc_linear_wgrad_workspace(n_tok, out, dim)]
+    ws = torch.zeros(max(sizes), dtype=torch.uint8, device="cuda")
+    kept = LC.saved_act(codes.data_ptr(), scales.data_ptr(), n_tok, dim)
+    prm = LC.norm_params(LC.LC_NORM_RMS, w.data_ptr(), 0, B, 1e-5)
+
+    def enqueue():
+        s, a, z = stream(), ws.data_ptr(), ws.numel()
+        LC.lc_embedding_forward(M(table), tokens.data_ptr(), LC.LC_IT_I64, n_tok, M(h), stream=s)
+        LC.lc_norm_forward(prm, M(h), M(y), rstd=rstd.data_ptr(), saved=kept, stream=s)
+        LC.lc_act_load(kept, M(back), stream=s)
+        LC.lc_linear_wgrad(M(dz), kept, M(dlin), a, z, col_scale=w.data_ptr(), param_dtype=B, stream=s)
+        LC.lc_norm_backward(prm, M(dy), rstd.data_ptr(), M(dx), dw.data_ptr(), 0, F, a, z, saved=kept, stream=s)
+        LC.lc_embedding_backward(M(dx), tokens.data_ptr(), LC.LC_IT_I64, n_tok, M(dtable), a, z, stream=s)
+
+    keepalive = (tokens, table, w, dz, dy, ws)
+    return enqueue, [h, y, rstd, codes, scales, back, dlin, dx, dw, dtable], keepalive
+
+
+@pytest.mark.parametrize("n_tok", [50, 9000])
+def test_calls_in_a_graph(n_tok):
+    enqueue, results, keepalive = a_step(n_tok, 300, 136, 200, 1)
+    enqueue()
+    torch.cuda.synchronize()
+    want = [r.clone() for r in results]
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        enqueue()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            enqueue()
+    for i in range(4):
+        for r in results:
+            r.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results, want)), i
+
+
+def test_calls_on_two_streams():
+    """Each stream with its own workspace and its own order; the caller's waits alone hold them together."""
+    steps = [a_step(700, 300, 136, 200, s) for s in (1, 2)]
+    want = []
+    for enqueue, results, _ in steps:
+        enqueue()
+        torch.cuda.synchronize()
+        want.append([r.clone() for r in results])
+    streams = [torch.cuda.Stream() for _ in steps]
+    for _ in range(3):
+        for _, results, _ in steps:
+            for r in results:
+                r.zero_()
+        torch.cuda.synchronize()
+        for st, (enqueue, _, _) in zip(streams, steps):
+            with torch.cuda.stream(st):
+                enqueue()
+        torch.cuda.synchronize()
+        for (_, results, _), w in zip(steps, want):
+            assert all(torch.equal(a, b) for a, b in zip(results, w))
+
+
+def test_offsets_beyond_32_bits():
+    """A table and a kept activation of more than 2^32 bytes: their last rows are reached."""
+    dim, vocab = 8192, (1 << 18) + 40  # 4.3 GB of bf16
+    table = torch.zeros(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    table[-8:] = torch.arange(8, device="cuda")[:, None] + 1
+    t = torch.tensor([vocab - 1, 0, vocab - 8, vocab], device="cuda")
+    out = torch.empty(4, dim, dtype=torch.bfloat16, device="cuda")
+    m = LC.matrix(table.data_ptr(), vocab, dim, LC.LC_DT_BF16)
+    LC.lc_embedding_forward(m, t.data_ptr(), LC.LC_IT_I64, 4, LC.matrix(out.data_ptr(), 4, dim, LC.LC_DT_BF16), stream=stream())
+    assert out[:, 0].tolist() == [8, 0, 1, 0] and out[:, -1].tolist() == [8, 0, 1, 0]
+    # the gradient of the whole table, then the rows of the same size kept and read back
+    need = LC.lc_embedding_backward_workspace(4, dim)
+    buf, ws, _ = space(need)
+    table.fill_(7)
+    LC.lc_embedding_backward(LC.matrix(out.data_ptr(), 4, dim, LC.LC_DT_BF16), t.data_ptr(), LC.LC_IT_I64, 4, m, ws, need,
+                             stream=stream())
+    touched = table[:, 0].nonzero()[:, 0].tolist()
+    assert touched == [vocab - 8, vocab - 1] and table[-1, -1].item() == 8 and not bool(table[:-8].any())
+    codes = torch.zeros(vocab, dim, dtype=torch.uint8, device="cuda")
+    wide = torch.zeros(vocab, 2 * dim, dtype=torch.uint8, device="cuda")  # code rows 2 * dim apart: 4.3 GB, too
+    scales = torch.zeros(vocab, dim // 32, dtype=torch.uint8, device="cuda")
+    del codes
+    k = LC.saved_act(wide.data_ptr(), scales.data_ptr(), vocab, dim, 2 * dim)
+    LC.lc_act_save(m, k, stream())
+    assert bool(wide[-1, :dim].any()) and not bool(wide[-1, dim:].any())
+    back = torch.empty_like(table)
+    LC.lc_act_load(k, LC.matrix(back.data_ptr(), vocab, dim, LC.LC_DT_BF16), stream())
+    assert torch.equal(back, table)
+
+
+def test_grids_capped_at_forty_blocks():
+    """Every kernel in the form that it takes beyond the dispatch limit: blocks that take several items."""
+    if not os.path.exists(GRID_CAPPED_LIB):
+        pytest.skip("the grid-capped library is built by __graft_entry__.build()")
+    if os.environ.get("LAYERCHECK_LIB"):
+        pytest.skip("runs in the parent only")
+    pick = ("(test_embedding and (20001 or 4096 or 300)) or (test_norm and 1200) or (test_linear_wgrad and 2100) or "
+            "(test_act_is_kept and 5000) or test_calls_in_a_graph")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-p", "no:cacheprovider", "-m", "gpu", "-k", pick,
+                        os.path.abspath(__file__)], env=dict(os.environ, LAYERCHECK_LIB=GRID_CAPPED_LIB),
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True,
+                       timeout=600)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-3000:]
