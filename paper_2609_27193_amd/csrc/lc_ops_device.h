@@ -46,6 +46,7 @@ __device__ __forceinline__ void store1(uint64_t p, float v) {
   else *(g_f32*)p = v;
 }
 // One element of a small array whose type only the call knows.
+// (`dtype` is the same for the whole grid: the branch costs nothing.)
 __device__ __forceinline__ float load_param(uint64_t p, uint64_t i, int dtype) {
   return dtype == kBf16 ? load1<kBf16>(p + 2 * i) : load1<kF32>(p + 4 * i);
 }
@@ -86,6 +87,43 @@ __device__ __forceinline__ Raw8<DT> load8_raw(uint64_t p, int n) {
   }
   return r;
 }
+// Group g of a row of dim >= 8 elements at `row`, zeros behind the row's end.
+// The last group of a row that is no multiple of eight is read from eight
+// elements before the end and moved down: one load, where an element at a time
+// takes seven and the registers for them.  n: the group's elements, at most 0
+// for a group that is not there.
+template <int DT>
+__device__ __forceinline__ Raw8<DT> load8_row(uint64_t row, uint32_t g, uint32_t dim, int n) {
+  Raw8<DT> r;
+  for (auto& q : r.v) q = u32x4{0, 0, 0, 0};
+  if (dim % 8 == 0) {  // the same for the whole grid
+    if (n > 0) r = load8_raw<DT>(row + 8ull * kEsz<DT> * g);
+    return r;
+  }
+  const uint32_t s = n > 0 && n < 8 ? 8 - n : 0;
+  if (n > 0) r = load8_raw<DT>(row + (8ull * g - s) * kEsz<DT>);
+  if constexpr (DT == kBf16) {
+    u32x4& v = r.v[0];
+    if (s & 4) v = u32x4{v[2], v[3], 0, 0};
+    if (s & 2) v = u32x4{v[1], v[2], v[3], 0};
+    if (s & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+  } else {
+    u32x4 &a = r.v[0], &b = r.v[1];
+    if (s & 4) {
+      a = b;
+      b = u32x4{0, 0, 0, 0};
+    }
+    if (s & 2) {
+      a = u32x4{a[2], a[3], b[0], b[1]};
+      b = u32x4{b[2], b[3], 0, 0};
+    }
+    if (s & 1) {
+      a = u32x4{a[1], a[2], a[3], b[0]};
+      b = u32x4{b[1], b[2], b[3], 0};
+    }
+  }
+  return r;
+}
 template <int DT>
 __device__ __forceinline__ void unpack8(const Raw8<DT>& r, float (&f)[8]) {
 #pragma unroll
@@ -111,6 +149,18 @@ __device__ __forceinline__ void store8(uint64_t p, const float (&f)[8], int n) {
 #pragma unroll
   for (int i = 0; i < 7; ++i)
     if (i < n) store1<DT>(p + kEsz<DT> * i, f[i]);
+}
+// Group g of a small array of `dim` elements, whose type only the call knows;
+// p 0: `other` for each.
+__device__ __forceinline__ void load_params8(uint64_t p, int dtype, uint32_t g, int n, float other, float (&f)[8]) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = other;
+  } else if (dtype == kBf16) {
+    unpack8<kBf16>(load8_raw<kBf16>(p + 16ull * g, n), f);
+  } else {
+    unpack8<kF32>(load8_raw<kF32>(p + 32ull * g, n), f);
+  }
 }
 // Elements of group g of a row of `dim` that exist (at most 0 when none does).
 __device__ __forceinline__ int in_group(uint32_t dim, uint32_t g) {
@@ -153,23 +203,30 @@ __device__ __forceinline__ float act_scale(uint32_t code) {  // 2^-127 is below 
 }
 // Eight neighbours of a block whose four groups of eight lie in one quad of
 // lanes: the eight bytes, and the block's code in every lane of the quad.
-__device__ __forceinline__ u32x2 act_encode8(const float (&f)[8], uint32_t& code) {
-  uint32_t top = 0;
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, dpp_f32<0xB1>(v));
+  return fmaxf(v, dpp_f32<0x4E>(v));
+}
+__device__ __forceinline__ u32x2 act_encode8(float (&f)[8], uint32_t& code) {
+  float top = 0;  // the larger of two passes over a NaN
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t a = __float_as_uint(f[i]) & 0x7fffffffu;
-    if (a < 0x7f800000u && a > top) top = a;
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+  top = quad_max(top);
+  if (!(top < __builtin_inff())) {  // an infinity, or a NaN that was not quiet
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool finite = (__float_as_uint(f[i]) & 0x7fffffffu) < 0x7f800000u;
+      f[i] = finite ? f[i] : __uint_as_float(0x7FC00000u);
+      top = finite ? fmaxf(top, fabsf(f[i])) : top;
+    }
+    top = quad_max(top);  // the whole quad is here: `top` was the same in its lanes
   }
-  uint32_t o = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(top), 0xB1, 0xF, 0xF, false));
-  top = o > top ? o : top;
-  o = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(top), 0x4E, 0xF, 0xF, false));
-  top = o > top ? o : top;
-  code = act_code(top);
+  code = act_code(__float_as_uint(top));
   const float inv = act_inverse(code);
   float q[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    q[i] = (__float_as_uint(f[i]) & 0x7fffffffu) < 0x7f800000u ? f[i] * inv : __uint_as_float(0x7FC00000u);
+  for (int i = 0; i < 8; ++i) q[i] = f[i] * inv;
   if (code == kActTopCode) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[i] = q[i] > 240.0f ? 240.0f : q[i] < -240.0f ? -240.0f : q[i];
@@ -215,6 +272,13 @@ __device__ __forceinline__ void store_codes8(uint64_t p, u32x2 b, int n) {
 #pragma unroll
   for (int i = 0; i < 7; ++i)
     if (i < n) *(g_u8*)(p + i) = static_cast<uint8_t>(b[i / 4] >> (8 * (i & 3)));
+}
+// The same of a row of dim >= 8 codes at `row`, as load8_row.
+__device__ __forceinline__ u32x2 load_codes8_row(uint64_t row, uint32_t g, int n) {
+  const uint32_t s = n > 0 && n < 8 ? 8 - n : 0;
+  u32x2 r = {0, 0};
+  if (n > 0) r = *(gc_u32x2_any1*)(row + 8ull * g - s);
+  return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, r) >> (8 * s));
 }
 // Group g of row r of a kept activation, and its block's scale.
 __device__ __forceinline__ u32x2 load_kept8(const Kept& k, uint64_t row, uint32_t g, int n) {
