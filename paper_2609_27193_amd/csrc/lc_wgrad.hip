@@ -28,6 +28,8 @@ constexpr uint32_t kTile = 128;     // of n and of k
 constexpr uint32_t kStep = 32;      // tokens in LDS at a time
 constexpr uint32_t kThreads = 256;  // four waves of 64 x 64
 constexpr uint32_t kPitch = kTile + 16;  // elements from token to token in LDS
+constexpr uint32_t kOut = 64 + 4;        // floats from row to row on their way out
+static_assert(4 * 16 * kOut * 4 <= 2 * kStep * kPitch * 2, "the rows on their way out fit X's buffers");
 
 struct Codes16 {
   u32x4 codes;
@@ -90,13 +92,89 @@ __device__ __forceinline__ bf16x8 read_cols(const uint16_t* tile, uint32_t col, 
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// How a product is cut: `full` tiles of the whole sum over the tokens, then the
+// others in `splits` parts each, whose sums wgrad_join_kernel adds.
 struct WgradTiles {
+  uint32_t tile;         // columns of n and of k
   uint32_t tn, tk;       // tiles of n and k
-  uint32_t splits;       // parts of the tokens
+  uint32_t splits;
+  uint64_t full, tiles;  // tiles of the whole sum, and all
   uint64_t per_split;    // tokens a part, a multiple of kStep
-  float* part;           // [splits][n][k], with more than one split
-  float* sums;           // [splits][n]
+  float* part;           // [tiles - full][splits][tile][tile]
+  float* sums;           // [sum_parts][n] column sums of dY
+  uint32_t sum_parts;
+  bool big;              // wgrad_big_kernel's tiles
 };
+
+struct WgradItem {
+  uint64_t tile;
+  uint32_t split, n0, k0;
+  bool whole;
+  uint64_t t_begin, t_end;
+};
+// Eight tiles of n by all of k follow each other, so that blocks that run side
+// by side read the same columns.
+__device__ __forceinline__ void wgrad_place(const WgradTiles& s, uint64_t tile, uint32_t& n0, uint32_t& k0) {
+  const uint64_t per_group = 8ull * s.tk;
+  const uint32_t group = static_cast<uint32_t>(tile / per_group) * 8, in_g = static_cast<uint32_t>(tile % per_group);
+  const uint32_t wide = s.tn - group < 8 ? s.tn - group : 8;
+  n0 = (group + in_g % wide) * s.tile;
+  k0 = in_g / wide * s.tile;
+}
+// Item b of the grid.  The whole tiles run first, then the parts; each in
+// contiguous eighths for the XCDs.
+__device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t rows, uint64_t b) {
+  WgradItem w;
+  w.whole = b < s.full;
+  if (w.whole) {
+    w.tile = s.full <= gridDim.x ? remap_xcd(static_cast<uint32_t>(b), static_cast<uint32_t>(s.full)) : b;
+    w.split = 0;
+    w.t_begin = 0;
+    w.t_end = rows;
+  } else {
+    const uint64_t parts = (s.tiles - s.full) * s.splits;
+    const uint64_t i = s.full + parts <= gridDim.x ? remap_xcd(static_cast<uint32_t>(b - s.full), static_cast<uint32_t>(parts)) : b - s.full;
+    w.tile = s.full + i / s.splits;
+    w.split = static_cast<uint32_t>(i % s.splits);
+    w.t_begin = w.split * s.per_split;
+    w.t_end = w.t_begin + s.per_split < rows ? w.t_begin + s.per_split : rows;
+  }
+  wgrad_place(s, w.tile, w.n0, w.k0);
+  return w;
+}
+// Row n of a part's sums.
+__device__ __forceinline__ float* wgrad_part(const WgradTiles& s, uint64_t tile, uint32_t split, uint32_t n) {
+  return s.part + (((tile - s.full) * s.splits + split) * s.tile + n) * s.tile;
+}
+
+// Eight neighbours of k of row n of the whole sum, with everything that the
+// result has besides.
+__device__ __forceinline__ void wgrad_write8(const Wgrad& a, uint64_t n, uint32_t k, int in, float sum, float (&v)[8]) {
+  float w[8];
+  if (a.col_scale) {
+    load_params8(a.col_scale, a.param_dtype, k / 8, in, 1.0f, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= w[e];
+  }
+  if (a.col_shift) {
+    load_params8(a.col_shift, a.param_dtype, k / 8, in, 0.0f, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += sum * w[e];
+  }
+  const uint64_t at = n * a.dw.stride + k;
+  if (a.accumulate) {
+    if (a.dw_dtype == kBf16) unpack8<kBf16>(load8_raw<kBf16>(a.dw.data + 2 * at, in), w);
+    else unpack8<kF32>(load8_raw<kF32>(a.dw.data + 4 * at, in), w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += w[e];
+  }
+  if (a.dw_dtype == kBf16) store8<kBf16>(a.dw.data + 2 * at, v, in);
+  else store8<kF32>(a.dw.data + 4 * at, v, in);
+}
+__device__ __forceinline__ void wgrad_write_bias(const Wgrad& a, uint64_t n, float sum) {
+  if (a.accumulate) sum += load_param(a.dbias, n, a.dw_dtype);
+  store_param(a.dbias, n, a.dw_dtype, sum);
+}
 
 template <int DT, bool SUMS>
 __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) {
@@ -105,14 +183,11 @@ __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) 
   __shared__ __align__(16) uint16_t xs[2][kStep * kPitch];
   __shared__ float colsum[SUMS ? kThreads / 16 : 1][kTile];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint64_t tiles = static_cast<uint64_t>(s.tn) * s.tk * s.splits;
-  for (uint64_t b = blockIdx.x; b < tiles; b += gridDim.x) {
-    const uint32_t split = static_cast<uint32_t>(b % s.splits);
-    const uint64_t tile = b / s.splits;
-    const uint32_t n0 = static_cast<uint32_t>(tile / s.tk) * kTile, k0 = static_cast<uint32_t>(tile % s.tk) * kTile;
-    const uint64_t t_begin = split * s.per_split;
-    const uint64_t t_end = t_begin + s.per_split < a.rows ? t_begin + s.per_split : a.rows;
-
+  const uint64_t items = s.full + (s.tiles - s.full) * s.splits;
+  for (uint64_t b = blockIdx.x; b < items; b += gridDim.x) {
+    const WgradItem w = wgrad_item(s, a.rows, b);
+    const uint32_t n0 = w.n0, k0 = w.k0;
+    const uint64_t t_begin = w.t_begin, t_end = w.t_end;
     // a thread's share of a step: two groups of eight of dY, sixteen codes of X
     const uint32_t dc = tid % 16, dr = tid / 16;
     const int d_in = static_cast<int>(a.n) - static_cast<int>(n0 + 8 * dc);
@@ -209,83 +284,373 @@ __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) 
         colsum[0][tid] = v;
         const uint64_t n = n0 + tid;
         if (k0 == 0 && n < a.n) {
-          if (s.splits > 1) {
-            s.sums[split * static_cast<uint64_t>(a.n) + n] = v;
-          } else if (a.dbias) {
-            store_param(a.dbias, n, a.dw_dtype, v + (a.accumulate ? load_param(a.dbias, n, a.dw_dtype) : 0.0f));
-          }
+          if (!w.whole) s.sums[w.split * static_cast<uint64_t>(a.n) + n] = v;
+          else if (a.dbias) wgrad_write_bias(a, n, v);
         }
       }
       __syncthreads();
     }
+    // out through LDS, 16 rows of dW a wave at a time, so that a lane has eight
+    // neighbours of k; the operands' last reads lie before the loop's barrier
+    float* const mine = reinterpret_cast<float*>(&xs[0][0]) + wave * 16 * kOut;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t ln = wn + 16 * j + lane % 16;
-      const uint64_t n = n0 + ln;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(mine + lane % 16 * kOut + 16 * i + lane / 16 * 4) = acc[i][j];
+      const uint32_t lk = wk + lane % 8 * 8;
+      const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
+#pragma unroll 1
+      for (uint32_t q = lane / 8; q < 16; q += 8) {
+        const uint32_t ln = wn + 16 * j + q;
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint64_t k = k0 + wk + 16 * i + lane / 16 * 4 + e;
-          if (n >= a.n || k >= a.k) continue;
-          float v = acc[i][j][e];
-          if (s.splits > 1) {
-            s.part[(split * static_cast<uint64_t>(a.n) + n) * a.k + k] = v;
-            continue;
-          }
-          if (a.col_scale) v *= load_param(a.col_scale, k, a.param_dtype);
-          if (SUMS && a.col_shift) v += colsum[0][ln] * load_param(a.col_shift, k, a.param_dtype);
-          const uint64_t at = n * a.dw.stride + k;
-          if (a.accumulate) v += load_param(a.dw.data, at, a.dw_dtype);
-          store_param(a.dw.data, at, a.dw_dtype, v);
-        }
+        for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + lane % 8 * 8 + e];
+        if (!w.whole)
+          store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + lk), v, 8);
+        else if (n0 + ln < a.n && in > 0)
+          wgrad_write8(a, n0 + ln, k0 + lk, in, SUMS ? colsum[0][ln] : 0.0f, v);
       }
     }
     __syncthreads();
   }
 }
 
-// The splits' sums, in order, with the columns' scale and shift.
-__global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTiles s, int with_sums) {
-  const uint64_t per_row = (a.k + kThreads - 1) / kThreads, items = per_row * a.n;
-  for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const uint64_t n = it / per_row, k = it % per_row * kThreads + threadIdx.x;
-    float sum = 0;
-    if (with_sums)
-      for (uint32_t p = 0; p < s.splits; ++p) sum += s.sums[p * static_cast<uint64_t>(a.n) + n];
-    if (k == 0 && a.dbias)
-      store_param(a.dbias, n, a.dw_dtype, sum + (a.accumulate ? load_param(a.dbias, n, a.dw_dtype) : 0.0f));
-    if (k >= a.k) continue;
-    float v = 0;
-    for (uint32_t p = 0; p < s.splits; ++p) v += s.part[(p * static_cast<uint64_t>(a.n) + n) * a.k + k];
-    if (a.col_scale) v *= load_param(a.col_scale, k, a.param_dtype);
-    if (a.col_shift) v += sum * load_param(a.col_shift, k, a.param_dtype);
-    const uint64_t at = n * a.dw.stride + k;
-    if (a.accumulate) v += load_param(a.dw.data, at, a.dw_dtype);
-    store_param(a.dw.data, at, a.dw_dtype, v);
+// ---- large products of a bf16 dY -------------------------------------------------------
+// 256 x 256 of dW a block, four waves of 128 x 128, one block a CU: at 64 x 64
+// a wave the LDS reads alone take as long as the products (128 B a clock;
+// 512 B a 16 x 16 x 32 product's two operands against its 16 clocks, halved by
+// each doubling of a wave's side).  Tokens come in steps of 32 through two LDS
+// buffers; a thread's loads run two to three steps ahead in registers, and the
+// operands of a half step are read while the half before it multiplies, so one
+// barrier a step is all that a wave waits for.
+//
+// A row of 256 columns is 16 slots of 32 bytes; slot c of token r lies at
+// c ^ 2 (r % 4), which spreads the four tokens that a transposing read takes
+// from a column over the banks.  Of X's columns, where a thread writes 16, the
+// first eight of every 16 are in the first eight slots and the others behind
+// them, so that the threads' 16 bytes lie side by side (two writes 32 bytes
+// apart would meet in the banks); a wave's 128 of k are therefore every other
+// eight.
+constexpr uint32_t kBigTile = 256;
+constexpr uint32_t kBigRow = kBigTile * 2;          // bytes
+constexpr uint32_t kBigBuf = kStep * kBigRow;       // bytes of one operand's step
+constexpr uint32_t kBigOut = 128 + 4;               // floats from row to row on their way out
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+// Kinds of instructions, for their order.
+constexpr int kValu = 0x2, kMfma = 0x8, kVmemRead = 0x20, kLdsRead = 0x100, kLdsWrite = 0x200;
+// What a thread holds of a step: 4 x 8 of dY, 2 x 16 codes of X.
+struct BigStage {
+  u32x4 dy[4];
+  u32x4 x[2];
+  uint32_t scale[2];
+};
+
+// The next `rows` of an operand, 32 at most: an offset past the last one's end
+// reads zeros; past another's end it reads the row behind it, whose columns
+// are not stored.
+__device__ __forceinline__ tile_t step_tile(uint64_t base, int rows, uint32_t pitch, uint32_t width) {
+  const int bytes = (rows - 1) * static_cast<int>(pitch) + static_cast<int>(width);
+  return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0);
+}
+
+__global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTiles s) {
+  // dY, dY, X, X; at the end the waves' 32 rows of 128
+  __shared__ __align__(256) uint8_t lds[4 * 32 * kBigOut * 4 > 4 * kBigBuf ? 4 * 32 * kBigOut * 4 : 4 * kBigBuf];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  lds_u8* const base = (lds_u8*)lds;
+  // where the thread's share of a step comes from and goes to
+  const uint32_t dr = tid / 32, dc = tid % 32, xr = tid / 16, xc = tid % 16;
+  const uint32_t dy_pitch = static_cast<uint32_t>(a.dy.stride * 2), x_pitch = static_cast<uint32_t>(a.x.code_stride);
+  const uint32_t s_pitch = static_cast<uint32_t>(a.x.scale_stride);
+  const uint32_t dy_from = dr * dy_pitch + dc * 16, x_from = xr * x_pitch + xc * 16, s_from = xr * s_pitch + xc / 2;
+  lds_u8* const dy_to = base + dr * kBigRow + (dc / 2 ^ dr % 4 * 2) * 32 + dc % 2 * 16;
+  lds_u8* const x_to = base + 2 * kBigBuf + xr * kBigRow + (xc / 2 ^ xr % 4 * 2) * 32 + xc % 2 * 16;
+  // where the wave's operands are: a lane reads column lane % 32, tokens lane / 32 * 8 and on
+  const uint32_t wk = wave % 2 * 128, wn = wave / 2 * 128;
+  const uint32_t x4 = lane % 16 / 4;  // token of the four that the lane's address names
+  const uint32_t row = lane / 32 * 8 + x4, half = lane / 16 % 2;
+  lds_u8 *x_at[4], *dy_at[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t at = row * kBigRow + (2 * (i ^ x4) + half) * 32 + lane % 4 * 8;
+    x_at[i] = base + 2 * kBigBuf + at + wk * 2;
+    dy_at[i] = base + at + wn * 2;
+  }
+  const uint64_t items = s.full + (s.tiles - s.full) * s.splits;
+  for (uint64_t b = blockIdx.x; b < items; b += gridDim.x) {
+    const WgradItem w = wgrad_item(s, a.rows, b);
+    const uint32_t n0 = w.n0, k0 = w.k0;
+    const uint64_t t_begin = w.t_begin, t_end = w.t_end;
+    // the next step to load; nothing is left of one behind the last
+    int left = static_cast<int>(t_end - t_begin);
+    uint64_t dy_next = a.dy.data + (t_begin * a.dy.stride + n0) * 2;
+    uint64_t x_next = a.x.codes + t_begin * a.x.code_stride + k0;
+    uint64_t s_next = a.x.scales + t_begin * a.x.scale_stride + k0 / kActBlock;
+    const uint32_t dy_width = (a.n - n0) * 2, x_width = a.k - k0, s_width = (x_width + kActBlock - 1) / kActBlock;
+    auto load = [&](BigStage& g) {
+      const int rows = left < static_cast<int>(kStep) ? left : static_cast<int>(kStep);
+      const tile_t td = step_tile(dy_next, rows, dy_pitch, dy_width);
+      const tile_t tx = step_tile(x_next, rows, x_pitch, x_width);
+      const tile_t ts = step_tile(s_next, rows, s_pitch, s_width);
+      left -= kStep;
+      dy_next += static_cast<uint64_t>(dy_pitch) * kStep;
+      x_next += static_cast<uint64_t>(x_pitch) * kStep;
+      s_next += static_cast<uint64_t>(s_pitch) * kStep;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g.dy[i] = __builtin_amdgcn_raw_buffer_load_b128(td, dy_from, i * 8 * dy_pitch, 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        g.x[i] = __builtin_amdgcn_raw_buffer_load_b128(tx, x_from, i * 16 * x_pitch, 0);
+        g.scale[i] = __builtin_amdgcn_raw_buffer_load_b8(ts, s_from, i * 16 * s_pitch, 0);
+      }
+    };
+    // a step's share in eight writes, a half step's operands in eight reads
+    auto store = [&](const BigStage& g, uint32_t buf, int part) {
+      if (part < 4) {
+        *(lds_u32x4*)(dy_to + buf * kBigBuf + part * 8 * kBigRow) = g.dy[part];
+        return;
+      }
+      const int i = part / 2 - 2, h = part % 2;
+      const float scale = __uint_as_float(g.scale[i] << 23);
+      const u32x2 lo = decode4(g.x[i][2 * h], scale), hi = decode4(g.x[i][2 * h + 1], scale);
+      *(lds_u32x4*)(x_to + buf * kBigBuf + i * 16 * kBigRow + h * 256) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    bf16x8 xf[2][4], df[2][4];
+    auto fetch = [&](uint32_t to, uint32_t buf, uint32_t h, int part) {
+      // in the order in which the products want them
+      lds_u8* const p = (part == 0 ? x_at[0] : part < 5 ? dy_at[part - 1] : x_at[part - 4]) + buf * kBigBuf + h * 16 * kBigRow;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * kBigRow));
+      const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      if (part == 0) xf[to][0] = v;
+      else if (part < 5) df[to][part - 1] = v;
+      else xf[to][part - 4] = v;
+    };
+    f32x16 acc[4][4];  // [k][n] tiles of 32: a lane holds four runs of 4 of k for one n
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+    auto multiply = [&](uint32_t of, int i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf[of][i], df[of][j], acc[i][j], 0, 0, 0);
+    };
+    // One step, out of buffer `buf`; g holds the one behind it.  Each product
+    // takes 32 clocks of the matrix core; the order below lays the other
+    // instructions between them, so that neither the LDS of the CU, which the
+    // four waves share, nor the wave's issue holds the products up.
+    auto step = [&](BigStage& g, uint32_t buf) {
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        fetch(1, buf, 1, p);
+        store(g, buf ^ 1, p);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) multiply(0, i);
+      multiply(1, 0);
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        if (p >= 4) __builtin_amdgcn_sched_group_barrier(kValu, 5, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      __syncthreads();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int p = 0; p < 8; ++p) fetch(0, buf ^ 1, 0, p);
+      load(g);
+#pragma unroll
+      for (int i = 1; i < 4; ++i) multiply(1, i);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    BigStage g0, g1;  // the odd steps on their way, and the even ones
+    load(g1);
+    load(g0);
+#pragma unroll
+    for (int p = 0; p < 8; ++p) store(g1, 0, p);
+    load(g1);
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 8; ++p) fetch(0, 0, 0, p);
+    for (uint64_t t = t_begin; t < t_end; t += 2 * kStep) {  // a step behind the last multiplies zeros
+      step(g0, 0);
+      step(g1, 1);
+    }
+    __syncthreads();
+
+    // out of the registers through LDS, 32 rows of dW a wave at a time, so
+    // that a lane has eight neighbours of k (every other eight: see above)
+    float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * kBigOut;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x4 v = {acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
+          *reinterpret_cast<f32x4*>(mine + lane % 32 * kBigOut + 32 * i + 8 * r + lane / 32 * 4) = v;
+        }
+      const uint32_t lk = lane % 16 * 16 + wk / 16;
+      const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
+#pragma unroll 1
+      for (uint32_t q = lane / 16; q < 32; q += 4) {
+        const uint32_t ln = wn + 32 * j + q;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = mine[q * kBigOut + lane % 16 * 8 + e];
+        if (!w.whole)
+          store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + lk), v, 8);
+        else if (n0 + ln < a.n && in > 0)
+          wgrad_write8(a, n0 + ln, k0 + lk, in, a.col_shift ? s.sums[n0 + ln] : 0.0f, v);
+      }
+    }
+    __syncthreads();
   }
 }
 
-// Splits of the tokens: as many as fill the chip with tiles, of 128 tokens at least.
-WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k) {
+// The parts' sums, in order, with the columns' scale and shift.
+__global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTiles s) {
+  const uint32_t per_row = s.tile / 8, per_tile = s.tile * per_row;
+  const uint64_t items = (s.tiles - s.full) * per_tile;
+  for (uint64_t it = blockIdx.x * static_cast<uint64_t>(kThreads) + threadIdx.x; it < items;
+       it += gridDim.x * static_cast<uint64_t>(kThreads)) {
+    const uint64_t tile = s.full + it / per_tile;
+    const uint32_t ln = static_cast<uint32_t>(it % per_tile) / per_row, lk = static_cast<uint32_t>(it % per_row) * 8;
+    uint32_t n0, k0;
+    wgrad_place(s, tile, n0, k0);
+    const uint64_t n = n0 + ln;
+    const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
+    if (n >= a.n || in <= 0) continue;
+    float v[8] = {}, f[8], sum = 0;
+#pragma unroll 4
+    for (uint32_t p = 0; p < s.splits; ++p) {
+      unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, tile, p, ln) + lk)), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += f[e];
+    }
+    const bool bias = a.dbias && !s.big && k0 + lk == 0;
+    if (a.col_shift || bias)
+      for (uint32_t p = 0; p < s.sum_parts; ++p) sum += s.sums[p * static_cast<uint64_t>(a.n) + n];
+    if (bias) wgrad_write_bias(a, n, sum);
+    wgrad_write8(a, n, k0 + lk, in, sum, v);
+  }
+}
+
+// Column sums of a bf16 dY, for wgrad_big_kernel: 512 columns and a part of the
+// tokens a block, then the parts in order.
+constexpr uint32_t kSumCols = 512, kSumParts = 64;
+__global__ __launch_bounds__(kThreads) void wgrad_sums_kernel(Wgrad a, float* parts) {
+  __shared__ float sums[kThreads / 64][kSumCols];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t chunks = (a.n + kSumCols - 1) / kSumCols, items = chunks * kSumParts;
+  for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const uint64_t c0 = it % chunks * kSumCols, p = it / chunks;
+    const uint64_t t0 = a.rows * p / kSumParts, t1 = a.rows * (p + 1) / kSumParts;
+    const int in = static_cast<int>(a.n) - static_cast<int>(c0 + 8 * lane);
+    float f[8], v[8] = {};
+#pragma unroll 4
+    for (uint64_t t = t0 + wave; t < t1; t += kThreads / 64) {
+      unpack8<kBf16>(load8_raw<kBf16>(a.dy.data + (t * a.dy.stride + c0 + 8 * lane) * 2, in), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += f[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = v[e];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kSumCols; i += kThreads) {
+      const uint64_t n = c0 + i % 64 * 8 + i / 64;
+      float w = sums[0][i];
+      for (uint32_t q = 1; q < kThreads / 64; ++q) w += sums[q][i];
+      if (n < a.n) parts[p * a.n + n] = w;
+    }
+    __syncthreads();
+  }
+}
+__global__ __launch_bounds__(64) void wgrad_sums_join_kernel(Wgrad a, const float* parts, float* sums) {
+  for (uint64_t n = blockIdx.x * 64ull + threadIdx.x; n < a.n; n += gridDim.x * 64ull) {
+    float v = 0;
+#pragma unroll 16
+    for (uint32_t p = 0; p < kSumParts; ++p) v += parts[p * static_cast<uint64_t>(a.n) + n];
+    sums[n] = v;
+    if (a.dbias) wgrad_write_bias(a, n, v);
+  }
+}
+
+// The cut.  More parts shorten what a block takes over the tokens and cost
+// their sums' way through memory; the figures are measured (us): a step of 32
+// tokens takes a block of 256 columns 0.88 and one of 128 about 1.0 (two a CU;
+// three times the products for an fp32 dY), a part's sums 0.105 and 0.026
+// there and back, the join's launch 4.
+WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big) {
   WgradTiles s{};
-  s.tn = static_cast<uint32_t>((n + kTile - 1) / kTile);
-  s.tk = static_cast<uint32_t>((k + kTile - 1) / kTile);
-  const uint64_t tiles = static_cast<uint64_t>(s.tn) * s.tk;
-  uint64_t splits = tiles >= 256 ? 1 : 512 / tiles;
-  const uint64_t most = rows / 128;
-  if (splits > most) splits = most;
-  if (splits > 64) splits = 64;
-  if (splits < 1) splits = 1;
-  s.per_split = ((rows + splits - 1) / splits + kStep - 1) / kStep * kStep;
-  if (s.per_split == 0) s.per_split = kStep;
-  s.splits = rows ? static_cast<uint32_t>((rows + s.per_split - 1) / s.per_split) : 1;
+  s.big = big;
+  s.tile = big ? kBigTile : kTile;
+  s.tn = static_cast<uint32_t>((n + s.tile - 1) / s.tile);
+  s.tk = static_cast<uint32_t>((k + s.tile - 1) / s.tile);
+  s.tiles = static_cast<uint64_t>(s.tn) * s.tk;
+  const uint64_t at_once = big ? 256 : 512, rest = s.tiles % at_once, steps = (rows + kStep - 1) / kStep;
+  const double step_us = big ? 0.88 : 1.0, part_us = big ? 0.105 : 0.026;
+  uint64_t best = 1;
+  double best_us = steps * step_us;
+  for (uint64_t splits = 2; rest && splits <= at_once / rest && splits <= steps; ++splits) {
+    const double us = (steps + splits - 1) / splits * step_us + splits * rest * part_us + 4.0;
+    if (us < best_us) {
+      best_us = us;
+      best = splits;
+    }
+  }
+  s.per_split = (steps + best - 1) / best * kStep;
+  s.splits = steps ? static_cast<uint32_t>((rows + s.per_split - 1) / s.per_split) : 1;
+  s.full = s.splits > 1 ? s.tiles - rest : s.tiles;
+  s.sum_parts = big ? 1 : s.splits;
   return s;
 }
 
+// The 256-column kernel takes what its loads can: a bf16 dY, rows of whole
+// 16-byte groups, and no tile that is mostly outside.
+bool wgrad_is_big(const Wgrad& a) {
+  const auto pad = [&](uint64_t t) { return (a.n + t - 1) / t * t * ((a.k + t - 1) / t * t); };
+  return a.dtype == kBf16 && a.n % 8 == 0 && a.k % 16 == 0 && a.dy.data % 16 == 0 && a.dy.stride % 8 == 0 &&
+         a.dy.stride < (1u << 25) && a.x.codes % 16 == 0 && a.x.code_stride % 16 == 0 && a.x.code_stride < (1u << 26) &&
+         a.x.scale_stride < (1u << 26) && a.rows < (1u << 30) && pad(kBigTile) * 2 <= pad(kTile) * 3;
+}
+
+// The small kernel takes a whole tile's column sums along and splits every
+// tile or none, so that the parts of a column of tiles are alike.
+WgradTiles wgrad_cut(uint64_t rows, uint64_t n, uint64_t k, bool big) {
+  WgradTiles s = wgrad_tiles(rows, n, k, big);
+  if (!big && s.full && s.full < s.tiles) {
+    s.splits = 1;
+    s.full = s.tiles;
+    s.sum_parts = 1;
+  }
+  return s;
+}
+
+uint64_t wgrad_part_bytes(const WgradTiles& s) { return (s.tiles - s.full) * s.splits * s.tile * s.tile * 4; }
+uint64_t wgrad_space(const WgradTiles& s, uint64_t n) {
+  return wgrad_part_bytes(s) + (s.sum_parts + (s.big ? kSumParts : 0)) * n * 4;
+}
+
 template <int DT>
-void wgrad_of(const Wgrad& a, const WgradTiles& s, bool sums, hipStream_t st) {
-  const uint32_t grid = grid_for(static_cast<uint64_t>(s.tn) * s.tk * s.splits, kThreads);
+void wgrad_of(const Wgrad& a, const WgradTiles& s, uint32_t grid, bool sums, hipStream_t st) {
   if (sums) hipLaunchKernelGGL((wgrad_kernel<DT, true>), dim3(grid), dim3(kThreads), 0, st, a, s);
   else hipLaunchKernelGGL((wgrad_kernel<DT, false>), dim3(grid), dim3(kThreads), 0, st, a, s);
 }
@@ -293,20 +658,36 @@ void wgrad_of(const Wgrad& a, const WgradTiles& s, bool sums, hipStream_t st) {
 }  // namespace
 
 uint64_t wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k) {
-  const WgradTiles s = wgrad_tiles(rows, n, k);
-  return s.splits > 1 ? s.splits * (n * k + n) * 4 : 0;
+  // which tiles a call takes goes by its types and alignment, too
+  const uint64_t big = wgrad_space(wgrad_cut(rows, n, k, true), n);
+  const uint64_t small = wgrad_space(wgrad_cut(rows, n, k, false), n);
+  return big > small ? big : small;
 }
 
 hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
-  WgradTiles s = wgrad_tiles(a.rows, a.n, a.k);
+  WgradTiles s = wgrad_cut(a.rows, a.n, a.k, wgrad_is_big(a));
   s.part = reinterpret_cast<float*>(a.ws);
-  s.sums = s.part + s.splits * static_cast<uint64_t>(a.n) * a.k;
+  s.sums = reinterpret_cast<float*>(a.ws + wgrad_part_bytes(s));
   const bool sums = a.dbias || a.col_shift;
-  if (a.dtype == kBf16) wgrad_of<kBf16>(a, s, sums, st);
-  else wgrad_of<kF32>(a, s, sums, st);
+  const uint32_t grid = grid_for(s.full + (s.tiles - s.full) * s.splits, kThreads);
+  if (s.big) {
+    if (sums) {
+      float* const parts = s.sums + a.n;
+      hipLaunchKernelGGL(wgrad_sums_kernel, dim3(grid_for((a.n + kSumCols - 1) / kSumCols * kSumParts, kThreads)),
+                         dim3(kThreads), 0, st, a, parts);
+      hipLaunchKernelGGL(wgrad_sums_join_kernel, dim3(grid_for((a.n + 63) / 64, 64)), dim3(64), 0, st, a,
+                         static_cast<const float*>(parts), s.sums);
+    }
+    hipLaunchKernelGGL(wgrad_big_kernel, dim3(grid), dim3(kThreads), 0, st, a, s);
+  } else if (a.dtype == kBf16) {
+    wgrad_of<kBf16>(a, s, grid, sums, st);
+  } else {
+    wgrad_of<kF32>(a, s, grid, sums, st);
+  }
   if (s.splits > 1) {
-    const uint64_t items = (a.k + kThreads - 1) / kThreads * static_cast<uint64_t>(a.n);
-    hipLaunchKernelGGL(wgrad_join_kernel, dim3(grid_for(items, kThreads)), dim3(kThreads), 0, st, a, s, sums ? 1 : 0);
+    const uint64_t items = (s.tiles - s.full) * s.tile * s.tile / 8;
+    hipLaunchKernelGGL(wgrad_join_kernel, dim3(grid_for((items + kThreads - 1) / kThreads, kThreads)), dim3(kThreads), 0,
+                       st, a, s);
   }
   return hipGetLastError();
 }
