@@ -3,9 +3,10 @@
 //   out[t] = scale * W[token[t] - first]            (zeros for a token outside the table)
 //   dW[v] (+)= scale * sum over t with token[t] - first = v of dout[t]
 //
-// Both are bound by memory.  The gradient sorts the tokens, so that every row
-// of the table is written once, and sums a row's tokens in the order of their
-// positions, in fp32: the result does not depend on how blocks are scheduled.
+// Both are bound by memory; of the gradient's, most is the table itself, which
+// is written whole.  The gradient sorts the tokens and sums a row's in the order
+// of their positions, in fp32: the result does not depend on how blocks are
+// scheduled.
 #include "lc_ops_device.h"
 
 namespace lc {
@@ -58,10 +59,35 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, ui
   }
 }
 
+// ---- clearing the table -------------------------------------------------------------
+// A block clears `per` rows, about 256 KB and 64 of them at most, or those of
+// them that are not in `skip`.
+struct Fill {
+  uint64_t data, pitch, first, rows;  // of the table: its first row, bytes a row; rows first to rows - 1
+  uint32_t bytes;                     // of a row that count, even
+  uint32_t per;
+};
+__host__ inline uint64_t fill_blocks(const Fill& f) { return (f.rows - f.first + f.per - 1) / f.per; }
+__device__ __forceinline__ void fill_rows(const Fill& f, uint64_t block, uint64_t skip) {
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t r0 = f.first + block * f.per;
+  for (uint32_t i = wave; i < f.per && r0 + i < f.rows; i += blockDim.x / 64) {
+    if (skip >> i & 1) continue;
+    const uint64_t p = f.data + (r0 + i) * f.pitch;
+    for (uint32_t at = lane * 16; at + 16 <= f.bytes; at += 64 * 16) st_any(reinterpret_cast<uint8_t*>(p + at), u32x4{0, 0, 0, 0});
+    const uint32_t tail = f.bytes & ~15u;
+    if (tail + lane * 2 < f.bytes) *(g_u16*)(p + tail + lane * 2) = 0;
+  }
+}
+
 // ---- sorting the tokens ------------------------------------------------------------
-// Up to kRankTokens one launch counts, for every token, the tokens that come
+// Few tokens need no order (embed_direct_kernel, below).  Up to kRankTokens one launch counts, for every token, the tokens that come
 // before it (a smaller row, or the same row at an earlier position); beyond
-// that a radix sort of kDigitBits a pass, two launches a pass.
+// that a radix sort of kDigitBits a pass, two launches a pass.  The sort's few
+// blocks leave the chip to others, which clear the table meanwhile, rows with a
+// token and without: writing the former twice costs less than the sort's time
+// alone (16384 tokens into 128256 x 2048: 152 us where the sums' launch cleared
+// the rows without a token).
 constexpr uint32_t kRankTokens = 8192;
 constexpr uint32_t kRankThreads = 256;
 constexpr uint32_t kRankOwn = 32;  // tokens of a block; its 8 slices of threads share the others
@@ -70,16 +96,22 @@ constexpr uint32_t kSortThreads = 512;
 constexpr uint32_t kSortWaves = kSortThreads / 64;
 static_assert(kSortThreads == kDigits, "one thread a digit");
 
-__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedBwd a, uint32_t* keys, uint32_t* pos) {
+__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedBwd a, Fill fill, uint32_t fill_from,
+                                                                  uint32_t* keys, uint32_t* pos) {
   __shared__ __align__(16) uint32_t all[kRankTokens];
   __shared__ uint32_t count[kRankThreads / kRankOwn][kRankOwn];
+  if (blockIdx.x >= fill_from) {
+    for (uint64_t b = blockIdx.x - fill_from; fill.first + b * fill.per < fill.rows; b += gridDim.x - fill_from)
+      fill_rows(fill, b, 0);
+    return;
+  }
   const uint32_t n = static_cast<uint32_t>(a.n);
   const uint32_t padded = (n + kRankOwn - 1) / kRankOwn * kRankOwn;
   for (uint32_t i = threadIdx.x; i < padded; i += kRankThreads)
     all[i] = i < n ? token_row(a.tokens, a.token64, i, a.first, a.vocab) : 0xFFFFFFFFu;
   __syncthreads();
   const uint32_t own = threadIdx.x % kRankOwn, slice = threadIdx.x / kRankOwn;
-  for (uint32_t base = blockIdx.x * kRankOwn; base < n; base += gridDim.x * kRankOwn) {
+  for (uint32_t base = blockIdx.x * kRankOwn; base < n; base += fill_from * kRankOwn) {
     const uint32_t i = base + own, key = all[i];
     uint32_t before = 0;
     // groups of kRankOwn tokens, dealt out to the slices
@@ -113,12 +145,12 @@ __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(EmbedBwd a, ui
   }
 }
 
-// The tile of a radix pass: a multiple of kSortThreads that leaves at most kSortTiles of them.
-constexpr uint32_t kSortTiles = 512;
+// The tile of a radix pass: a multiple of kSortThreads that leaves at most
+// kSortTiles of them, for every tile reads the counts of all.
+constexpr uint32_t kSortTiles = 64;
 __host__ __device__ inline uint32_t sort_tile(uint64_t n) {
   const uint64_t per = (n + kSortTiles - 1) / kSortTiles;
-  const uint64_t t = (per + kSortThreads - 1) / kSortThreads * kSortThreads;
-  return static_cast<uint32_t>(t < 4 * kSortThreads ? 4 * kSortThreads : t);
+  return static_cast<uint32_t>((per + kSortThreads - 1) / kSortThreads * kSortThreads);
 }
 
 // keys null: the tokens themselves, at position i.
@@ -126,11 +158,17 @@ __device__ __forceinline__ uint32_t sort_key(const EmbedBwd& a, const uint32_t* 
   return keys ? keys[i] : token_row(a.tokens, a.token64, i, a.first, a.vocab);
 }
 
-__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(EmbedBwd a, const uint32_t* keys, uint32_t shift,
-                                                                   uint32_t tile, uint32_t* hist) {
+__global__ __launch_bounds__(kSortThreads) void embed_count_kernel(EmbedBwd a, Fill fill, uint32_t fill_from,
+                                                                   const uint32_t* keys, uint32_t shift, uint32_t tile,
+                                                                   uint32_t* hist) {
   __shared__ uint32_t bins[kDigits];
+  if (blockIdx.x >= fill_from) {
+    for (uint64_t b = blockIdx.x - fill_from; fill.first + b * fill.per < fill.rows; b += gridDim.x - fill_from)
+      fill_rows(fill, b, 0);
+    return;
+  }
   const uint64_t tiles = (a.n + tile - 1) / tile;
-  for (uint64_t b = blockIdx.x; b < tiles; b += gridDim.x) {
+  for (uint64_t b = blockIdx.x; b < tiles; b += fill_from) {
     bins[threadIdx.x] = 0;
     __syncthreads();
     const uint64_t end = b * tile + tile < a.n ? b * tile + tile : a.n;
@@ -142,18 +180,24 @@ __global__ __launch_bounds__(kSortThreads) void embed_count_kernel(EmbedBwd a, c
   }
 }
 
-__global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a, const uint32_t* keys,
-                                                                     const uint32_t* pos, uint32_t shift, uint32_t tile,
-                                                                     const uint32_t* hist, uint32_t* keys_out,
-                                                                     uint32_t* pos_out) {
+__global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a, Fill fill, uint32_t fill_from,
+                                                                     const uint32_t* keys, const uint32_t* pos,
+                                                                     uint32_t shift, uint32_t tile, const uint32_t* hist,
+                                                                     uint32_t* keys_out, uint32_t* pos_out) {
   __shared__ uint32_t next[kDigits];              // where a digit's next key goes
   __shared__ uint32_t wave_count[kSortWaves][kDigits];
   __shared__ uint32_t wave_total[kSortWaves];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint64_t tiles = (a.n + tile - 1) / tile;
-  for (uint64_t b = blockIdx.x; b < tiles; b += gridDim.x) {
+  if (blockIdx.x >= fill_from) {
+    for (uint64_t b = blockIdx.x - fill_from; fill.first + b * fill.per < fill.rows; b += gridDim.x - fill_from)
+      fill_rows(fill, b, 0);
+    return;
+  }
+  const uint32_t tiles = static_cast<uint32_t>((a.n + tile - 1) / tile);
+  for (uint64_t b = blockIdx.x; b < tiles; b += fill_from) {
     uint32_t total = 0, before = 0;
-    for (uint64_t j = 0; j < tiles; ++j) {
+#pragma unroll 16
+    for (uint32_t j = 0; j < tiles; ++j) {
       const uint32_t h = hist[j * kDigits + tid];
       total += h;
       before += j < b ? h : 0;
@@ -219,7 +263,6 @@ __global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a,
 // over the chip like any others.
 constexpr uint32_t kSumThreads = 256;
 constexpr uint32_t kSumCols = 512;
-constexpr uint32_t kFillRows = 64;  // rows of the table that one block clears, where no token has them
 
 __host__ __device__ inline uint32_t sum_run(uint64_t n) {  // sorted positions of a tile: at most 2048 tiles up to n = 2^31
   uint64_t r = 16;
@@ -318,46 +361,28 @@ __device__ void sum_tile(const SumArgs& a, uint64_t item) {
   flush(cur == right);
 }
 
-// Zeros into the rows of the table that no token has.
-template <int GDT>
-__device__ void fill_rows(const SumArgs& a, uint64_t block) {
-  __shared__ uint64_t touched;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t r0 = block * kFillRows;
-  if (wave == 0) {  // each lane looks for its row among the sorted tokens
-    uint64_t lo = 0, hi = a.n;
-    const uint64_t row = r0 + lane;
-    while (__ballot(lo < hi)) {
-      const uint64_t mid = (lo + hi) / 2;
-      const bool on = lo < hi;
-      const uint32_t k = on ? a.keys[mid] : 0;
-      if (on && k < row) lo = mid + 1;
-      else if (on) hi = mid;
-    }
-    const uint64_t found = __ballot(lo < a.n && a.keys[lo < a.n ? lo : 0] == row);
-    if (lane == 0) touched = found;
+// The first of the n sorted keys that is not below `key`: the wave looks at 64
+// of them at once, evenly spread over what is left.
+__device__ __forceinline__ uint64_t first_not_below(const uint32_t* keys, uint64_t n, uint64_t key) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint64_t lo = 0, hi = n;  // keys before lo are below, keys from hi on are not
+  while (lo < hi) {
+    const uint64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const uint64_t below = __ballot(at < hi && keys[at < hi ? at : lo] < key);
+    const uint32_t c = __popcll(below);  // the samples are sorted: the first c are below
+    const uint64_t next = lo + c * step;
+    lo = c ? lo + (c - 1) * step + 1 : lo;
+    hi = next < hi ? next : hi;
   }
-  __syncthreads();
-  const uint64_t skip = touched;
-  __syncthreads();  // a block that takes another range writes it anew
-  const float zero[8] = {};
-  const uint32_t groups = (a.dim + 7) / 8;
-  for (uint32_t i = wave; i < kFillRows && r0 + i < a.vocab; i += kSumThreads / 64) {
-    if (skip >> i & 1) continue;
-    const uint64_t p = a.dw.data + (r0 + i) * a.dw.stride * kEsz<GDT>;
-    for (uint32_t g = lane; g < groups; g += 64) store8<GDT>(p + 8ull * kEsz<GDT> * g, zero, in_group(a.dim, g));
-  }
+  return lo;
 }
 
 template <int DDT, int GDT>
-__global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(SumArgs a, uint64_t sum_blocks, uint64_t fill_blocks) {
-  for (uint64_t b = blockIdx.x; b < sum_blocks + fill_blocks; b += gridDim.x) {
-    if (b < sum_blocks) {
-      const uint64_t item = b * (kSumThreads / 64) + (threadIdx.x >> 6);
-      if (item < static_cast<uint64_t>(a.tiles) * a.chunks) sum_tile<DDT, GDT>(a, item);
-    } else {
-      fill_rows<GDT>(a, b - sum_blocks);
-    }
+__global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(SumArgs a) {
+  const uint64_t items = static_cast<uint64_t>(a.tiles) * a.chunks;
+  for (uint64_t b = blockIdx.x; b * (kSumThreads / 64) < items; b += gridDim.x) {
+    const uint64_t item = b * (kSumThreads / 64) + (threadIdx.x >> 6);
+    if (item < items) sum_tile<DDT, GDT>(a, item);
   }
 }
 
@@ -374,25 +399,32 @@ __global__ __launch_bounds__(kSumThreads) void embed_join_kernel(SumArgs a) {
     const uint64_t b0 = static_cast<uint64_t>(tile) * a.run, b1 = b0 + a.run;  // b1 < n: not the last tile
     const uint32_t key = a.keys[b1 - 1];
     if (key == a.vocab || a.keys[b1] != key || (b0 && a.keys[b0 - 1] == key)) continue;
-    // the last tile that holds the row: tiles whose first position has it are consecutive
-    uint32_t lo = tile + 1, hi = a.tiles - 1;
-    while (lo < hi) {
-      const uint32_t mid = (lo + hi + 1) / 2;
-      if (a.keys[static_cast<uint64_t>(mid) * a.run] == key) lo = mid;
-      else hi = mid - 1;
-    }
+    // the last tile that holds the row
+    const uint64_t behind = b1 + first_not_below(a.keys + b1, a.n - b1, static_cast<uint64_t>(key) + 1);
+    const uint32_t lo = static_cast<uint32_t>((behind - 1) / a.run);
     const uint32_t count = lo - tile + 1;  // [tile][1], then [tile + 1][0] to [lo][0]
     const uint32_t g = chunk * (kSumCols / 8) + lane;
     const int in = in_group(a.dim, g);
     float acc[8] = {};
     const uint32_t j1 = static_cast<uint32_t>(static_cast<uint64_t>(count) * (wave + 1) / W);
-    for (uint32_t j = static_cast<uint32_t>(static_cast<uint64_t>(count) * wave / W); j < j1; ++j) {
-      if (in <= 0) break;
-      float f[8];
-      const float* p = j ? sum_part(a, tile + j, 0) : sum_part(a, tile, 1);
-      unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(p) + 32ull * g, in), f);
+    constexpr uint32_t U = 8;  // parts in flight
+    for (uint32_t j0 = static_cast<uint32_t>(static_cast<uint64_t>(count) * wave / W); j0 < j1; j0 += U) {
+      Raw8<kF32> r[U];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += f[e];
+      for (uint32_t u = 0; u < U; ++u) {
+        const uint32_t j = j0 + u;
+        const float* p = j ? sum_part(a, tile + j, 0) : sum_part(a, tile, 1);
+        r[u] = load8_raw<kF32>(reinterpret_cast<uint64_t>(p) + 32ull * g, j < j1 ? in : 0);
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < U; ++u) {
+        float f[8];
+        unpack8<kF32>(r[u], f);
+        if (j0 + u < j1) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] += f[e];
+        }
+      }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = acc[e];
@@ -407,6 +439,121 @@ __global__ __launch_bounds__(kSumThreads) void embed_join_kernel(SumArgs a) {
   }
 }
 
+// ---- few tokens: one launch ---------------------------------------------------------------
+// A block takes a token, looks for it among all of them, and where it is the
+// first of its row sums the row; its four waves share the row's columns, or,
+// of few columns, its tokens.  Other blocks clear the rows without a token.
+constexpr uint32_t kDirectTokens = 1024;
+constexpr uint32_t kDirectWaves = kSumThreads / 64;
+
+template <int DDT, int GDT>
+__global__ __launch_bounds__(kSumThreads) void embed_direct_kernel(EmbedBwd a, Fill fill, uint64_t fills) {
+  constexpr uint32_t W = kDirectWaves, PER = kDirectTokens / W;
+  constexpr int U = 8;  // rows in flight
+  __shared__ uint16_t list[W][PER];  // positions of the row's tokens, a quarter of them a wave's find
+  __shared__ uint32_t found[W];
+  __shared__ uint32_t earlier;
+  __shared__ unsigned long long touched;
+  __shared__ float sums[W][kSumCols];
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t n = static_cast<uint32_t>(a.n);
+  for (uint64_t b = blockIdx.x; b < n + fills; b += gridDim.x) {
+    if (b >= n) {
+      const uint64_t r0 = (b - n) * fill.per;
+      if (threadIdx.x == 0) touched = 0;
+      __syncthreads();
+      for (uint32_t j = threadIdx.x; j < n; j += kSumThreads) {
+        const uint64_t row = token_row(a.tokens, a.token64, j, a.first, a.vocab);
+        if (row >= r0 && row < r0 + fill.per) atomicOr(&touched, 1ull << (row - r0));  // any order gives the same
+      }
+      __syncthreads();
+      const uint64_t skip = touched;
+      __syncthreads();
+      fill_rows(fill, b - n, skip);
+      continue;
+    }
+    const uint32_t i = static_cast<uint32_t>(b);
+    const uint32_t row = token_row(a.tokens, a.token64, i, a.first, a.vocab);
+    if (row >= a.vocab) continue;  // the same for the whole block
+    if (threadIdx.x == 0) earlier = 0;
+    __syncthreads();
+    const uint32_t per = (n + W - 1) / W, j0 = wave * per, j1 = j0 + per < n ? j0 + per : n;
+    uint32_t count = 0;
+    for (uint32_t j = j0 + lane; j < j0 + per; j += 64) {  // whole waves
+      const bool same = j < j1 && token_row(a.tokens, a.token64, j, a.first, a.vocab) == row;
+      const uint64_t all = __ballot(same);
+      if (same) {
+        list[wave][count + __popcll(all & ((1ull << lane) - 1))] = static_cast<uint16_t>(j);
+        if (j < i) earlier = 1;
+      }
+      count += __popcll(all);
+    }
+    if (lane == 0) found[wave] = count;
+    __syncthreads();
+    const bool first = earlier == 0;
+    uint32_t start[W + 1] = {};
+#pragma unroll
+    for (uint32_t w = 0; w < W; ++w) start[w + 1] = start[w] + found[w];
+    __syncthreads();
+    if (!first) continue;
+    const uint32_t total = start[W];
+    // token t of the row, in the order of the positions
+    auto position = [&](uint32_t t) {
+      uint32_t w = 0;
+#pragma unroll
+      for (uint32_t q = 1; q < W; ++q) w += t >= start[q];
+      uint32_t from = 0;
+#pragma unroll
+      for (uint32_t q = 0; q < W; ++q) from = q == w ? start[q] : from;
+      return static_cast<uint32_t>(list[w][t - from]);
+    };
+    const uint32_t chunks = (a.dim + kSumCols - 1) / kSumCols;
+    const uint32_t share = chunks == 1 ? 4 : chunks == 2 ? 2 : 1;  // waves of a chunk
+    for (uint32_t c0 = 0; c0 < chunks; c0 += W / share) {
+      const uint32_t chunk = c0 + wave / share, part = wave % share;
+      const uint32_t g = chunk * (kSumCols / 8) + lane;
+      const int in = in_group(a.dim, g);
+      const uint64_t to = a.dw.data + (static_cast<uint64_t>(row) * a.dw.stride + 8ull * g) * kEsz<GDT>;
+      Raw8<GDT> old = load8_raw<GDT>(to, a.accumulate && part == 0 ? in : 0);
+      float acc[8] = {};
+      const uint32_t t1 = total * (part + 1) / share;
+      for (uint32_t t0 = total * part / share; t0 < t1; t0 += U) {
+        Raw8<DDT> r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const uint32_t p = t0 + u < t1 ? position(t0 + u) : 0;
+          r[u] = load8_raw<DDT>(a.dout.data + (p * a.dout.stride + 8ull * g) * kEsz<DDT>, t0 + u < t1 ? in : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float f[8];
+          unpack8<DDT>(r[u], f);
+          if (t0 + u < t1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += f[e];
+          }
+        }
+      }
+      if (share > 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = acc[e];
+        __syncthreads();
+        if (part == 0)
+          for (uint32_t q = 1; q < share; ++q)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += sums[wave + q][e * 64 + lane];
+        __syncthreads();
+      }
+      if (part != 0 || in <= 0) continue;
+      float f[8];
+      unpack8<GDT>(old, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = a.accumulate ? acc[e] * a.scale + f[e] : acc[e] * a.scale;
+      store8<GDT>(to, f, in);
+    }
+  }
+}
+
 uint64_t pad256(uint64_t x) { return (x + 255) / 256 * 256; }
 
 struct BwdRegions {
@@ -415,6 +562,7 @@ struct BwdRegions {
 };
 BwdRegions bwd_regions(uint64_t n, uint64_t dim) {
   BwdRegions r{};
+  if (n <= kDirectTokens) return r;
   r.run = sum_run(n);
   r.tiles = static_cast<uint32_t>((n + r.run - 1) / r.run);
   const bool radix = n > kRankTokens;
@@ -450,15 +598,43 @@ hipError_t embed_fwd_of(const EmbedFwd& a, hipStream_t st) {
 template <int DDT, int GDT>
 hipError_t embed_sums(const SumArgs& s, hipStream_t st) {
   const uint64_t items = static_cast<uint64_t>(s.tiles) * s.chunks;
-  const uint64_t sum_blocks = (items + kSumThreads / 64 - 1) / (kSumThreads / 64);
-  const uint64_t fill_blocks = s.accumulate ? 0 : (s.vocab + kFillRows - 1) / kFillRows;
-  if (sum_blocks + fill_blocks == 0) return hipSuccess;
-  hipLaunchKernelGGL((embed_sum_kernel<DDT, GDT>), dim3(grid_for(sum_blocks + fill_blocks, kSumThreads)),
-                     dim3(kSumThreads), 0, st, s, sum_blocks, fill_blocks);
+  hipLaunchKernelGGL((embed_sum_kernel<DDT, GDT>),
+                     dim3(grid_for((items + kSumThreads / 64 - 1) / (kSumThreads / 64), kSumThreads)), dim3(kSumThreads), 0,
+                     st, s);
   if (s.tiles > 1)
     hipLaunchKernelGGL((embed_join_kernel<GDT>),
                        dim3(grid_for(static_cast<uint64_t>(s.tiles - 1) * s.chunks, kSumThreads)), dim3(kSumThreads), 0,
                        st, s);
+  return hipGetLastError();
+}
+
+Fill whole_table(const EmbedBwd& a) {
+  const uint64_t e = a.dw_dtype == kBf16 ? 2 : 4;
+  const uint64_t bytes = a.dim * e, per = bytes < 262144 ? 262144 / bytes : 1;
+  return Fill{a.dw.data, a.dw.stride * e, 0, a.accumulate ? 0 : a.vocab, static_cast<uint32_t>(bytes),
+              static_cast<uint32_t>(per < 64 ? per : 64)};
+}
+
+// Blocks for `work` items and behind them for the rows to clear; a capped grid
+// leaves some of each.
+struct SortGrid {
+  uint32_t fill_from, blocks;
+};
+SortGrid sort_grid(uint64_t work, const Fill& f, uint32_t threads) {
+  SortGrid g;
+  const uint64_t fills = fill_blocks(f);
+  const uint32_t cap = grid_for(~0ull >> 1, threads);
+  g.fill_from = static_cast<uint32_t>(work < cap / 2 ? work : cap / 2);
+  g.blocks = g.fill_from + static_cast<uint32_t>(fills < cap - g.fill_from ? fills : cap - g.fill_from);
+  return g;
+}
+
+template <int DDT, int GDT>
+hipError_t embed_direct(const EmbedBwd& a, hipStream_t st) {
+  const Fill f = whole_table(a);
+  if (a.n + fill_blocks(f) > 0)
+    hipLaunchKernelGGL((embed_direct_kernel<DDT, GDT>), dim3(grid_for(a.n + fill_blocks(f), kSumThreads)),
+                       dim3(kSumThreads), 0, st, a, f, fill_blocks(f));
   return hipGetLastError();
 }
 
@@ -471,6 +647,11 @@ hipError_t launch_embed_fwd(const EmbedFwd& a, hipStream_t st) {
 uint64_t embed_bwd_workspace(uint64_t n, uint64_t dim) { return bwd_regions(n, dim).end; }
 
 hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
+  if (a.n <= kDirectTokens) {
+    if (a.dout_dtype == kBf16)
+      return a.dw_dtype == kBf16 ? embed_direct<kBf16, kBf16>(a, st) : embed_direct<kBf16, kF32>(a, st);
+    return a.dw_dtype == kBf16 ? embed_direct<kF32, kBf16>(a, st) : embed_direct<kF32, kF32>(a, st);
+  }
   const BwdRegions r = bwd_regions(a.n, a.dim);
   uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(a.ws + r.keys[0]), reinterpret_cast<uint32_t*>(a.ws + r.keys[1])};
   uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(a.ws + r.pos[0]), reinterpret_cast<uint32_t*>(a.ws + r.pos[1])};
@@ -478,21 +659,35 @@ hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
   if (a.n > kRankTokens) {
     uint32_t* hist = reinterpret_cast<uint32_t*>(a.ws + r.hist);
     const uint32_t tile = sort_tile(a.n);
-    const uint32_t grid = grid_for((a.n + tile - 1) / tile, kSortThreads);
+    const uint64_t tiles = (a.n + tile - 1) / tile;
+    uint32_t launches = 0, launch = 0;
+    for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += kDigitBits) launches += 2;  // keys 0 to vocab
+    Fill f = whole_table(a);
+    const uint64_t rows = f.rows, share = (rows / launches + f.per) / f.per * f.per;
+    auto next = [&] {  // the launch's share of the table
+      f.first = share * launch < rows ? share * launch : rows;
+      ++launch;
+      f.rows = share * launch < rows ? share * launch : rows;
+      return sort_grid(tiles, f, kSortThreads);
+    };
     int from = -1;
-    for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += kDigitBits) {  // keys 0 to vocab
+    for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += kDigitBits) {
       const int to = from == 0 ? 1 : 0;
       const uint32_t* ki = from < 0 ? nullptr : keys[from];
       const uint32_t* pi = from < 0 ? nullptr : pos[from];
-      hipLaunchKernelGGL(embed_count_kernel, dim3(grid), dim3(kSortThreads), 0, st, a, ki, shift, tile, hist);
-      hipLaunchKernelGGL(embed_scatter_kernel, dim3(grid), dim3(kSortThreads), 0, st, a, ki, pi, shift, tile,
-                         static_cast<const uint32_t*>(hist), keys[to], pos[to]);
+      SortGrid g = next();
+      hipLaunchKernelGGL(embed_count_kernel, dim3(g.blocks), dim3(kSortThreads), 0, st, a, f, g.fill_from, ki, shift,
+                         tile, hist);
+      g = next();
+      hipLaunchKernelGGL(embed_scatter_kernel, dim3(g.blocks), dim3(kSortThreads), 0, st, a, f, g.fill_from, ki, pi,
+                         shift, tile, static_cast<const uint32_t*>(hist), keys[to], pos[to]);
       from = to;
     }
     sorted = from;
-  } else if (a.n > 0) {
-    const uint32_t grid = grid_for((a.n + kRankOwn - 1) / kRankOwn, kRankThreads);
-    hipLaunchKernelGGL(embed_rank_kernel, dim3(grid), dim3(kRankThreads), 0, st, a, keys[0], pos[0]);
+  } else {
+    const Fill f = whole_table(a);
+    const SortGrid g = sort_grid((a.n + kRankOwn - 1) / kRankOwn, f, kRankThreads);
+    hipLaunchKernelGGL(embed_rank_kernel, dim3(g.blocks), dim3(kRankThreads), 0, st, a, f, g.fill_from, keys[0], pos[0]);
   }
   SumArgs s;
   s.dout = a.dout;

@@ -66,18 +66,19 @@ def test_embedding():
     refused(embed_fwd, out=mat(A[2], cols=9), says="out")
     refused(embed_fwd, out=mat(A[0] + 16), says="overlap")
     refused(embed_fwd, out=mat(A[1]), says="overlap")
-    refused(embed_bwd, ws=0, says="workspace is NULL")
-    refused(embed_bwd, ws=A[3] + 8, says="aligned")
-    refused(embed_bwd, size=100, code=LC.LC_ERR_CAPACITY, says="workspace")
+    many = dict(n=5000, dout=mat(A[2], rows=5000))  # sorted in the workspace
+    refused(embed_bwd, ws=0, says="workspace is NULL", **many)
+    refused(embed_bwd, ws=A[3] + 8, says="aligned", **many)
+    refused(embed_bwd, size=100, code=LC.LC_ERR_CAPACITY, says="workspace", **many)
+    refused(embed_bwd, ws=A[2], says="overlap", **many)
     refused(embed_bwd, dout=mat(A[2], cols=9), says="dout")
-    refused(embed_bwd, ws=A[2], says="overlap")
     refused(embed_bwd, dweight=mat(A[2], rows=10), says="overlap")
     lib = LC.load_library()
     assert lib.lc_embedding_backward(mat(A[2]), A[1], 2, 4, 0, 1.0, 2, mat(rows=10), A[3], 1 << 20, None) == LC.LC_ERR_INVALID_ARG
     assert lib.lc_embedding_forward(None, A[1], 2, 4, 0, 1.0, mat(), None) == LC.LC_ERR_INVALID_ARG
     assert LC.lc_embedding_backward_workspace(1 << 40, 8) == 0
     assert LC.lc_embedding_backward_workspace(0, 8) == 0
-    assert LC.lc_embedding_backward_workspace(1, 8) >= 8
+    assert LC.lc_embedding_backward_workspace(5000, 8) >= 5000 * 8
 
 
 def norm(kind=LC.LC_NORM_LAYER, weight=A[4], bias=A[5], dtype=F, eps=1e-5):
