@@ -588,24 +588,19 @@ hipError_t embed_fwd_of(const EmbedFwd& a, hipStream_t st) {
   while ((1u << lg) < groups && (1u << lg) < kEmbedThreads) ++lg;
   const uint64_t per_block = kEmbedThreads >> lg;
   const uint32_t grid = grid_for((a.n + per_block - 1) / per_block, kEmbedThreads);
-  if (a.out_dtype == kBf16)
-    hipLaunchKernelGGL((embed_fwd_kernel<WDT, kBf16>), dim3(grid), dim3(kEmbedThreads), 0, st, a, lg);
-  else
-    hipLaunchKernelGGL((embed_fwd_kernel<WDT, kF32>), dim3(grid), dim3(kEmbedThreads), 0, st, a, lg);
-  return hipGetLastError();
+  return launch_op(a.out_dtype == kBf16 ? embed_fwd_kernel<WDT, kBf16> : embed_fwd_kernel<WDT, kF32>, grid,
+                   kEmbedThreads, st, a, lg);
 }
 
 template <int DDT, int GDT>
 hipError_t embed_sums(const SumArgs& s, hipStream_t st) {
   const uint64_t items = static_cast<uint64_t>(s.tiles) * s.chunks;
-  hipLaunchKernelGGL((embed_sum_kernel<DDT, GDT>),
-                     dim3(grid_for((items + kSumThreads / 64 - 1) / (kSumThreads / 64), kSumThreads)), dim3(kSumThreads), 0,
-                     st, s);
-  if (s.tiles > 1)
-    hipLaunchKernelGGL((embed_join_kernel<GDT>),
-                       dim3(grid_for(static_cast<uint64_t>(s.tiles - 1) * s.chunks, kSumThreads)), dim3(kSumThreads), 0,
-                       st, s);
-  return hipGetLastError();
+  const hipError_t e =
+      launch_op(embed_sum_kernel<DDT, GDT>, grid_for((items + kSumThreads / 64 - 1) / (kSumThreads / 64), kSumThreads),
+                kSumThreads, st, s);
+  if (e != hipSuccess || s.tiles <= 1) return e;
+  return launch_op(embed_join_kernel<GDT>, grid_for(static_cast<uint64_t>(s.tiles - 1) * s.chunks, kSumThreads),
+                   kSumThreads, st, s);
 }
 
 Fill whole_table(const EmbedBwd& a) {
@@ -632,10 +627,9 @@ SortGrid sort_grid(uint64_t work, const Fill& f, uint32_t threads) {
 template <int DDT, int GDT>
 hipError_t embed_direct(const EmbedBwd& a, hipStream_t st) {
   const Fill f = whole_table(a);
-  if (a.n + fill_blocks(f) > 0)
-    hipLaunchKernelGGL((embed_direct_kernel<DDT, GDT>), dim3(grid_for(a.n + fill_blocks(f), kSumThreads)),
-                       dim3(kSumThreads), 0, st, a, f, fill_blocks(f));
-  return hipGetLastError();
+  if (a.n + fill_blocks(f) == 0) return hipSuccess;
+  return launch_op(embed_direct_kernel<DDT, GDT>, grid_for(a.n + fill_blocks(f), kSumThreads), kSumThreads, st, a, f,
+                   fill_blocks(f));
 }
 
 }  // namespace
@@ -676,18 +670,20 @@ hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
       const uint32_t* ki = from < 0 ? nullptr : keys[from];
       const uint32_t* pi = from < 0 ? nullptr : pos[from];
       SortGrid g = next();
-      hipLaunchKernelGGL(embed_count_kernel, dim3(g.blocks), dim3(kSortThreads), 0, st, a, f, g.fill_from, ki, shift,
-                         tile, hist);
+      hipError_t e = launch_op(embed_count_kernel, g.blocks, kSortThreads, st, a, f, g.fill_from, ki, shift, tile, hist);
+      if (e != hipSuccess) return e;
       g = next();
-      hipLaunchKernelGGL(embed_scatter_kernel, dim3(g.blocks), dim3(kSortThreads), 0, st, a, f, g.fill_from, ki, pi,
-                         shift, tile, static_cast<const uint32_t*>(hist), keys[to], pos[to]);
+      e = launch_op(embed_scatter_kernel, g.blocks, kSortThreads, st, a, f, g.fill_from, ki, pi, shift, tile, hist, keys[to],
+                    pos[to]);
+      if (e != hipSuccess) return e;
       from = to;
     }
     sorted = from;
   } else {
     const Fill f = whole_table(a);
     const SortGrid g = sort_grid((a.n + kRankOwn - 1) / kRankOwn, f, kRankThreads);
-    hipLaunchKernelGGL(embed_rank_kernel, dim3(g.blocks), dim3(kRankThreads), 0, st, a, f, g.fill_from, keys[0], pos[0]);
+    const hipError_t e = launch_op(embed_rank_kernel, g.blocks, kRankThreads, st, a, f, g.fill_from, keys[0], pos[0]);
+    if (e != hipSuccess) return e;
   }
   SumArgs s;
   s.dout = a.dout;

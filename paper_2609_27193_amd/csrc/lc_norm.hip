@@ -447,41 +447,46 @@ NormParts norm_parts(uint64_t rows, uint64_t dim) {
   const uint32_t block_waves = tpr < 256 ? 4 : tpr / 64;
   const uint64_t most = 256 * (waves > block_waves ? waves / block_waves : 1);
   const uint64_t items = (rows + p.rpb - 1) / p.rpb;
-  uint64_t blocks = items < most ? items : most;
+  const uint64_t turns = (items + most - 1) / most;
+  // few turns are dealt out evenly: 1025 over 768 blocks as two each for 513
+  uint64_t blocks = turns > 3 ? most : turns ? (items + turns - 1) / turns : 0;
   if (LC_MAX_GRID_BLOCKS > 0 && blocks > LC_MAX_GRID_BLOCKS) blocks = LC_MAX_GRID_BLOCKS;
   p.parts = static_cast<uint32_t>(blocks);
   return p;
 }
 
 template <int DT, bool LAYER, int TPR, int NV>
-void norm_fwd_shape(const NormFwd& a, hipStream_t st) {
+hipError_t norm_fwd_shape(const NormFwd& a, hipStream_t st) {
   constexpr uint32_t threads = kNormThreads<TPR>, rpb = threads / TPR;
-  hipLaunchKernelGGL((norm_fwd_kernel<DT, LAYER, TPR, NV>), dim3(grid_for((a.rows + rpb - 1) / rpb, threads)),
-                     dim3(threads), 0, st, a);
+  return launch_op(norm_fwd_kernel<DT, LAYER, TPR, NV>, grid_for((a.rows + rpb - 1) / rpb, threads), threads, st, a);
 }
 
 template <int DT, bool LAYER>
 hipError_t norm_fwd_of(const NormFwd& a, hipStream_t st) {
   const uint32_t dim = a.dim;
-#define LC_NORM_SHAPE(TPR, NV) norm_fwd_shape<DT, LAYER, TPR, NV>(a, st)
   if (!norm_has_shape(dim))
-    hipLaunchKernelGGL((norm_fwd_long_kernel<DT, LAYER>), dim3(grid_for(a.rows, kLongThreads)), dim3(kLongThreads), 0,
-                       st, a);
-  else LC_NORM_SHAPES(LC_NORM_SHAPE);
+    return launch_op(norm_fwd_long_kernel<DT, LAYER>, grid_for(a.rows, kLongThreads), kLongThreads, st, a);
+#define LC_NORM_SHAPE(TPR, NV) return norm_fwd_shape<DT, LAYER, TPR, NV>(a, st)
+  LC_NORM_SHAPES(LC_NORM_SHAPE);
 #undef LC_NORM_SHAPE
-  return hipGetLastError();
 }
 
 template <int DT, bool LAYER, bool KEPT>
-void norm_bwd_of(const NormBwd& a, const NormParts& p, hipStream_t st) {
+hipError_t norm_bwd_of(const NormBwd& a, const NormParts& p, hipStream_t st) {
   const uint32_t dim = a.dim;
-#define LC_NORM_SHAPE(TPR, NV)                                                                                     \
-  hipLaunchKernelGGL((norm_bwd_kernel<DT, LAYER, KEPT, TPR, NV>), dim3(p.parts), dim3(kNormThreads<TPR>), 0, st, a, \
-                     p.parts)
   if (!norm_has_shape(dim))
-    hipLaunchKernelGGL((norm_bwd_long_kernel<DT, LAYER, KEPT>), dim3(p.parts), dim3(kLongThreads), 0, st, a, p.parts);
-  else LC_NORM_SHAPES(LC_NORM_SHAPE);
+    return launch_op(norm_bwd_long_kernel<DT, LAYER, KEPT>, p.parts, kLongThreads, st, a, p.parts);
+#define LC_NORM_SHAPE(TPR, NV) \
+  return launch_op(norm_bwd_kernel<DT, LAYER, KEPT, TPR, NV>, p.parts, kNormThreads<TPR>, st, a, p.parts)
+  LC_NORM_SHAPES(LC_NORM_SHAPE);
 #undef LC_NORM_SHAPE
+}
+
+template <int DT>
+hipError_t norm_bwd_kind(const NormBwd& a, const NormParts& p, hipStream_t st) {
+  const bool kept = a.kept.codes != 0;
+  if (a.layer) return kept ? norm_bwd_of<DT, true, true>(a, p, st) : norm_bwd_of<DT, true, false>(a, p, st);
+  return kept ? norm_bwd_of<DT, false, true>(a, p, st) : norm_bwd_of<DT, false, false>(a, p, st);
 }
 
 }  // namespace
@@ -497,19 +502,13 @@ uint64_t norm_bwd_workspace(uint64_t rows, uint64_t dim) { return norm_parts(row
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t st) {
   const NormParts p = norm_parts(a.rows, a.dim);
   if (a.rows > 0 && (a.part || a.dx.data)) {
-    const bool kept = a.kept.codes != 0;
-    if (a.dtype == kBf16) {
-      if (a.layer) kept ? norm_bwd_of<kBf16, true, true>(a, p, st) : norm_bwd_of<kBf16, true, false>(a, p, st);
-      else kept ? norm_bwd_of<kBf16, false, true>(a, p, st) : norm_bwd_of<kBf16, false, false>(a, p, st);
-    } else {
-      if (a.layer) kept ? norm_bwd_of<kF32, true, true>(a, p, st) : norm_bwd_of<kF32, true, false>(a, p, st);
-      else kept ? norm_bwd_of<kF32, false, true>(a, p, st) : norm_bwd_of<kF32, false, false>(a, p, st);
-    }
+    const hipError_t e = a.dtype == kBf16 ? norm_bwd_kind<kBf16>(a, p, st) : norm_bwd_kind<kF32>(a, p, st);
+    if (e != hipSuccess) return e;
   }
-  if (a.dweight || a.dbias)
-    hipLaunchKernelGGL(norm_join_kernel, dim3(grid_for((a.dim + kJoinCols - 1) / kJoinCols, kJoinCols * kJoinSlices), a.dbias ? 2 : 1),
-                       dim3(kJoinCols * kJoinSlices), 0, st, a, p.parts);
-  return hipGetLastError();
+  if (!a.dweight && !a.dbias) return hipSuccess;
+  return launch_op(norm_join_kernel,
+                   dim3(grid_for((a.dim + kJoinCols - 1) / kJoinCols, kJoinCols * kJoinSlices), a.dbias ? 2 : 1),
+                   kJoinCols * kJoinSlices, st, a, p.parts);
 }
 
 }  // namespace lc

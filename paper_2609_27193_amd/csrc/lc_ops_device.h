@@ -3,11 +3,23 @@
 // the 8-bit form of a kept activation.
 #pragma once
 
+#include <type_traits>
+
 #include "lc_device.h"
 #include "lc_ops.h"
 
 namespace lc {
 namespace {
+
+// A launch that reports its own error and leaves the program's alone.
+template <typename... P>
+__host__ hipError_t launch_op(void (*kernel)(P...), dim3 grid, uint32_t threads, hipStream_t st,
+                              std::common_type_t<P>... args) {
+  void* at[] = {&args...};
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, st);
+  if (e != hipSuccess) (void)hipGetLastError();  // reported here
+  return e;
+}
 
 constexpr int kBf16 = 1;
 constexpr int kF32 = 2;

@@ -29,7 +29,6 @@ constexpr uint32_t kStep = 32;      // tokens in LDS at a time
 constexpr uint32_t kThreads = 256;  // four waves of 64 x 64
 constexpr uint32_t kPitch = kTile + 16;  // elements from token to token in LDS
 constexpr uint32_t kOut = 64 + 4;        // floats from row to row on their way out
-static_assert(4 * 16 * kOut * 4 <= 2 * kStep * kPitch * 2, "the rows on their way out fit X's buffers");
 
 struct Codes16 {
   u32x4 codes;
@@ -57,6 +56,31 @@ __device__ __forceinline__ Codes16 load_codes16(const Kept& x, uint64_t row, uin
   return r;
 }
 
+// The same of a row of `cols` >= 16 codes: the last group is read from sixteen
+// before the end and moved down.
+__device__ __forceinline__ Codes16 load_codes16_row(const Kept& x, uint64_t row, uint32_t col, int n) {
+  Codes16 r;
+  r.codes = u32x4{0, 0, 0, 0};
+  r.code = 127;
+  if (n > 0) {
+    const uint32_t s = n < 16 ? 16 - n : 0;
+    r.codes = *(gc_u32x4_any1*)(x.codes + row * x.code_stride + col - s);
+    r.code = *(gc_u8*)(x.scales + row * x.scale_stride + col / kActBlock);
+    uint64_t lo = r.codes[0] | static_cast<uint64_t>(r.codes[1]) << 32, hi = r.codes[2] | static_cast<uint64_t>(r.codes[3]) << 32;
+    if (s & 8) {
+      lo = hi;
+      hi = 0;
+    }
+    const uint32_t bits = s % 8 * 8;
+    if (bits) {
+      lo = lo >> bits | hi << (64 - bits);
+      hi >>= bits;
+    }
+    r.codes = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+  }
+  return r;
+}
+
 // Four bytes to four bf16, times 2^(code - 127); exact, and code 255 gives NaN.
 __device__ __forceinline__ u32x2 decode4(uint32_t b, float scale) {
   const auto lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
@@ -64,19 +88,23 @@ __device__ __forceinline__ u32x2 decode4(uint32_t b, float scale) {
   return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
-// An fp32 value as three bf16 parts of 8 bits each, whose sum it is.
-__device__ __forceinline__ void split3(float v, uint32_t (&part)[3]) {
-  const uint32_t u = __float_as_uint(v);
-  if ((u & 0x7fffffffu) >= 0x7f800000u) {  // not finite: the first part says so alone
-    part[0] = (u & 0x007fffffu ? 0x7FC0u : u >> 16);
-    part[1] = part[2] = 0;
-    return;
+// Two fp32 values as three pairs of bf16 parts, of 8 bits each, whose sums they
+// are; of what is not finite the first part says so alone.
+__device__ __forceinline__ void split3(float a, float b, uint32_t (&part)[3]) {
+  float v[2] = {a, b};
+  uint32_t top[2];
+  part[0] = part[1] = part[2] = 0;
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      top[i] = __float_as_uint(v[i]);
+      if (p == 0) top[i] = v[i] != v[i] ? 0x7FC00000u : top[i];  // its low bits may be all that says NaN
+      const float rest = v[i] - __uint_as_float(top[i] & 0xffff0000u);
+      v[i] = p > 0 || fabsf(v[i]) < __builtin_inff() ? rest : 0.0f;
+    }
+    part[p] = top[0] >> 16 | (top[1] & 0xffff0000u);
   }
-  part[0] = u >> 16;
-  const float r1 = v - __uint_as_float(u & 0xffff0000u);
-  part[1] = __float_as_uint(r1) >> 16;
-  const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-  part[2] = __float_as_uint(r2) >> 16;
 }
 
 template <int DT>
@@ -98,7 +126,7 @@ struct WgradTiles {
   uint32_t tile;         // columns of n and of k
   uint32_t tn, tk;       // tiles of n and k
   uint32_t splits;
-  uint64_t full, tiles;  // tiles of the whole sum, and all
+  uint32_t full, tiles;  // tiles of the whole sum, and all: dW's 2^46 bytes hold fewer than 2^32
   uint64_t per_split;    // tokens a part, a multiple of kStep
   float* part;           // [tiles - full][splits][tile][tile]
   float* sums;           // [sum_parts][n] column sums of dY
@@ -107,35 +135,34 @@ struct WgradTiles {
 };
 
 struct WgradItem {
-  uint64_t tile;
-  uint32_t split, n0, k0;
+  uint32_t tile, split, n0, k0;
   bool whole;
   uint64_t t_begin, t_end;
 };
 // Eight tiles of n by all of k follow each other, so that blocks that run side
 // by side read the same columns.
-__device__ __forceinline__ void wgrad_place(const WgradTiles& s, uint64_t tile, uint32_t& n0, uint32_t& k0) {
-  const uint64_t per_group = 8ull * s.tk;
-  const uint32_t group = static_cast<uint32_t>(tile / per_group) * 8, in_g = static_cast<uint32_t>(tile % per_group);
-  const uint32_t wide = s.tn - group < 8 ? s.tn - group : 8;
-  n0 = (group + in_g % wide) * s.tile;
-  k0 = in_g / wide * s.tile;
+__device__ __forceinline__ void wgrad_place(const WgradTiles& s, uint32_t tile, uint32_t& n0, uint32_t& k0) {
+  const uint32_t group = tile / (8 * s.tk), in_g = tile - group * 8 * s.tk;
+  const uint32_t wide = s.tn - group * 8 < 8 ? s.tn - group * 8 : 8, k = in_g / wide;
+  n0 = (group * 8 + in_g - k * wide) * s.tile;
+  k0 = k * s.tile;
 }
 // Item b of the grid.  The whole tiles run first, then the parts; each in
 // contiguous eighths for the XCDs.
-__device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t rows, uint64_t b) {
+__device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t rows, uint32_t b) {
   WgradItem w;
   w.whole = b < s.full;
   if (w.whole) {
-    w.tile = s.full <= gridDim.x ? remap_xcd(static_cast<uint32_t>(b), static_cast<uint32_t>(s.full)) : b;
+    w.tile = s.full <= gridDim.x ? remap_xcd(b, s.full) : b;
     w.split = 0;
     w.t_begin = 0;
     w.t_end = rows;
   } else {
-    const uint64_t parts = (s.tiles - s.full) * s.splits;
-    const uint64_t i = s.full + parts <= gridDim.x ? remap_xcd(static_cast<uint32_t>(b - s.full), static_cast<uint32_t>(parts)) : b - s.full;
-    w.tile = s.full + i / s.splits;
-    w.split = static_cast<uint32_t>(i % s.splits);
+    const uint32_t parts = (s.tiles - s.full) * s.splits;
+    const uint32_t i = s.full + parts <= gridDim.x ? remap_xcd(b - s.full, parts) : b - s.full;
+    const uint32_t tile = i / s.splits;
+    w.tile = s.full + tile;
+    w.split = i - tile * s.splits;
     w.t_begin = w.split * s.per_split;
     w.t_end = w.t_begin + s.per_split < rows ? w.t_begin + s.per_split : rows;
   }
@@ -143,48 +170,78 @@ __device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t ro
   return w;
 }
 // Row n of a part's sums.
-__device__ __forceinline__ float* wgrad_part(const WgradTiles& s, uint64_t tile, uint32_t split, uint32_t n) {
-  return s.part + (((tile - s.full) * s.splits + split) * s.tile + n) * s.tile;
+__device__ __forceinline__ float* wgrad_part(const WgradTiles& s, uint32_t tile, uint32_t split, uint32_t n) {
+  return s.part + ((static_cast<uint64_t>(tile - s.full) * s.splits + split) * s.tile + n) * s.tile;
 }
 
-// Eight neighbours of k of row n of the whole sum, with everything that the
-// result has besides.
-__device__ __forceinline__ void wgrad_write8(const Wgrad& a, uint64_t n, uint32_t k, int in, float sum, float (&v)[8]) {
+// The whole sum at (n, k), and eight neighbours of k of it, with everything that
+// the result has besides.
+__device__ __forceinline__ void wgrad_write1(const Wgrad& a, uint64_t n, uint32_t k, float sum, float v) {
+  if (a.col_scale) v *= load_param(a.col_scale, k, a.param_dtype);
+  if (a.col_shift) v += sum * load_param(a.col_shift, k, a.param_dtype);
+  const uint64_t at = n * a.dw.stride + k;
+  if (a.accumulate) v += load_param(a.dw.data, at, a.dw_dtype);
+  store_param(a.dw.data, at, a.dw_dtype, v);
+}
+__device__ __forceinline__ void load8_of(uint64_t p, uint64_t i, int dtype, float (&f)[8]) {
+  if (dtype == kBf16) unpack8<kBf16>(load8_raw<kBf16>(p + 2 * i), f);
+  else unpack8<kF32>(load8_raw<kF32>(p + 4 * i), f);
+}
+__device__ __forceinline__ void wgrad_write8(const Wgrad& a, uint64_t n, uint32_t k, float sum, float (&v)[8]) {
   float w[8];
   if (a.col_scale) {
-    load_params8(a.col_scale, a.param_dtype, k / 8, in, 1.0f, w);
+    load8_of(a.col_scale, k, a.param_dtype, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= w[e];
   }
   if (a.col_shift) {
-    load_params8(a.col_shift, a.param_dtype, k / 8, in, 0.0f, w);
+    load8_of(a.col_shift, k, a.param_dtype, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += sum * w[e];
   }
   const uint64_t at = n * a.dw.stride + k;
   if (a.accumulate) {
-    if (a.dw_dtype == kBf16) unpack8<kBf16>(load8_raw<kBf16>(a.dw.data + 2 * at, in), w);
-    else unpack8<kF32>(load8_raw<kF32>(a.dw.data + 4 * at, in), w);
+    load8_of(a.dw.data, at, a.dw_dtype, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += w[e];
   }
-  if (a.dw_dtype == kBf16) store8<kBf16>(a.dw.data + 2 * at, v, in);
-  else store8<kF32>(a.dw.data + 4 * at, v, in);
+  if (a.dw_dtype == kBf16) store8<kBf16>(a.dw.data + 2 * at, v, 8);
+  else store8<kF32>(a.dw.data + 4 * at, v, 8);
+}
+// Row `ln` of the tile from column `lk` on, which lies at `src`: into the part
+// of a split tile, else into dW.
+__device__ __forceinline__ void wgrad_out8(const Wgrad& a, const WgradTiles& s, const WgradItem& w, uint32_t ln, uint32_t lk,
+                                           float sum, const float* src) {
+  const uint64_t n = w.n0 + ln;
+  const uint32_t k = w.k0 + lk;
+  if (!w.whole || (n < a.n && k + 8 <= a.k)) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = src[e];
+    if (!w.whole) store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + lk), v, 8);
+    else wgrad_write8(a, n, k, sum, v);
+  } else if (n < a.n) {
+#pragma unroll 1
+    for (uint32_t e = 0; k + e < a.k; ++e) wgrad_write1(a, n, k + e, sum, src[e]);
+  }
 }
 __device__ __forceinline__ void wgrad_write_bias(const Wgrad& a, uint64_t n, float sum) {
   if (a.accumulate) sum += load_param(a.dbias, n, a.dw_dtype);
   store_param(a.dbias, n, a.dw_dtype, sum);
 }
 
-template <int DT, bool SUMS>
-__global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) {
+// NARROW: fewer than 8 columns of n or 16 of k, read an element at a time.
+template <int DT, bool SUMS, bool NARROW>
+__global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles s) {
   constexpr int P = kPlanes<DT>;
-  __shared__ __align__(16) uint16_t dys[2][P][kStep * kPitch];
-  __shared__ __align__(16) uint16_t xs[2][kStep * kPitch];
+  constexpr uint32_t kIn = 2 * (P + 1) * kStep * kPitch * 2, kOutBytes = 4 * 64 * kOut * 4;
+  __shared__ __align__(16) uint8_t lds[kIn > kOutBytes ? kIn : kOutBytes];  // two steps; then the waves' 64 rows of 64
+  auto* const dys = reinterpret_cast<uint16_t(*)[P][kStep * kPitch]>(lds);
+  auto* const xs = reinterpret_cast<uint16_t(*)[kStep * kPitch]>(lds + 2 * P * kStep * kPitch * 2);
   __shared__ float colsum[SUMS ? kThreads / 16 : 1][kTile];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint64_t items = s.full + (s.tiles - s.full) * s.splits;
-  for (uint64_t b = blockIdx.x; b < items; b += gridDim.x) {
+  const uint32_t items = s.full + (s.tiles - s.full) * s.splits;
+  for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
     const WgradItem w = wgrad_item(s, a.rows, b);
     const uint32_t n0 = w.n0, k0 = w.k0;
     const uint64_t t_begin = w.t_begin, t_end = w.t_end;
@@ -193,49 +250,55 @@ __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) 
     const int d_in = static_cast<int>(a.n) - static_cast<int>(n0 + 8 * dc);
     const uint32_t xc = tid % 8, xr = tid / 8;
     const int x_in = static_cast<int>(a.k) - static_cast<int>(k0 + 16 * xc);
-    Raw8<DT> d[2];
-    Codes16 c;
+    struct Stage {
+      Raw8<DT> d[2];
+      Codes16 c;
+    };
     float sum[8] = {};
-    auto load = [&](uint64_t t) {
+    auto load = [&](Stage& g, uint64_t t) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint64_t r = t + dr + 16 * i;
-        d[i] = load8_raw<DT>(a.dy.data + (r * a.dy.stride + n0 + 8 * dc) * kEsz<DT>, r < t_end ? d_in : 0);
+        const uint64_t dy = a.dy.data + r * a.dy.stride * kEsz<DT>;
+        const int in = r < t_end ? d_in : 0;
+        if constexpr (NARROW) g.d[i] = load8_raw<DT>(dy + (n0 + 8ull * dc) * kEsz<DT>, in);
+        else g.d[i] = load8_row<DT>(dy, n0 / 8 + dc, a.n, in);
       }
       const uint64_t r = t + xr;
-      c = load_codes16(a.x, r, k0 + 16 * xc, r < t_end ? x_in : 0);
+      const int in = r < t_end ? x_in : 0;
+      if constexpr (NARROW) g.c = load_codes16(a.x, r, k0 + 16 * xc, in);
+      else g.c = load_codes16_row(a.x, r, k0 + 16 * xc, in);
     };
-    auto store = [&](int buf) {
+    auto store = [&](const Stage& g, int buf) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t at = (dr + 16 * i) * kPitch + 8 * dc;
         if constexpr (SUMS) {
           float f[8];
-          unpack8<DT>(d[i], f);
+          unpack8<DT>(g.d[i], f);
 #pragma unroll
           for (int e = 0; e < 8; ++e) sum[e] += f[e];
         }
         if constexpr (P == 1) {
-          *reinterpret_cast<u32x4*>(&dys[buf][0][at]) = d[i].v[0];
+          *reinterpret_cast<u32x4*>(&dys[buf][0][at]) = g.d[i].v[0];
         } else {
           float f[8];
-          unpack8<DT>(d[i], f);
+          unpack8<DT>(g.d[i], f);
           u32x4 q[3];
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
-            uint32_t lo[3], hi[3];
-            split3(f[e], lo);
-            split3(f[e + 1], hi);
+            uint32_t part[3];
+            split3(f[e], f[e + 1], part);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) q[p][e / 2] = lo[p] | hi[p] << 16;
+            for (int p = 0; p < 3; ++p) q[p][e / 2] = part[p];
           }
 #pragma unroll
           for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(&dys[buf][p][at]) = q[p];
         }
       }
-      const float scale = __uint_as_float(c.code << 23);
-      const u32x2 q0 = decode4(c.codes[0], scale), q1 = decode4(c.codes[1], scale);
-      const u32x2 q2 = decode4(c.codes[2], scale), q3 = decode4(c.codes[3], scale);
+      const float scale = __uint_as_float(g.c.code << 23);
+      const u32x2 q0 = decode4(g.c.codes[0], scale), q1 = decode4(g.c.codes[1], scale);
+      const u32x2 q2 = decode4(g.c.codes[2], scale), q3 = decode4(g.c.codes[3], scale);
       u32x4* p = reinterpret_cast<u32x4*>(&xs[buf][xr * kPitch + 16 * xc]);
       p[0] = u32x4{q0[0], q0[1], q1[0], q1[1]};
       p[1] = u32x4{q2[0], q2[1], q3[0], q3[1]};
@@ -247,15 +310,18 @@ __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) 
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
     const uint32_t wk = wave % 2 * 64, wn = wave / 2 * 64;
+    // the next step is on its way while one multiplies (two ahead: registers,
+    // and half the waves; 8192 x 4096 x 4096 fp32 990 us, 1078 with two)
+    Stage g;
     if (t_begin < t_end) {
-      load(t_begin);
-      store(0);
+      load(g, t_begin);
+      store(g, 0);
     }
     __syncthreads();
     int buf = 0;
     for (uint64_t t = t_begin; t < t_end; t += kStep) {
       const bool more = t + kStep < t_end;
-      if (more) load(t + kStep);
+      if (more) load(g, t + kStep);
       bf16x8 xf[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) xf[i] = read_cols(xs[buf], wk + 16 * i, lane);
@@ -268,7 +334,7 @@ __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) 
           for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], df, acc[i][j], 0, 0, 0);
         }
       }
-      if (more) store(buf ^ 1);
+      if (more) store(g, buf ^ 1);
       __syncthreads();
       buf ^= 1;
     }
@@ -290,28 +356,17 @@ __global__ __launch_bounds__(kThreads) void wgrad_kernel(Wgrad a, WgradTiles s) 
       }
       __syncthreads();
     }
-    // out through LDS, 16 rows of dW a wave at a time, so that a lane has eight
-    // neighbours of k; the operands' last reads lie before the loop's barrier
-    float* const mine = reinterpret_cast<float*>(&xs[0][0]) + wave * 16 * kOut;
+    // out through LDS, so that a lane has eight neighbours of k; the operands'
+    // last reads lie before the loop's barrier
+    float* const mine = reinterpret_cast<float*>(lds) + wave * 64 * kOut;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(mine + lane % 16 * kOut + 16 * i + lane / 16 * 4) = acc[i][j];
-      const uint32_t lk = wk + lane % 8 * 8;
-      const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
+        *reinterpret_cast<f32x4*>(mine + (16 * j + lane % 16) * kOut + 16 * i + lane / 16 * 4) = acc[i][j];
 #pragma unroll 1
-      for (uint32_t q = lane / 8; q < 16; q += 8) {
-        const uint32_t ln = wn + 16 * j + q;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + lane % 8 * 8 + e];
-        if (!w.whole)
-          store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + lk), v, 8);
-        else if (n0 + ln < a.n && in > 0)
-          wgrad_write8(a, n0 + ln, k0 + lk, in, SUMS ? colsum[0][ln] : 0.0f, v);
-      }
-    }
+    for (uint32_t q = lane / 8; q < 64; q += 8)
+      wgrad_out8(a, s, w, wn + q, wk + lane % 8 * 8, SUMS ? colsum[0][wn + q] : 0.0f, mine + q * kOut + lane % 8 * 8);
     __syncthreads();
   }
 }
@@ -380,8 +435,8 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
     x_at[i] = base + 2 * kBigBuf + at + wk * 2;
     dy_at[i] = base + at + wn * 2;
   }
-  const uint64_t items = s.full + (s.tiles - s.full) * s.splits;
-  for (uint64_t b = blockIdx.x; b < items; b += gridDim.x) {
+  const uint32_t items = s.full + (s.tiles - s.full) * s.splits;
+  for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
     const WgradItem w = wgrad_item(s, a.rows, b);
     const uint32_t n0 = w.n0, k0 = w.k0;
     const uint64_t t_begin = w.t_begin, t_end = w.t_end;
@@ -507,18 +562,11 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
           const f32x4 v = {acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
           *reinterpret_cast<f32x4*>(mine + lane % 32 * kBigOut + 32 * i + 8 * r + lane / 32 * 4) = v;
         }
-      const uint32_t lk = lane % 16 * 16 + wk / 16;
-      const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
 #pragma unroll 1
       for (uint32_t q = lane / 16; q < 32; q += 4) {
         const uint32_t ln = wn + 32 * j + q;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = mine[q * kBigOut + lane % 16 * 8 + e];
-        if (!w.whole)
-          store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + lk), v, 8);
-        else if (n0 + ln < a.n && in > 0)
-          wgrad_write8(a, n0 + ln, k0 + lk, in, a.col_shift ? s.sums[n0 + ln] : 0.0f, v);
+        const float sum = a.col_shift && n0 + ln < a.n ? s.sums[n0 + ln] : 0.0f;
+        wgrad_out8(a, s, w, ln, lane % 16 * 16 + wk / 16, sum, mine + q * kBigOut + lane % 16 * 8);
       }
     }
     __syncthreads();
@@ -527,29 +575,35 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
 
 // The parts' sums, in order, with the columns' scale and shift.
 __global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTiles s) {
-  const uint32_t per_row = s.tile / 8, per_tile = s.tile * per_row;
-  const uint64_t items = (s.tiles - s.full) * per_tile;
-  for (uint64_t it = blockIdx.x * static_cast<uint64_t>(kThreads) + threadIdx.x; it < items;
-       it += gridDim.x * static_cast<uint64_t>(kThreads)) {
-    const uint64_t tile = s.full + it / per_tile;
-    const uint32_t ln = static_cast<uint32_t>(it % per_tile) / per_row, lk = static_cast<uint32_t>(it % per_row) * 8;
+  const uint32_t per_row = s.tile / 8, blocks = s.tile * per_row / kThreads;  // of a tile
+  for (uint32_t it = blockIdx.x; it < (s.tiles - s.full) * blocks; it += gridDim.x) {
+    const uint32_t tile = s.full + it / blocks, in_t = it % blocks * kThreads + threadIdx.x;
+    const uint32_t ln = in_t / per_row, lk = in_t % per_row * 8;
     uint32_t n0, k0;
     wgrad_place(s, tile, n0, k0);
     const uint64_t n = n0 + ln;
     const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
     if (n >= a.n || in <= 0) continue;
     float v[8] = {}, f[8], sum = 0;
-#pragma unroll 4
-    for (uint32_t p = 0; p < s.splits; ++p) {
+#pragma unroll 8
+    for (uint32_t p = 0; p < s.splits; ++p) {  // a part is a whole tile, also where dW ends
       unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, tile, p, ln) + lk)), f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += f[e];
     }
     const bool bias = a.dbias && !s.big && k0 + lk == 0;
-    if (a.col_shift || bias)
+    if (a.col_shift || bias) {
+#pragma unroll 8
       for (uint32_t p = 0; p < s.sum_parts; ++p) sum += s.sums[p * static_cast<uint64_t>(a.n) + n];
+    }
     if (bias) wgrad_write_bias(a, n, sum);
-    wgrad_write8(a, n, k0 + lk, in, sum, v);
+    if (in >= 8) {
+      wgrad_write8(a, n, k0 + lk, sum, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < in) wgrad_write1(a, n, k0 + lk + e, sum, v[e]);
+    }
   }
 }
 
@@ -604,7 +658,7 @@ WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big) {
   s.tile = big ? kBigTile : kTile;
   s.tn = static_cast<uint32_t>((n + s.tile - 1) / s.tile);
   s.tk = static_cast<uint32_t>((k + s.tile - 1) / s.tile);
-  s.tiles = static_cast<uint64_t>(s.tn) * s.tk;
+  s.tiles = s.tn * s.tk;
   const uint64_t at_once = big ? 256 : 512, rest = s.tiles % at_once, steps = (rows + kStep - 1) / kStep;
   const double step_us = big ? 0.88 : 1.0, part_us = big ? 0.105 : 0.026;
   uint64_t best = 1;
@@ -618,7 +672,7 @@ WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big) {
   }
   s.per_split = (steps + best - 1) / best * kStep;
   s.splits = steps ? static_cast<uint32_t>((rows + s.per_split - 1) / s.per_split) : 1;
-  s.full = s.splits > 1 ? s.tiles - rest : s.tiles;
+  s.full = s.splits > 1 ? s.tiles - static_cast<uint32_t>(rest) : s.tiles;
   s.sum_parts = big ? 1 : s.splits;
   return s;
 }
@@ -644,15 +698,17 @@ WgradTiles wgrad_cut(uint64_t rows, uint64_t n, uint64_t k, bool big) {
   return s;
 }
 
-uint64_t wgrad_part_bytes(const WgradTiles& s) { return (s.tiles - s.full) * s.splits * s.tile * s.tile * 4; }
+uint64_t wgrad_part_bytes(const WgradTiles& s) {
+  return static_cast<uint64_t>(s.tiles - s.full) * s.splits * s.tile * s.tile * 4;
+}
+template <int DT>
+hipError_t wgrad_of(const Wgrad& a, const WgradTiles& s, uint32_t grid, bool sums, hipStream_t st) {
+  if (a.n < 8 || a.k < 16)
+    return launch_op(sums ? wgrad_kernel<DT, true, true> : wgrad_kernel<DT, false, true>, grid, kThreads, st, a, s);
+  return launch_op(sums ? wgrad_kernel<DT, true, false> : wgrad_kernel<DT, false, false>, grid, kThreads, st, a, s);
+}
 uint64_t wgrad_space(const WgradTiles& s, uint64_t n) {
   return wgrad_part_bytes(s) + (s.sum_parts + (s.big ? kSumParts : 0)) * n * 4;
-}
-
-template <int DT>
-void wgrad_of(const Wgrad& a, const WgradTiles& s, uint32_t grid, bool sums, hipStream_t st) {
-  if (sums) hipLaunchKernelGGL((wgrad_kernel<DT, true>), dim3(grid), dim3(kThreads), 0, st, a, s);
-  else hipLaunchKernelGGL((wgrad_kernel<DT, false>), dim3(grid), dim3(kThreads), 0, st, a, s);
 }
 
 }  // namespace
@@ -670,26 +726,22 @@ hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
   s.sums = reinterpret_cast<float*>(a.ws + wgrad_part_bytes(s));
   const bool sums = a.dbias || a.col_shift;
   const uint32_t grid = grid_for(s.full + (s.tiles - s.full) * s.splits, kThreads);
+  hipError_t e;
   if (s.big) {
     if (sums) {
       float* const parts = s.sums + a.n;
-      hipLaunchKernelGGL(wgrad_sums_kernel, dim3(grid_for((a.n + kSumCols - 1) / kSumCols * kSumParts, kThreads)),
-                         dim3(kThreads), 0, st, a, parts);
-      hipLaunchKernelGGL(wgrad_sums_join_kernel, dim3(grid_for((a.n + 63) / 64, 64)), dim3(64), 0, st, a,
-                         static_cast<const float*>(parts), s.sums);
+      e = launch_op(wgrad_sums_kernel, grid_for((a.n + kSumCols - 1) / kSumCols * kSumParts, kThreads), kThreads, st, a, parts);
+      if (e != hipSuccess) return e;
+      e = launch_op(wgrad_sums_join_kernel, grid_for((a.n + 63) / 64, 64), 64, st, a, parts, s.sums);
+      if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(wgrad_big_kernel, dim3(grid), dim3(kThreads), 0, st, a, s);
-  } else if (a.dtype == kBf16) {
-    wgrad_of<kBf16>(a, s, grid, sums, st);
+    e = launch_op(wgrad_big_kernel, grid, kThreads, st, a, s);
   } else {
-    wgrad_of<kF32>(a, s, grid, sums, st);
+    e = a.dtype == kBf16 ? wgrad_of<kBf16>(a, s, grid, sums, st) : wgrad_of<kF32>(a, s, grid, sums, st);
   }
-  if (s.splits > 1) {
-    const uint64_t items = (s.tiles - s.full) * s.tile * s.tile / 8;
-    hipLaunchKernelGGL(wgrad_join_kernel, dim3(grid_for((items + kThreads - 1) / kThreads, kThreads)), dim3(kThreads), 0,
-                       st, a, s);
-  }
-  return hipGetLastError();
+  if (e != hipSuccess || s.splits == 1) return e;
+  return launch_op(wgrad_join_kernel, grid_for((s.tiles - s.full) * (s.tile * s.tile / 8 / kThreads), kThreads), kThreads,
+                   st, a, s);
 }
 
 }  // namespace lc
