@@ -26,7 +26,7 @@ __global__ __launch_bounds__(kActThreads) void act_save_kernel(ActCopy a, uint32
 #pragma unroll
       for (int i = 0; i < kActVecs; ++i) {
         const uint32_t g = g0 + i * lanes;
-        r[i] = load8_raw<DT>(a.x.data + (row * a.x.stride + 8ull * g) * kEsz<DT>, g < groups ? in_group(a.dim, g) : 0);
+        r[i] = load8_raw<DT, true>(a.x.data + (row * a.x.stride + 8ull * g) * kEsz<DT>, g < groups ? in_group(a.dim, g) : 0);
       }
 #pragma unroll
       for (int i = 0; i < kActVecs; ++i) {
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kActThreads) void act_load_kernel(ActCopy a, uint32
         if (g >= groups) break;
         float f[8];
         act_decode8(b[i], act_scale(code[i]), f);
-        store8<DT>(a.x.data + (row * a.x.stride + 8ull * g) * kEsz<DT>, f, in_group(a.dim, g));
+        store8<DT, kStreams<DT>>(a.x.data + (row * a.x.stride + 8ull * g) * kEsz<DT>, f, in_group(a.dim, g));
       }
     }
   }

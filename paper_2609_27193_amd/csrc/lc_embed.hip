@@ -24,7 +24,10 @@ __device__ __forceinline__ uint32_t token_row(uint64_t tokens, int token64, uint
 constexpr uint32_t kEmbedThreads = 256;
 constexpr int kEmbedVecs = 4;  // groups of eight that a thread has in flight
 
-// `lanes` threads (a power of two) take one token's row, 8 elements each at a time.
+// `lanes` threads (a power of two) take one token's row, 8 elements each at a
+// time.  Bound by memory, 16384 rows of 4096 out of 128256 in bf16: 33 us, 8 TB/s
+// with the rows that come again out of the caches; the output goes past them
+// (through them 38.6 us).
 template <int WDT, int ODT>
 __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, uint32_t lanes_log2) {
   const uint32_t lanes = 1u << lanes_log2, per_block = kEmbedThreads >> lanes_log2;
@@ -53,7 +56,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, ui
         unpack8<WDT>(r[i], f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = held ? f[e] * a.scale : 0.0f;
-        store8<ODT>(dst + 8ull * kEsz<ODT> * g, f, in_group(a.dim, g));
+        store8<ODT, kStreams<ODT>>(dst + 8ull * kEsz<ODT> * g, f, in_group(a.dim, g));
       }
     }
   }

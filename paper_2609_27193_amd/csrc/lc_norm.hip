@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_fwd_kernel(NormFwd a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const uint32_t g = i * TPR + t;
-      r[i] = load8_row<DT>(a.x.data + row * a.x.stride * kEsz<DT>, g, a.dim, on ? in_group(a.dim, g) : 0);
+      r[i] = load8_row<DT, kStreams<DT>>(a.x.data + row * a.x.stride * kEsz<DT>, g, a.dim, on ? in_group(a.dim, g) : 0);
     }
     float v[8];
     float mean = 0;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_fwd_kernel(NormFwd a) 
         y[e] = v[e] * w[e];
         if constexpr (LAYER) y[e] += b[e];
       }
-      store8<DT>(a.y.data + (row * a.y.stride + 8ull * g) * kEsz<DT>, y, n);
+      store8<DT, kStreams<DT>>(a.y.data + (row * a.y.stride + 8ull * g) * kEsz<DT>, y, n);
       if (a.kept.codes) {
         if (n < 8) {  // what is no element must not set its block's power: a NaN row has one here, too
 #pragma unroll
@@ -204,13 +204,13 @@ template <int DT, bool KEPT, bool ANY>
 __device__ __forceinline__ NormIn<DT, KEPT> load_normed(const NormBwd& a, uint64_t row, uint32_t g, int n) {
   NormIn<DT, KEPT> in;
   const uint64_t dy = a.dy.data + row * a.dy.stride * kEsz<DT>;
-  in.dy = ANY ? load8_raw<DT>(dy + 8ull * g * kEsz<DT>, n) : load8_row<DT>(dy, g, a.dim, n);
+  in.dy = ANY ? load8_raw<DT>(dy + 8ull * g * kEsz<DT>, n) : load8_row<DT, kStreams<DT>>(dy, g, a.dim, n);
   if constexpr (KEPT) {
     in.code = n > 0 ? load_kept_code(a.kept, row, g) : 0;
     in.codes = ANY ? load_kept8(a.kept, row, g, n) : load_codes8_row(a.kept.codes + row * a.kept.code_stride, g, n);
   } else {
     const uint64_t x = a.x.data + row * a.x.stride * kEsz<DT>;
-    in.x = ANY ? load8_raw<DT>(x + 8ull * g * kEsz<DT>, n) : load8_row<DT>(x, g, a.dim, n);
+    in.x = ANY ? load8_raw<DT>(x + 8ull * g * kEsz<DT>, n) : load8_row<DT, kStreams<DT>>(x, g, a.dim, n);
   }
   return in;
 }

@@ -371,7 +371,7 @@ extern "C" lc_status lc_act_load(const lc_saved_act* saved, const lc_matrix* out
 }
 
 extern "C" uint64_t lc_linear_wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k) {
-  if (rows > kMaxRows || n == 0 || k == 0 || n > kMaxCols || k > kMaxCols) return 0;
+  if (rows > kMaxRows || n == 0 || k == 0 || n > kMaxCols || k > kMaxCols || n > kMaxSpan / 4 / k) return 0;
   return wgrad_workspace(rows, n, k);
 }
 
@@ -384,6 +384,7 @@ extern "C" lc_status lc_linear_wgrad(const lc_matrix* dy, const lc_saved_act* sa
   LC_CHECK(check_matrix("dweight", dweight));
   if (saved->rows != dy->rows) LC_CHECK(check_shape("saved", saved->rows, saved->cols, dy->rows, saved->cols));
   LC_CHECK(check_shape("dweight", dweight->rows, dweight->cols, dy->cols, saved->cols));
+  if (dweight->rows > kMaxSpan / 4 / dweight->cols) return fail(LC_ERR_INVALID_ARG, "dweight is too large");
   LC_CHECK(check_flag("accumulate", accumulate));
   if ((col_scale || col_shift) && !dtype_ok(param_dtype))
     return fail(LC_ERR_INVALID_ARG, "unknown param dtype %d", param_dtype);

@@ -408,8 +408,8 @@ struct BigStage {
 // reads zeros; past another's end it reads the row behind it, whose columns
 // are not stored.
 __device__ __forceinline__ tile_t step_tile(uint64_t base, int rows, uint32_t pitch, uint32_t width) {
-  const int bytes = (rows - 1) * static_cast<int>(pitch) + static_cast<int>(width);
-  return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0);
+  const uint32_t bytes = static_cast<uint32_t>(rows - 1) * pitch + width;
+  return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0u);
 }
 
 __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTiles s) {

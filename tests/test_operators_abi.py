@@ -163,6 +163,7 @@ def test_saved_activations_and_wgrad():
     refused(wgrad, size=64, code=LC.LC_ERR_CAPACITY, **big)
     refused(wgrad, ws=A[0], size=1 << 30, says="overlap", **big)
     assert LC.lc_linear_wgrad_workspace(1, 0, 5) == 0 and LC.lc_linear_wgrad_workspace(1, 5, 1 << 31) == 0
+    assert LC.lc_linear_wgrad_workspace(1, 1 << 30, 1 << 30) == 0
 
 
 def test_columns_beside_each_other_are_apart():
