@@ -19,7 +19,7 @@ __global__ __launch_bounds__(kActThreads) void act_save_kernel(ActCopy a, uint32
   const uint32_t groups = (a.dim + 31) / 32 * 4, lane = threadIdx.x & (lanes - 1);
   const uint64_t items = (a.rows + per_block - 1) / per_block;
   for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const uint64_t row = it * per_block + (threadIdx.x >> lanes_log2);
+    const uint64_t row = row_item(it, items) * per_block + (threadIdx.x >> lanes_log2);
     if (row >= a.rows) continue;
     for (uint32_t g0 = lane; g0 < groups; g0 += lanes * kActVecs) {
       Raw8<DT> r[kActVecs];
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kActThreads) void act_load_kernel(ActCopy a, uint32
   const uint32_t groups = (a.dim + 7) / 8, lane = threadIdx.x & (lanes - 1);
   const uint64_t items = (a.rows + per_block - 1) / per_block;
   for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const uint64_t row = it * per_block + (threadIdx.x >> lanes_log2);
+    const uint64_t row = row_item(it, items) * per_block + (threadIdx.x >> lanes_log2);
     if (row >= a.rows) continue;
     for (uint32_t g0 = lane; g0 < groups; g0 += lanes * kActVecs) {
       u32x2 b[kActVecs];

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_fwd_kernel(NormFwd a) 
   const float inv_dim = 1.0f / static_cast<float>(a.dim);
   const uint64_t items = (a.rows + RPB - 1) / RPB;
   for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const uint64_t row = it * RPB + threadIdx.x / TPR;
+    const uint64_t row = row_item(it, items) * RPB + threadIdx.x / TPR;
     const bool on = row < a.rows;  // the others only take part in the barriers
     Raw8<DT> r[NV];
     float sum = 0, unused = 0;
@@ -233,13 +233,11 @@ __device__ __forceinline__ void normed8(const NormIn<DT, KEPT>& in, int n, float
 }
 
 // A block keeps its columns' weights and sums in registers and takes its turn
-// at the rows; up to 256 threads a row the next row's loads are under way while
-// one is summed and written (beyond that the registers for them cost more:
-// 16384 columns 102.8 us with them, 72.9 without).
+// at the rows.  (The next row's loads under way meanwhile, for fewer blocks a
+// CU: no faster up to 4096 columns, 16384 columns 102.8 us for 72.9.)
 template <int DT, bool LAYER, bool KEPT, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads<TPR>) void norm_bwd_kernel(NormBwd a, uint32_t parts) {
   constexpr uint32_t RPB = kNormThreads<TPR> / TPR;
-  constexpr bool AHEAD = TPR <= 256;
   __shared__ float2 red[2][kNormThreads<TPR> / 64];
   uint32_t turn = 0;
   const uint32_t t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -251,28 +249,16 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_bwd_kernel(NormBwd a, 
     load_params8(a.weight, a.param_dtype, g, in_group(a.dim, g), 1.0f, w[i]);
   }
   const uint64_t items = (a.rows + RPB - 1) / RPB;
-  NormIn<DT, KEPT> in[NV];
-  float rstd = 0, mean = 0;
-  auto load = [&](uint64_t row) {
-    const bool on = row < a.rows;
-    rstd = on ? a.rstd[row] : 0.0f;
-    if constexpr (LAYER && !KEPT) mean = on ? a.mean[row] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const uint32_t g = i * TPR + t;
-      in[i] = load_normed<DT, KEPT, false>(a, row, g, on ? in_group(a.dim, g) : 0);
-    }
-  };
-  if (AHEAD) load(blockIdx.x * static_cast<uint64_t>(RPB) + sub);
   for (uint64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const uint64_t row = it * RPB + sub;
     const bool on = row < a.rows;
-    if (!AHEAD) load(row);
+    const float rs = on ? a.rstd[row] : 0.0f, mu = on && LAYER && !KEPT ? a.mean[row] : 0.0f;
     NormIn<DT, KEPT> cur[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) cur[i] = in[i];
-    const float rs = rstd, mu = mean;
-    if (AHEAD && it + gridDim.x < items) load(row + static_cast<uint64_t>(gridDim.x) * RPB);
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t g = i * TPR + t;
+      cur[i] = load_normed<DT, KEPT, false>(a, row, g, on ? in_group(a.dim, g) : 0);
+    }
     float c1 = 0, c2 = 0;
     float d[8], n[8];
 #pragma unroll
@@ -432,13 +418,13 @@ constexpr bool norm_has_shape(uint64_t dim) { return dim >= 8 && dim <= kNormLon
   else if (dim <= 8192) F(512, 2); \
   else F(1024, 2)
 
-// As many blocks as are resident at once: more only add parts (16384 x 5120
-// backward: two blocks of 256 threads a CU 86 us, three 109; 16384 x 4096:
-// three 71, four 83).
-NormParts norm_parts(uint64_t rows, uint64_t dim) {
-  uint32_t tpr = kLongThreads, waves = 12;
+// As many blocks as are resident at once, for more only add parts (16384 x
+// 4096 layer norm, 12 waves a CU 85 us, 16 97; RMS norm in bf16, which holds no
+// sums of db and narrower rows, 71 and 67).
+NormParts norm_parts(uint64_t rows, uint64_t dim, bool light) {
+  uint32_t tpr = kLongThreads, waves = 16;
   if (norm_has_shape(dim)) {
-#define LC_NORM_SHAPE(TPR, NV) tpr = TPR, waves = NV == 1 ? 20 : NV == 2 ? 12 : 8
+#define LC_NORM_SHAPE(TPR, NV) tpr = TPR, waves = NV == 1 ? 20 : NV == 2 ? (light ? 16 : 12) : light ? 12 : 8
     LC_NORM_SHAPES(LC_NORM_SHAPE);
 #undef LC_NORM_SHAPE
   }
@@ -497,10 +483,14 @@ hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t st) {
   return a.layer ? norm_fwd_of<kF32, true>(a, st) : norm_fwd_of<kF32, false>(a, st);
 }
 
-uint64_t norm_bwd_workspace(uint64_t rows, uint64_t dim) { return norm_parts(rows, dim).parts * 2ull * dim * 4; }
+uint64_t norm_bwd_workspace(uint64_t rows, uint64_t dim) {
+  // whether a call is light goes by its kind and types
+  const uint64_t a = norm_parts(rows, dim, true).parts, b = norm_parts(rows, dim, false).parts;
+  return (a > b ? a : b) * 2 * dim * 4;
+}
 
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t st) {
-  const NormParts p = norm_parts(a.rows, a.dim);
+  const NormParts p = norm_parts(a.rows, a.dim, !a.layer && a.dtype == kBf16);
   if (a.rows > 0 && (a.part || a.dx.data)) {
     const hipError_t e = a.dtype == kBf16 ? norm_bwd_kind<kBf16>(a, p, st) : norm_bwd_kind<kF32>(a, p, st);
     if (e != hipSuccess) return e;
