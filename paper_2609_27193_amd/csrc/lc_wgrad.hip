@@ -132,6 +132,7 @@ struct WgradTiles {
   float* sums;           // [sum_parts][n] column sums of dY
   uint32_t sum_parts;
   bool big;              // wgrad_big_kernel's tiles
+  bool ragged;           // of rows that end inside 16 bytes
 };
 
 struct WgradItem {
@@ -405,8 +406,9 @@ struct BigStage {
 };
 
 // The next `rows` of an operand, 32 at most: an offset past the last one's end
-// reads zeros; past another's end it reads the row behind it, whose columns
-// are not stored.
+// (and what may be read behind it) reads zeros; past another's end it reads the
+// row behind it, whose columns are not stored.  The hardware looks at four bytes
+// at a time: those that the end divides read zeros, too.
 __device__ __forceinline__ tile_t step_tile(uint64_t base, int rows, uint32_t pitch, uint32_t width) {
   const uint32_t bytes = static_cast<uint32_t>(rows - 1) * pitch + width;
   return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0u);
@@ -439,13 +441,19 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
   for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
     const WgradItem w = wgrad_item(s, a.rows, b);
     const uint32_t n0 = w.n0, k0 = w.k0;
-    const uint64_t t_begin = w.t_begin, t_end = w.t_end;
+    // Where rows end inside 16 bytes, a thread reads up to 16 bytes behind them:
+    // the row that follows has them.  Nothing follows the last one, whose product
+    // is added at the end.
+    const uint32_t behind = s.ragged ? 16 : 0;
+    const bool last = s.ragged && w.t_end == a.rows && a.rows > 0;
+    const uint64_t t_begin = w.t_begin, t_end = last ? w.t_end - 1 : w.t_end;
     // the next step to load; nothing is left of one behind the last
     int left = static_cast<int>(t_end - t_begin);
     uint64_t dy_next = a.dy.data + (t_begin * a.dy.stride + n0) * 2;
     uint64_t x_next = a.x.codes + t_begin * a.x.code_stride + k0;
     uint64_t s_next = a.x.scales + t_begin * a.x.scale_stride + k0 / kActBlock;
-    const uint32_t dy_width = (a.n - n0) * 2, x_width = a.k - k0, s_width = (x_width + kActBlock - 1) / kActBlock;
+    const uint32_t dy_width = (a.n - n0) * 2 + behind, x_width = a.k - k0 + behind;
+    const uint32_t s_width = (a.k - k0 + kActBlock - 1) / kActBlock;
     auto load = [&](BigStage& g) {
       const int rows = left < static_cast<int>(kStep) ? left : static_cast<int>(kStep);
       const tile_t td = step_tile(dy_next, rows, dy_pitch, dy_width);
@@ -553,6 +561,12 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
     // out of the registers through LDS, 32 rows of dW a wave at a time, so
     // that a lane has eight neighbours of k (every other eight: see above)
     float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * kBigOut;
+    const uint32_t lk = lane % 16 * 16 + wk / 16;
+    float x_last[8] = {};
+    if (last && k0 + lk < a.k) {
+      const uint32_t g = (k0 + lk) / 8;
+      act_decode8(load_kept8(a.x, a.rows - 1, g, in_group(a.k, g)), act_scale(load_kept_code(a.x, a.rows - 1, g)), x_last);
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -566,7 +580,13 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
       for (uint32_t q = lane / 16; q < 32; q += 4) {
         const uint32_t ln = wn + 32 * j + q;
         const float sum = a.col_shift && n0 + ln < a.n ? s.sums[n0 + ln] : 0.0f;
-        wgrad_out8(a, s, w, ln, lane % 16 * 16 + wk / 16, sum, mine + q * kBigOut + lane % 16 * 8);
+        float* const row = mine + q * kBigOut + lane % 16 * 8;
+        if (last && n0 + ln < a.n) {
+          const float d = load1<kBf16>(a.dy.data + ((a.rows - 1) * a.dy.stride + n0 + ln) * 2);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) row[e] = __builtin_fmaf(d, x_last[e], row[e]);
+        }
+        wgrad_out8(a, s, w, ln, lk, sum, row);
       }
     }
     __syncthreads();
@@ -677,12 +697,11 @@ WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big) {
   return s;
 }
 
-// The 256-column kernel takes what its loads can: a bf16 dY, rows of whole
-// 16-byte groups, and no tile that is mostly outside.
+// The 256-column kernel takes a bf16 dY where its tiles are not mostly outside
+// and its loads' 32-bit offsets reach.
 bool wgrad_is_big(const Wgrad& a) {
   const auto pad = [&](uint64_t t) { return (a.n + t - 1) / t * t * ((a.k + t - 1) / t * t); };
-  return a.dtype == kBf16 && a.n % 8 == 0 && a.k % 16 == 0 && a.dy.data % 16 == 0 && a.dy.stride % 8 == 0 &&
-         a.dy.stride < (1u << 25) && a.x.codes % 16 == 0 && a.x.code_stride % 16 == 0 && a.x.code_stride < (1u << 26) &&
+  return a.dtype == kBf16 && a.n >= 8 && a.k >= 16 && a.dy.stride < (1u << 25) && a.x.code_stride < (1u << 26) &&
          a.x.scale_stride < (1u << 26) && a.rows < (1u << 30) && pad(kBigTile) * 2 <= pad(kTile) * 3;
 }
 
@@ -722,6 +741,7 @@ uint64_t wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k) {
 
 hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
   WgradTiles s = wgrad_cut(a.rows, a.n, a.k, wgrad_is_big(a));
+  s.ragged = a.n % 8 != 0 || a.k % 16 != 0;
   s.part = reinterpret_cast<float*>(a.ws);
   s.sums = reinterpret_cast<float*>(a.ws + wgrad_part_bytes(s));
   const bool sums = a.dbias || a.col_shift;

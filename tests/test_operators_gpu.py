@@ -543,7 +543,9 @@ WGRAD = [(0, 5, 9), (1, 1, 1), (3, 7, 5), (31, 16, 33), (32, 128, 128), (33, 130
          (513, 300, 260), (1000, 40, 1030), (4100, 70, 50), (300, 2100, 2050), (96, 4112, 520),
          # whole 16-byte groups: the tiles of 256, ragged, split and not, behind the last step and at one token
          (1, 256, 256), (31, 200, 208), (64, 264, 512), (65, 512, 272), (1000, 520, 1040), (4099, 256, 272),
-         (700, 4096, 4352), (520, 2312, 4096)]
+         (700, 4096, 4352), (520, 2312, 4096),
+         # rows that end inside 16 bytes: the last token apart
+         (1, 250, 251), (2, 251, 500), (33, 510, 249), (64, 765, 1021), (129, 257, 511), (4096, 253, 255), (2000, 1001, 3000)]
 
 
 @pytest.mark.parametrize("rows,n,k", WGRAD)
