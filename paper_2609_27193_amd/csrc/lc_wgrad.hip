@@ -175,56 +175,54 @@ __device__ __forceinline__ float* wgrad_part(const WgradTiles& s, uint32_t tile,
   return s.part + ((static_cast<uint64_t>(tile - s.full) * s.splits + split) * s.tile + n) * s.tile;
 }
 
-// The whole sum at (n, k), and eight neighbours of k of it, with everything that
-// the result has besides.
-__device__ __forceinline__ void wgrad_write1(const Wgrad& a, uint64_t n, uint32_t k, float sum, float v) {
-  if (a.col_scale) v *= load_param(a.col_scale, k, a.param_dtype);
-  if (a.col_shift) v += sum * load_param(a.col_shift, k, a.param_dtype);
-  const uint64_t at = n * a.dw.stride + k;
-  if (a.accumulate) v += load_param(a.dw.data, at, a.dw_dtype);
-  store_param(a.dw.data, at, a.dw_dtype, v);
+// What a lane's eight columns of k have besides their sums.
+struct WgradCols {
+  uint32_t k;
+  int in;  // of the eight, that exist
+  float scale[8], shift[8];
+};
+__device__ __forceinline__ WgradCols wgrad_cols(const Wgrad& a, uint32_t k) {
+  WgradCols c;
+  c.k = k;
+  c.in = static_cast<int>(a.k) - static_cast<int>(k);
+  load_params8(a.col_scale, a.param_dtype, k / 8, c.in, 1.0f, c.scale);
+  load_params8(a.col_shift, a.param_dtype, k / 8, c.in, 0.0f, c.shift);
+  return c;
 }
-__device__ __forceinline__ void load8_of(uint64_t p, uint64_t i, int dtype, float (&f)[8]) {
-  if (dtype == kBf16) unpack8<kBf16>(load8_raw<kBf16>(p + 2 * i), f);
-  else unpack8<kF32>(load8_raw<kF32>(p + 4 * i), f);
-}
-__device__ __forceinline__ void wgrad_write8(const Wgrad& a, uint64_t n, uint32_t k, float sum, float (&v)[8]) {
-  float w[8];
-  if (a.col_scale) {
-    load8_of(a.col_scale, k, a.param_dtype, w);
+// The whole sums of row n at these columns, into dW.
+__device__ __forceinline__ void wgrad_write8(const Wgrad& a, uint64_t n, const WgradCols& c, float sum, float (&v)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= w[e];
-  }
+  for (int e = 0; e < 8; ++e) v[e] *= c.scale[e];
   if (a.col_shift) {
-    load8_of(a.col_shift, k, a.param_dtype, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += sum * w[e];
+    for (int e = 0; e < 8; ++e) v[e] += sum * c.shift[e];
   }
-  const uint64_t at = n * a.dw.stride + k;
-  if (a.accumulate) {
-    load8_of(a.dw.data, at, a.dw_dtype, w);
+  const uint64_t at = n * a.dw.stride + c.k;
+  float w[8];
+  if (a.dw_dtype == kBf16) {
+    const uint64_t p = a.dw.data + 2 * at;
+    if (a.accumulate) {
+      unpack8<kBf16>(load8_raw<kBf16>(p, c.in), w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += w[e];
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
+    store8<kBf16>(p, v, c.in);
+  } else {
+    const uint64_t p = a.dw.data + 4 * at;
+    if (a.accumulate) {
+      unpack8<kF32>(load8_raw<kF32>(p, c.in), w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += w[e];
+    }
+    store8<kF32>(p, v, c.in);
   }
-  if (a.dw_dtype == kBf16) store8<kBf16>(a.dw.data + 2 * at, v, 8);
-  else store8<kF32>(a.dw.data + 4 * at, v, 8);
 }
-// Row `ln` of the tile from column `lk` on, which lies at `src`: into the part
-// of a split tile, else into dW.
-__device__ __forceinline__ void wgrad_out8(const Wgrad& a, const WgradTiles& s, const WgradItem& w, uint32_t ln, uint32_t lk,
-                                           float sum, const float* src) {
-  const uint64_t n = w.n0 + ln;
-  const uint32_t k = w.k0 + lk;
-  if (!w.whole || (n < a.n && k + 8 <= a.k)) {
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = src[e];
-    if (!w.whole) store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + lk), v, 8);
-    else wgrad_write8(a, n, k, sum, v);
-  } else if (n < a.n) {
-#pragma unroll 1
-    for (uint32_t e = 0; k + e < a.k; ++e) wgrad_write1(a, n, k + e, sum, src[e]);
-  }
+// Row `ln` of the tile from the columns' first on: into the part of a split
+// tile, else into dW.
+__device__ __forceinline__ void wgrad_out8(const Wgrad& a, const WgradTiles& s, const WgradItem& w, const WgradCols& c,
+                                           uint32_t ln, float sum, float (&v)[8]) {
+  if (!w.whole) store8<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, w.tile, w.split, ln) + (c.k - w.k0)), v, 8);
+  else if (w.n0 + ln < a.n && c.in > 0) wgrad_write8(a, w.n0 + ln, c, sum, v);
 }
 __device__ __forceinline__ void wgrad_write_bias(const Wgrad& a, uint64_t n, float sum) {
   if (a.accumulate) sum += load_param(a.dbias, n, a.dw_dtype);
@@ -365,9 +363,14 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<f32x4*>(mine + (16 * j + lane % 16) * kOut + 16 * i + lane / 16 * 4) = acc[i][j];
-#pragma unroll 1
-    for (uint32_t q = lane / 8; q < 64; q += 8)
-      wgrad_out8(a, s, w, wn + q, wk + lane % 8 * 8, SUMS ? colsum[0][wn + q] : 0.0f, mine + q * kOut + lane % 8 * 8);
+    const WgradCols cols = wgrad_cols(a, k0 + wk + lane % 8 * 8);
+#pragma unroll 2
+    for (uint32_t q = lane / 8; q < 64; q += 8) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + lane % 8 * 8 + e];
+      wgrad_out8(a, s, w, cols, wn + q, SUMS ? colsum[0][wn + q] : 0.0f, v);
+    }
     __syncthreads();
   }
 }
@@ -561,12 +564,10 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
     // out of the registers through LDS, 32 rows of dW a wave at a time, so
     // that a lane has eight neighbours of k (every other eight: see above)
     float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * kBigOut;
-    const uint32_t lk = lane % 16 * 16 + wk / 16;
+    const WgradCols cols = wgrad_cols(a, k0 + lane % 16 * 16 + wk / 16);
     float x_last[8] = {};
-    if (last && k0 + lk < a.k) {
-      const uint32_t g = (k0 + lk) / 8;
-      act_decode8(load_kept8(a.x, a.rows - 1, g, in_group(a.k, g)), act_scale(load_kept_code(a.x, a.rows - 1, g)), x_last);
-    }
+    if (last && cols.in > 0)
+      act_decode8(load_kept8(a.x, a.rows - 1, cols.k / 8, cols.in), act_scale(load_kept_code(a.x, a.rows - 1, cols.k / 8)), x_last);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -579,14 +580,16 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
 #pragma unroll 1
       for (uint32_t q = lane / 16; q < 32; q += 4) {
         const uint32_t ln = wn + 32 * j + q;
-        const float sum = a.col_shift && n0 + ln < a.n ? s.sums[n0 + ln] : 0.0f;
-        float* const row = mine + q * kBigOut + lane % 16 * 8;
-        if (last && n0 + ln < a.n) {
+        const bool on = n0 + ln < a.n;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = mine[q * kBigOut + lane % 16 * 8 + e];
+        if (last && on) {
           const float d = load1<kBf16>(a.dy.data + ((a.rows - 1) * a.dy.stride + n0 + ln) * 2);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) row[e] = __builtin_fmaf(d, x_last[e], row[e]);
+          for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(d, x_last[e], v[e]);
         }
-        wgrad_out8(a, s, w, ln, lk, sum, row);
+        wgrad_out8(a, s, w, cols, ln, a.col_shift && on ? s.sums[n0 + ln] : 0.0f, v);
       }
     }
     __syncthreads();
@@ -617,13 +620,7 @@ __global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTile
       for (uint32_t p = 0; p < s.sum_parts; ++p) sum += s.sums[p * static_cast<uint64_t>(a.n) + n];
     }
     if (bias) wgrad_write_bias(a, n, sum);
-    if (in >= 8) {
-      wgrad_write8(a, n, k0 + lk, sum, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < in) wgrad_write1(a, n, k0 + lk + e, sum, v[e]);
-    }
+    wgrad_write8(a, n, wgrad_cols(a, k0 + lk), sum, v);
   }
 }
 
@@ -668,53 +665,51 @@ __global__ __launch_bounds__(64) void wgrad_sums_join_kernel(Wgrad a, const floa
 }
 
 // The cut.  More parts shorten what a block takes over the tokens and cost
-// their sums' way through memory; the figures are measured (us): a step of 32
-// tokens takes a block of 256 columns 0.88 and one of 128 about 1.0 (two a CU;
-// three times the products for an fp32 dY), a part's sums 0.105 and 0.026
-// there and back, the join's launch 4.
-WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big) {
+// their sums' way through memory.  The figures are measured (us): what a block
+// of 256 columns takes beside its steps 14 (ragged 19), a step of 32 tokens 0.6,
+// with every CU at work 0.85; of 128 columns 7, 0.65 and, two a CU, 1.0; a part's
+// sums there and back 0.105 and 0.018, the join's launch 4 and 0.12 a part.  By
+// it (measured) 4096 tokens x 512 x 512 take 23 (23) in tiles of 128 and 31 (30)
+// of 256, 16000 x 1500 x 2100 147 (134) of 256, and 64 x 14000 x 2000 26 (24) and
+// 31 (34).
+WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big, double* best_us) {
   WgradTiles s{};
   s.big = big;
+  s.ragged = n % 8 != 0 || k % 16 != 0;
   s.tile = big ? kBigTile : kTile;
   s.tn = static_cast<uint32_t>((n + s.tile - 1) / s.tile);
   s.tk = static_cast<uint32_t>((k + s.tile - 1) / s.tile);
   s.tiles = s.tn * s.tk;
-  const uint64_t at_once = big ? 256 : 512, rest = s.tiles % at_once, steps = (rows + kStep - 1) / kStep;
-  const double step_us = big ? 0.88 : 1.0, part_us = big ? 0.105 : 0.026;
+  const uint32_t at_once = big ? 256 : 512, rest = s.tiles % at_once;
+  const uint64_t rounds = s.tiles / at_once, steps = (rows + kStep - 1) / kStep;
+  const double block_us = !big ? 7.0 : s.ragged ? 19.0 : 14.0, part_us = big ? 0.105 : 0.018;
+  const double whole_us = rounds * (steps * (big ? 0.85 : 1.0) + (big ? block_us : 3.0)) + (big ? 0.0 : block_us);
   uint64_t best = 1;
-  double best_us = steps * step_us;
-  for (uint64_t splits = 2; rest && splits <= at_once / rest && splits <= steps; ++splits) {
-    const double us = (steps + splits - 1) / splits * step_us + splits * rest * part_us + 4.0;
-    if (us < best_us) {
-      best_us = us;
+  *best_us = 1e30;
+  // the small kernel splits every tile or none: it takes a whole tile's column
+  // sums along, and the parts of a column of tiles have to be alike
+  for (uint64_t splits = 1; splits == 1 || (rest && (big || !rounds) && splits <= at_once / rest && splits <= steps); ++splits) {
+    const double blocks = static_cast<double>(splits) * rest;
+    const double step_us = big ? 0.6 + 0.25 * blocks / 256 : 0.65 + (blocks > 256 ? 0.35 * (blocks - 256) / 256 : 0.0);
+    const double us = whole_us + (rest ? (steps + splits - 1) / splits * step_us + (big ? block_us : rounds ? 3.0 : 0.0) : 0.0) +
+                      (splits > 1 ? blocks * part_us + 4.0 + 0.12 * splits : 0.0);
+    if (us < *best_us) {
+      *best_us = us;
       best = splits;
     }
   }
   s.per_split = (steps + best - 1) / best * kStep;
   s.splits = steps ? static_cast<uint32_t>((rows + s.per_split - 1) / s.per_split) : 1;
-  s.full = s.splits > 1 ? s.tiles - static_cast<uint32_t>(rest) : s.tiles;
+  s.full = s.splits > 1 ? s.tiles - rest : s.tiles;
   s.sum_parts = big ? 1 : s.splits;
   return s;
 }
 
-// The 256-column kernel takes a bf16 dY where its tiles are not mostly outside
-// and its loads' 32-bit offsets reach.
-bool wgrad_is_big(const Wgrad& a) {
-  const auto pad = [&](uint64_t t) { return (a.n + t - 1) / t * t * ((a.k + t - 1) / t * t); };
+// The 256-column kernel takes a bf16 dY, as far as its loads' 32-bit offsets
+// reach.
+bool wgrad_may_be_big(const Wgrad& a) {
   return a.dtype == kBf16 && a.n >= 8 && a.k >= 16 && a.dy.stride < (1u << 25) && a.x.code_stride < (1u << 26) &&
-         a.x.scale_stride < (1u << 26) && a.rows < (1u << 30) && pad(kBigTile) * 2 <= pad(kTile) * 3;
-}
-
-// The small kernel takes a whole tile's column sums along and splits every
-// tile or none, so that the parts of a column of tiles are alike.
-WgradTiles wgrad_cut(uint64_t rows, uint64_t n, uint64_t k, bool big) {
-  WgradTiles s = wgrad_tiles(rows, n, k, big);
-  if (!big && s.full && s.full < s.tiles) {
-    s.splits = 1;
-    s.full = s.tiles;
-    s.sum_parts = 1;
-  }
-  return s;
+         a.x.scale_stride < (1u << 26) && a.rows < (1u << 30);
 }
 
 uint64_t wgrad_part_bytes(const WgradTiles& s) {
@@ -734,14 +729,19 @@ uint64_t wgrad_space(const WgradTiles& s, uint64_t n) {
 
 uint64_t wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k) {
   // which tiles a call takes goes by its types and alignment, too
-  const uint64_t big = wgrad_space(wgrad_cut(rows, n, k, true), n);
-  const uint64_t small = wgrad_space(wgrad_cut(rows, n, k, false), n);
+  double us;
+  const uint64_t big = wgrad_space(wgrad_tiles(rows, n, k, true, &us), n);
+  const uint64_t small = wgrad_space(wgrad_tiles(rows, n, k, false, &us), n);
   return big > small ? big : small;
 }
 
 hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
-  WgradTiles s = wgrad_cut(a.rows, a.n, a.k, wgrad_is_big(a));
-  s.ragged = a.n % 8 != 0 || a.k % 16 != 0;
+  double us, big_us;
+  WgradTiles s = wgrad_tiles(a.rows, a.n, a.k, false, &us);
+  if (wgrad_may_be_big(a)) {
+    const WgradTiles big = wgrad_tiles(a.rows, a.n, a.k, true, &big_us);
+    if (big_us <= us) s = big;
+  }
   s.part = reinterpret_cast<float*>(a.ws);
   s.sums = reinterpret_cast<float*>(a.ws + wgrad_part_bytes(s));
   const bool sums = a.dbias || a.col_shift;

@@ -51,9 +51,10 @@ def calls(h):
         out.append((f"dw {dim}", lambda back=back: back(dx=False), [bwd, "join"]))
     out.append(("save", lambda: LC.lc_act_save(M(5, 40), K(5, 40)), ["save"]))
     out.append(("load", lambda: LC.lc_act_load(K(5, 40), M(5, 40)), ["load"]))
-    for rows, n, k, dt, bias, kernels in [(64, 256, 256, B, False, ["big"]), (4096, 256, 256, B, False, ["big", "join"]),
-                                          (64, 256, 256, B, True, ["sums_k", "sums_join", "big"]),
-                                          (64, 100, 256, B, True, ["wgrad_kernel"]), (64, 256, 256, F, False, ["wgrad_kernel"]),
+    for rows, n, k, dt, bias, kernels in [(4096, 4096, 4096, B, False, ["big"]), (8192, 1024, 4096, B, False, ["big", "join"]),
+                                          (4096, 4096, 4096, B, True, ["sums_k", "sums_join", "big"]),
+                                          (4096, 4095, 4097, B, False, ["big", "join"]), (64, 100, 256, B, True, ["wgrad_kernel"]),
+                                          (64, 256, 256, F, False, ["wgrad_kernel"]),
                                           (4096, 256, 256, F, True, ["wgrad_kernel", "join"])]:
         def go(rows=rows, n=n, k=k, dt=dt, bias=bias):
             need = LC.lc_linear_wgrad_workspace(rows, n, k)
