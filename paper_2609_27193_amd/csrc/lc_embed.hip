@@ -84,16 +84,20 @@ __device__ __forceinline__ void fill_rows(const Fill& f, uint64_t block, uint64_
 }
 
 // ---- sorting the tokens ------------------------------------------------------------
-// Few tokens need no order (embed_direct_kernel, below).  Up to kRankTokens one launch counts, for every token, the tokens that come
-// before it (a smaller row, or the same row at an earlier position); beyond
-// that a radix sort of kDigitBits a pass, two launches a pass.  The sort's few
+// Few tokens need no order (embed_direct_kernel, below).  Up to kRankTokens one
+// launch counts, for every token, the tokens that come before it (a smaller row,
+// or the same row at an earlier position); beyond that a radix sort of kDigitBits
+// a pass, two launches a pass.  Of the whole gradient into 32000 x 1024, added to
+// what is there: 4096 tokens 22 us by counts and 32 by passes, 8192 tokens 38 and
+// 31.  Both are bound by latency: 4096 tokens, counted, about 8 us; a pass of
+// 16384 tokens 2.5 to 4.7 and 4.5 to 5.3 us for its two launches.  Their few
 // blocks leave the chip to others, which clear the table meanwhile, rows with a
 // token and without: writing the former twice costs less than the sort's time
-// alone (16384 tokens into 128256 x 2048: 152 us where the sums' launch cleared
-// the rows without a token).
-constexpr uint32_t kRankTokens = 8192;
+// alone (16384 tokens into 128256 x 2048: 123 us, and 152 where the sums' launch
+// cleared the rows without a token).
+constexpr uint32_t kRankTokens = 4096;
 constexpr uint32_t kRankThreads = 256;
-constexpr uint32_t kRankOwn = 32;  // tokens of a block; its 8 slices of threads share the others
+constexpr uint32_t kRankOwn = 8;  // tokens of a block; its 32 slices of threads share the others
 constexpr uint32_t kDigitBits = 9, kDigits = 1u << kDigitBits;
 constexpr uint32_t kSortThreads = 512;
 constexpr uint32_t kSortWaves = kSortThreads / 64;
@@ -278,6 +282,34 @@ __host__ inline uint32_t sum_run(uint64_t n, uint64_t chunks) {
   return static_cast<uint32_t>(r);
 }
 
+// The eight columns that a lane sums.  Every load of a group of rows goes out
+// without a condition, or the compiler waits for each: a lane without columns
+// reads the row's last eight, and so does the lane of a row's last, smaller
+// group, which moves its sums down at the end (WHOLE: rows of at least eight
+// columns).
+struct Cols {
+  uint32_t g, at;  // the group of eight, and the first column that is read
+  int in;          // columns of the group
+};
+__device__ __forceinline__ Cols sum_cols(uint32_t dim, uint32_t chunk) {
+  const uint32_t g = chunk * (kSumCols / 8) + (threadIdx.x & 63);
+  return Cols{g, dim >= 8 && 8 * g > dim - 8 ? dim - 8 : 8 * g, in_group(dim, g)};
+}
+template <int DT, bool WHOLE>
+__device__ __forceinline__ Raw8<DT> load_cols(uint64_t row, const Cols& c) {
+  if constexpr (WHOLE) return load8_raw<DT>(row + c.at * static_cast<uint64_t>(kEsz<DT>));
+  else return load8_raw<DT>(row, c.in);
+}
+__device__ __forceinline__ void move_down(const Cols& c, float (&f)[8]) {
+  const uint32_t s = 8 * c.g - c.at;
+  if (c.in <= 0 || s == 0) return;
+#pragma unroll
+  for (int b = 4; b; b >>= 1)
+    if (s & b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = e + b < 8 ? f[e + b] : 0.0f;
+}
+
 struct SumArgs {
   Rows dout, dw;
   const uint32_t* keys;
@@ -312,13 +344,12 @@ __device__ __forceinline__ void part_write(float* p, uint32_t g, const float (&a
   store8<kF32>(reinterpret_cast<uint64_t>(p) + 32ull * g, acc, n);
 }
 
-template <int DDT, int GDT>
+template <int DDT, int GDT, bool WHOLE>
 __device__ void sum_tile(const SumArgs& a, uint64_t item) {
   constexpr int U = 8;  // rows in flight
   const uint32_t lane = threadIdx.x & 63;
   const uint32_t tile = static_cast<uint32_t>(item / a.chunks), chunk = static_cast<uint32_t>(item % a.chunks);
-  const uint32_t g = chunk * (kSumCols / 8) + lane;
-  const int in = in_group(a.dim, g);
+  const Cols cols = sum_cols(a.dim, chunk);
   const uint64_t b0 = static_cast<uint64_t>(tile) * a.run;
   const uint64_t b1 = b0 + a.run < a.n ? b0 + a.run : a.n;
   const uint32_t none = static_cast<uint32_t>(a.vocab);
@@ -328,10 +359,11 @@ __device__ void sum_tile(const SumArgs& a, uint64_t item) {
   uint32_t cur = none;
   bool open_left = false;
   auto flush = [&](bool open_right) {
-    if (cur == none || in <= 0) return;
-    if (open_left) part_write(sum_part(a, tile, 0), g, acc, in);
-    else if (open_right) part_write(sum_part(a, tile, 1), g, acc, in);
-    else sum_write<GDT>(a, cur, g, acc, in);
+    if (cur == none || cols.in <= 0) return;
+    if constexpr (WHOLE) move_down(cols, acc);
+    if (open_left) part_write(sum_part(a, tile, 0), cols.g, acc, cols.in);
+    else if (open_right) part_write(sum_part(a, tile, 1), cols.g, acc, cols.in);
+    else sum_write<GDT>(a, cur, cols.g, acc, cols.in);
   };
   for (uint64_t c0 = b0; c0 < b1; c0 += 64) {
     const uint32_t m = static_cast<uint32_t>(b1 - c0 < 64 ? b1 - c0 : 64);
@@ -340,12 +372,12 @@ __device__ void sum_tile(const SumArgs& a, uint64_t item) {
     for (uint32_t u0 = 0; u0 < m; u0 += U) {
       Raw8<DDT> r[U];
       uint32_t k[U];
+      if (static_cast<uint32_t>(__builtin_amdgcn_readlane(key, u0)) == none) break;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        k[u] = u0 + u < m ? __builtin_amdgcn_readlane(key, u0 + u) : none;
-        const uint32_t p = __builtin_amdgcn_readlane(at, (u0 + u) & 63);
-        if (k[u] != none && in > 0)
-          r[u] = load8_raw<DDT>(a.dout.data + (static_cast<uint64_t>(p) * a.dout.stride + 8ull * g) * kEsz<DDT>, in);
+        k[u] = __builtin_amdgcn_readlane(key, u0 + u);  // `none` behind the last token, at position 0
+        const uint32_t p = __builtin_amdgcn_readlane(at, u0 + u);
+        r[u] = load_cols<DDT, WHOLE>(a.dout.data + static_cast<uint64_t>(p) * a.dout.stride * kEsz<DDT>, cols);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -358,11 +390,9 @@ __device__ void sum_tile(const SumArgs& a, uint64_t item) {
           for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
         }
         float f[8];
-        if (in > 0) {
-          unpack8<DDT>(r[u], f);
+        unpack8<DDT>(r[u], f);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) acc[e] += f[e];
-        }
+        for (int e = 0; e < 8; ++e) acc[e] += f[e];
       }
     }
   }
@@ -390,7 +420,9 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(SumArgs a) {
   const uint64_t items = static_cast<uint64_t>(a.tiles) * a.chunks;
   for (uint64_t b = blockIdx.x; b * (kSumThreads / 64) < items; b += gridDim.x) {
     const uint64_t item = b * (kSumThreads / 64) + (threadIdx.x >> 6);
-    if (item < items) sum_tile<DDT, GDT>(a, item);
+    if (item >= items) continue;
+    if (a.dim >= 8) sum_tile<DDT, GDT, true>(a, item);
+    else sum_tile<DDT, GDT, false>(a, item);
   }
 }
 
@@ -448,29 +480,38 @@ __global__ __launch_bounds__(kSumThreads) void embed_join_kernel(SumArgs a) {
 }
 
 // ---- few tokens: one launch ---------------------------------------------------------------
-// A block takes a token, looks for it among all of them, and where it is the
-// first of its row sums the row; its four waves share the row's columns, or,
-// of few columns, its tokens.  Other blocks clear the rows without a token.
-constexpr uint32_t kDirectTokens = 1024;
-constexpr uint32_t kDirectWaves = kSumThreads / 64;
+// A block takes a token and lists the positions of its row in their order.  A
+// row of up to kDirectAlone tokens is summed by the block of the first of them,
+// 512 columns a wave.  Of more, the block of token q takes columns 512 q and on:
+// there each wave sums a run of the tokens and the first wave adds the others'
+// sums.  Other blocks clear the rows without a token.
+// Bound by the launch and the reads' latency: 1024 tokens, as often as words,
+// added to rows of 2048 columns in bf16 5.8 us (sorted 20.2); all of one row
+// 29.5 (sorted 15.7), for one block then reads a column's tokens.  Up to 1024
+// tokens blocks of 256 threads (512: 8.8 and 18.6 us), to 2048 of 512, where the
+// one row costs more (rows of 1024: 14.9, 256 threads 11.2, sorted 20.7; one row
+// 33, 59 and 20).  4096 tokens: 36 us, sorted 25.
+constexpr uint32_t kDirectTokens = 2048;
+constexpr uint32_t kDirectSlots = 4;  // tokens of a thread: 256 threads up to 1024 tokens, then 512
+constexpr uint32_t kDirectAlone = 8;
 
-template <int DDT, int GDT>
-__global__ __launch_bounds__(kSumThreads) void embed_direct_kernel(EmbedBwd a, Fill fill, uint64_t fills) {
-  constexpr uint32_t W = kDirectWaves, PER = kDirectTokens / W;
-  constexpr int U = 8;  // rows in flight
-  __shared__ uint16_t list[W][PER];  // positions of the row's tokens, a quarter of them a wave's find
+template <int DDT, int GDT, bool WHOLE, uint32_t THREADS>
+__global__ __launch_bounds__(THREADS) void embed_direct_kernel(EmbedBwd a, Fill fill, uint64_t fills) {
+  constexpr uint32_t W = THREADS / 64;
+  constexpr int U = kDirectAlone;  // rows in flight
+  __shared__ uint16_t list[kDirectSlots * THREADS];  // positions of the row's tokens
   __shared__ uint32_t found[W];
-  __shared__ uint32_t earlier;
+  __shared__ uint32_t own;  // where the block's token is in the list
   __shared__ unsigned long long touched;
   __shared__ float sums[W][kSumCols];
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t n = static_cast<uint32_t>(a.n);
+  const uint32_t n = static_cast<uint32_t>(a.n), chunks = (a.dim + kSumCols - 1) / kSumCols;
   for (uint64_t b = blockIdx.x; b < n + fills; b += gridDim.x) {
     if (b >= n) {
       const uint64_t r0 = (b - n) * fill.per;
       if (threadIdx.x == 0) touched = 0;
       __syncthreads();
-      for (uint32_t j = threadIdx.x; j < n; j += kSumThreads) {
+      for (uint32_t j = threadIdx.x; j < n; j += THREADS) {
         const uint64_t row = token_row(a.tokens, a.token64, j, a.first, a.vocab);
         if (row >= r0 && row < r0 + fill.per) atomicOr(&touched, 1ull << (row - r0));  // any order gives the same
       }
@@ -483,81 +524,80 @@ __global__ __launch_bounds__(kSumThreads) void embed_direct_kernel(EmbedBwd a, F
     const uint32_t i = static_cast<uint32_t>(b);
     const uint32_t row = token_row(a.tokens, a.token64, i, a.first, a.vocab);
     if (row >= a.vocab) continue;  // the same for the whole block
-    if (threadIdx.x == 0) earlier = 0;
-    __syncthreads();
-    const uint32_t per = (n + W - 1) / W, j0 = wave * per, j1 = j0 + per < n ? j0 + per : n;
+    const uint32_t j0 = wave * (64 * kDirectSlots) + lane;
+    uint64_t same[kDirectSlots];
     uint32_t count = 0;
-    for (uint32_t j = j0 + lane; j < j0 + per; j += 64) {  // whole waves
-      const bool same = j < j1 && token_row(a.tokens, a.token64, j, a.first, a.vocab) == row;
-      const uint64_t all = __ballot(same);
-      if (same) {
-        list[wave][count + __popcll(all & ((1ull << lane) - 1))] = static_cast<uint16_t>(j);
-        if (j < i) earlier = 1;
-      }
-      count += __popcll(all);
+#pragma unroll
+    for (uint32_t s = 0; s < kDirectSlots; ++s) {
+      const uint32_t j = j0 + s * 64;
+      same[s] = __ballot(j < n && token_row(a.tokens, a.token64, j < n ? j : 0, a.first, a.vocab) == row);
+      count += __popcll(same[s]);
     }
     if (lane == 0) found[wave] = count;
     __syncthreads();
-    const bool first = earlier == 0;
-    uint32_t start[W + 1] = {};
+    uint32_t total = 0, at = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < W; ++w) start[w + 1] = start[w] + found[w];
+    for (uint32_t w = 0; w < W; ++w) {
+      total += found[w];
+      at += w < wave ? found[w] : 0;
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < kDirectSlots; ++s) {
+      const uint32_t to = at + __popcll(same[s] & ((1ull << lane) - 1));
+      if (same[s] >> lane & 1) list[to] = static_cast<uint16_t>(j0 + s * 64);
+      if (j0 + s * 64 == i) own = to;
+      at += __popcll(same[s]);
+    }
     __syncthreads();
-    if (!first) continue;
-    const uint32_t total = start[W];
-    // token t of the row, in the order of the positions
-    auto position = [&](uint32_t t) {
-      uint32_t w = 0;
-#pragma unroll
-      for (uint32_t q = 1; q < W; ++q) w += t >= start[q];
-      uint32_t from = 0;
-#pragma unroll
-      for (uint32_t q = 0; q < W; ++q) from = q == w ? start[q] : from;
-      return static_cast<uint32_t>(list[w][t - from]);
-    };
-    const uint32_t chunks = (a.dim + kSumCols - 1) / kSumCols;
-    const uint32_t share = chunks == 1 ? 4 : chunks == 2 ? 2 : 1;  // waves of a chunk
-    for (uint32_t c0 = 0; c0 < chunks; c0 += W / share) {
-      const uint32_t chunk = c0 + wave / share, part = wave % share;
-      const uint32_t g = chunk * (kSumCols / 8) + lane;
-      const int in = in_group(a.dim, g);
-      const uint64_t to = a.dw.data + (static_cast<uint64_t>(row) * a.dw.stride + 8ull * g) * kEsz<GDT>;
-      Raw8<GDT> old = load8_raw<GDT>(to, a.accumulate && part == 0 ? in : 0);
+    // the same for the whole block; the next list is written behind a barrier
+    const bool shared = total > kDirectAlone;
+    const uint32_t from = shared ? own : own * chunks + wave, step = shared ? total : W;
+    const uint32_t run = shared ? (total + W - 1) / W : total;
+    const uint32_t t0 = shared ? wave * run : 0, t1 = t0 + run < total ? t0 + run : total;
+    for (uint32_t chunk = from; chunk < chunks; chunk += step) {
+      const Cols cols = sum_cols(a.dim, chunk);
+      const uint64_t to = a.dw.data + (static_cast<uint64_t>(row) * a.dw.stride + 8ull * cols.g) * kEsz<GDT>;
+      const bool writes = !shared || wave == 0;
+      Raw8<GDT> old = load8_raw<GDT>(to, a.accumulate && writes ? cols.in : 0);
       float acc[8] = {};
-      const uint32_t t1 = total * (part + 1) / share;
-      for (uint32_t t0 = total * part / share; t0 < t1; t0 += U) {
-        Raw8<DDT> r[U];
+      for (uint32_t c0 = t0; c0 < t1; c0 += 64) {
+        const uint32_t m = t1 - c0 < 64 ? t1 - c0 : 64;
+        const uint32_t mine = list[lane < m ? c0 + lane : c0];
+        for (uint32_t u0 = 0; u0 < m; u0 += U) {
+          Raw8<DDT> r[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const uint32_t p = t0 + u < t1 ? position(t0 + u) : 0;
-          r[u] = load8_raw<DDT>(a.dout.data + (p * a.dout.stride + 8ull * g) * kEsz<DDT>, t0 + u < t1 ? in : 0);
-        }
+          for (int u = 0; u < U; ++u) {
+            const uint32_t p = __builtin_amdgcn_readlane(mine, u0 + u);
+            r[u] = load_cols<DDT, WHOLE>(a.dout.data + p * a.dout.stride * kEsz<DDT>, cols);
+          }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float f[8];
-          unpack8<DDT>(r[u], f);
-          if (t0 + u < t1) {
+          for (int u = 0; u < U; ++u) {
+            float f[8];
+            unpack8<DDT>(r[u], f);
+            if (u0 + u < m) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += f[e];
+              for (int e = 0; e < 8; ++e) acc[e] += f[e];
+            }
           }
         }
       }
-      if (share > 1) {
+      if (shared) {
+        __syncthreads();  // the sums before are read
 #pragma unroll
         for (int e = 0; e < 8; ++e) sums[wave][e * 64 + lane] = acc[e];
         __syncthreads();
-        if (part == 0)
-          for (uint32_t q = 1; q < share; ++q)
+        if (wave == 0)
+          for (uint32_t w = 1; w < W; ++w)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += sums[wave + q][e * 64 + lane];
-        __syncthreads();
+            for (int e = 0; e < 8; ++e) acc[e] += sums[w][e * 64 + lane];
       }
-      if (part != 0 || in <= 0) continue;
+      if (!writes || cols.in <= 0) continue;
+      if constexpr (WHOLE) move_down(cols, acc);
       float f[8];
       unpack8<GDT>(old, f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = a.accumulate ? acc[e] * a.scale + f[e] : acc[e] * a.scale;
-      store8<GDT>(to, f, in);
+      store8<GDT>(to, f, cols.in);
     }
   }
 }
@@ -632,12 +672,20 @@ SortGrid sort_grid(uint64_t work, const Fill& f, uint32_t threads) {
   return g;
 }
 
-template <int DDT, int GDT>
+template <int DDT, int GDT, bool WHOLE>
 hipError_t embed_direct(const EmbedBwd& a, hipStream_t st) {
   const Fill f = whole_table(a);
-  if (a.n + fill_blocks(f) == 0) return hipSuccess;
-  return launch_op(embed_direct_kernel<DDT, GDT>, grid_for(a.n + fill_blocks(f), kSumThreads), kSumThreads, st, a, f,
-                   fill_blocks(f));
+  const uint64_t fills = fill_blocks(f);
+  if (a.n + fills == 0) return hipSuccess;
+  if (a.n <= 256 * kDirectSlots)
+    return launch_op(embed_direct_kernel<DDT, GDT, WHOLE, 256>, grid_for(a.n + fills, 256), 256, st, a, f, fills);
+  return launch_op(embed_direct_kernel<DDT, GDT, WHOLE, 512>, grid_for(a.n + fills, 512), 512, st, a, f, fills);
+}
+
+template <int DDT, int GDT>
+hipError_t embed_bwd_of(const EmbedBwd& a, const SumArgs& s, hipStream_t st) {
+  if (a.n > kDirectTokens) return embed_sums<DDT, GDT>(s, st);
+  return a.dim >= 8 ? embed_direct<DDT, GDT, true>(a, st) : embed_direct<DDT, GDT, false>(a, st);
 }
 
 }  // namespace
@@ -649,11 +697,6 @@ hipError_t launch_embed_fwd(const EmbedFwd& a, hipStream_t st) {
 uint64_t embed_bwd_workspace(uint64_t n, uint64_t dim) { return bwd_regions(n, dim).end; }
 
 hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
-  if (a.n <= kDirectTokens) {
-    if (a.dout_dtype == kBf16)
-      return a.dw_dtype == kBf16 ? embed_direct<kBf16, kBf16>(a, st) : embed_direct<kBf16, kF32>(a, st);
-    return a.dw_dtype == kBf16 ? embed_direct<kF32, kBf16>(a, st) : embed_direct<kF32, kF32>(a, st);
-  }
   const BwdRegions r = bwd_regions(a.n, a.dim);
   uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(a.ws + r.keys[0]), reinterpret_cast<uint32_t*>(a.ws + r.keys[1])};
   uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(a.ws + r.pos[0]), reinterpret_cast<uint32_t*>(a.ws + r.pos[1])};
@@ -687,7 +730,7 @@ hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
       from = to;
     }
     sorted = from;
-  } else {
+  } else if (a.n > kDirectTokens) {
     const Fill f = whole_table(a);
     const SortGrid g = sort_grid((a.n + kRankOwn - 1) / kRankOwn, f, kRankThreads);
     const hipError_t e = launch_op(embed_rank_kernel, g.blocks, kRankThreads, st, a, f, g.fill_from, keys[0], pos[0]);
@@ -708,8 +751,8 @@ hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
   s.scale = a.scale;
   s.accumulate = a.accumulate;
   if (a.dout_dtype == kBf16)
-    return a.dw_dtype == kBf16 ? embed_sums<kBf16, kBf16>(s, st) : embed_sums<kBf16, kF32>(s, st);
-  return a.dw_dtype == kBf16 ? embed_sums<kF32, kBf16>(s, st) : embed_sums<kF32, kF32>(s, st);
+    return a.dw_dtype == kBf16 ? embed_bwd_of<kBf16, kBf16>(a, s, st) : embed_bwd_of<kBf16, kF32>(a, s, st);
+  return a.dw_dtype == kBf16 ? embed_bwd_of<kF32, kBf16>(a, s, st) : embed_bwd_of<kF32, kF32>(a, s, st);
 }
 
 }  // namespace lc

@@ -222,7 +222,8 @@ def some_tokens(n, vocab, first, seed, kind):
 EMBED = [(0, 5, 8, "mixed"), (1, 1, 1, "one"), (1, 10, 4096, "mixed"), (5, 3, 7, "mixed"), (37, 50, 33, "mixed"),
          (64, 9, 513, "skewed"), (300, 1000, 256, "mixed"), (1000, 7, 1025, "skewed"), (777, 400, 96, "none"),
          (4096, 30, 64, "one"), (8192, 5000, 40, "skewed"), (8193, 5000, 40, "skewed"), (20001, 300, 72, "skewed"),
-         (9000, 300000, 8, "mixed"), (2048, 50, 2000, "skewed"), (2049, 50, 1100, "skewed"), (512, 5, 600, "one"), (33000, 11, 24, "one"), (50000, 600, 9, "none")]
+         (9000, 300000, 8, "mixed"), (2048, 50, 2000, "skewed"), (2049, 50, 1100, "skewed"), (512, 5, 600, "one"), (33000, 11, 24, "one"), (50000, 600, 9, "none"),
+         (5000, 40, 5, "skewed"), (9000, 3, 1, "mixed"), (1000, 4, 2600, "mixed"), (1024, 4, 3, "one"), (1900, 90, 1027, "skewed")]
 
 
 @pytest.mark.parametrize("n,vocab,dim,kind", EMBED)

@@ -30,8 +30,8 @@ def calls(h):
     K = lambda rows, cols: LC.saved_act(at + next(apart), at + next(apart), rows, cols)  # noqa: E731
     V = lambda: at + next(apart)  # noqa: E731
     out = [("embedding", lambda: LC.lc_embedding_forward(M(99, 64), V(), 2, 7, M(7, 64)), ["embed_fwd"])]
-    for n, vocab, kernels in [(7, 99, ["direct"]), (1024, 99, ["direct"]), (1025, 99, ["rank", "sum", "join"]),
-                              (8193, 99, ["count", "scatter", "sum", "join"]),
+    for n, vocab, kernels in [(7, 99, ["direct"]), (2048, 99, ["direct"]), (2049, 99, ["rank", "sum", "join"]),
+                              (4096, 99, ["rank", "sum", "join"]), (4097, 99, ["count", "scatter", "sum", "join"]),
                               (8193, 512, ["count", "scatter"] * 2 + ["sum", "join"]),
                               (8193, 511, ["count", "scatter", "sum", "join"]),
                               (8193, 1 << 18, ["count", "scatter"] * 3 + ["sum", "join"])]:
