@@ -150,9 +150,14 @@ lc_status launched(const char* func, hipError_t e) {
   return e == hipSuccess ? LC_OK : fail(LC_ERR_HIP, "%s: %s", func, hipGetErrorString(e));
 }
 
-Rows rows_of(const lc_matrix* m) { return m ? Rows{addr(m->data), m->stride} : Rows{0, 0}; }
+// A single row's strides are the caller's to leave unset; the kernels reckon
+// with those of rows that follow it closely.
+Rows rows_of(const lc_matrix* m) { return m ? Rows{addr(m->data), m->rows > 1 ? m->stride : m->cols} : Rows{0, 0}; }
 Kept kept_of(const lc_saved_act* s) {
-  return s ? Kept{addr(s->codes), addr(s->scales), s->code_stride, s->scale_stride} : Kept{0, 0, 0, 0};
+  if (!s) return Kept{0, 0, 0, 0};
+  const bool many = s->rows > 1;
+  return Kept{addr(s->codes), addr(s->scales), many ? s->code_stride : s->cols,
+              many ? s->scale_stride : (s->cols + kActBlock - 1) / kActBlock};
 }
 
 lc_status check_norm(const lc_norm_params* p) {

@@ -594,6 +594,25 @@ def test_linear_wgrad(rows, n, k, dtype, out, affine):
             assert torch.equal(again.view, dw.view)
 
 
+@pytest.mark.parametrize("n,k", [(40, 70), (264, 272), (4096, 4352)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("strides", [0, 1, 2 ** 60])
+def test_a_single_rows_strides_are_not_looked_at(n, k, dtype, strides):
+    dt, code, _ = DT[dtype]
+    dy = torch.randn(1, n, generator=gen(n), device="cuda").to(dt)
+    kept = kept_normal(1, k, 3)
+    act = LC.lc_saved_act(kept.codes.addr, kept.scales.addr, 1, k, strides, strides)
+    one = LC.lc_matrix(dy.data_ptr(), 1, n, strides, code, 0)
+    dw, back, db = torch.empty(n, k, device="cuda"), torch.empty(1, k, device="cuda"), torch.empty(n, device="cuda")
+    need = LC.lc_linear_wgrad_workspace(1, n, k)
+    buf, ws, _ = space(need)
+    LC.lc_linear_wgrad(one, act, LC.matrix(dw.data_ptr(), n, k, LC.LC_DT_F32), ws, need, dbias=db.data_ptr(), stream=stream())
+    assert torch.equal(dw, (dy.double().t() @ kept.values()).float())  # one product each: rounded once
+    assert torch.equal(db, dy[0].float())
+    LC.lc_act_load(act, LC.lc_matrix(back.data_ptr(), 1, k, strides, LC.LC_DT_F32, 0), stream())
+    assert torch.equal(back.double(), kept.values())
+
+
 def test_wgrad_takes_all_bits_of_a_32_bit_gradient():
     """One token and a kept 1.0: the gradient is dy itself, to the last bit, from the largest to the smallest normal."""
     g = gen(9)
