@@ -63,8 +63,10 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_fwd_kernel(NormFwd a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const uint32_t g = i * TPR + t;
-      r[i] = load8_row<DT, kStreams<DT>>(a.x.data + row * a.x.stride * kEsz<DT>, g, a.dim, on ? in_group(a.dim, g) : 0);
+      r[i] = load8_row<DT, kStreams<DT>>(a.x.data + row * a.x.stride * kEsz<DT>, g, on ? in_group(a.dim, g) : 0);
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) trim8_row<DT>(r[i], a.dim, in_group(a.dim, i * TPR + t));
     float v[8];
     float mean = 0;
     if constexpr (LAYER) {
@@ -204,15 +206,21 @@ template <int DT, bool KEPT, bool ANY>
 __device__ __forceinline__ NormIn<DT, KEPT> load_normed(const NormBwd& a, uint64_t row, uint32_t g, int n) {
   NormIn<DT, KEPT> in;
   const uint64_t dy = a.dy.data + row * a.dy.stride * kEsz<DT>;
-  in.dy = ANY ? load8_raw<DT>(dy + 8ull * g * kEsz<DT>, n) : load8_row<DT, kStreams<DT>>(dy, g, a.dim, n);
+  in.dy = ANY ? load8_raw<DT>(dy + 8ull * g * kEsz<DT>, n) : load8_row<DT, kStreams<DT>>(dy, g, n);
   if constexpr (KEPT) {
     in.code = n > 0 ? load_kept_code(a.kept, row, g) : 0;
     in.codes = ANY ? load_kept8(a.kept, row, g, n) : load_codes8_row(a.kept.codes + row * a.kept.code_stride, g, n);
   } else {
     const uint64_t x = a.x.data + row * a.x.stride * kEsz<DT>;
-    in.x = ANY ? load8_raw<DT>(x + 8ull * g * kEsz<DT>, n) : load8_row<DT, kStreams<DT>>(x, g, a.dim, n);
+    in.x = ANY ? load8_raw<DT>(x + 8ull * g * kEsz<DT>, n) : load8_row<DT, kStreams<DT>>(x, g, n);
   }
   return in;
+}
+template <int DT, bool KEPT>
+__device__ __forceinline__ void trim_normed(NormIn<DT, KEPT>& in, uint32_t dim, int n) {
+  trim8_row<DT>(in.dy, dim, n);
+  if constexpr (KEPT) in.codes = trim_codes8_row(in.codes, n);
+  else trim8_row<DT>(in.x, dim, n);
 }
 // dy and n of the group; zeros behind the row's end.
 template <int DT, bool KEPT>
@@ -259,6 +267,8 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_bwd_kernel(NormBwd a, 
       const uint32_t g = i * TPR + t;
       cur[i] = load_normed<DT, KEPT, false>(a, row, g, on ? in_group(a.dim, g) : 0);
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) trim_normed<DT, KEPT>(cur[i], a.dim, in_group(a.dim, i * TPR + t));
     float c1 = 0, c2 = 0;
     float d[8], n[8];
 #pragma unroll

@@ -111,21 +111,9 @@ __device__ __forceinline__ Raw8<DT> load8_raw(uint64_t p, int n) {
   }
   return r;
 }
-// Group g of a row of dim >= 8 elements at `row`, zeros behind the row's end.
-// The last group of a row that is no multiple of eight is read from eight
-// elements before the end and moved down: one load, where an element at a time
-// takes seven and the registers for them.  n: the group's elements, at most 0
-// for a group that is not there.
-template <int DT, bool NT = false>
-__device__ __forceinline__ Raw8<DT> load8_row(uint64_t row, uint32_t g, uint32_t dim, int n) {
-  Raw8<DT> r;
-  for (auto& q : r.v) q = u32x4{0, 0, 0, 0};
-  if (dim % 8 == 0) {  // the same for the whole grid
-    if (n > 0) r = load8_raw<DT, NT>(row + 8ull * kEsz<DT> * g);
-    return r;
-  }
-  const uint32_t s = n > 0 && n < 8 ? 8 - n : 0;
-  if (n > 0) r = load8_raw<DT, NT>(row + (8ull * g - s) * kEsz<DT>);
+// The eight elements moved down by s, zeros behind them.
+template <int DT>
+__device__ __forceinline__ void move_down8(Raw8<DT>& r, uint32_t s) {
   if constexpr (DT == kBf16) {
     u32x4& v = r.v[0];
     if (s & 4) v = u32x4{v[2], v[3], 0, 0};
@@ -146,7 +134,24 @@ __device__ __forceinline__ Raw8<DT> load8_row(uint64_t row, uint32_t g, uint32_t
       b = u32x4{b[1], b[2], b[3], 0};
     }
   }
+}
+// Group g of a row of dim >= 8 elements at `row`, in two steps.  The last group
+// of a row that is no multiple of eight is read from eight elements before the
+// end and moved down by trim8_row: one load, where an element at a time takes
+// seven and the registers for them.  A thread moves its groups when all their
+// loads are under way, for that is where it waits for them.  n: the group's
+// elements, at most 0 for a group that is not there, which reads zeros.
+__device__ __forceinline__ uint32_t missing8(int n) { return n > 0 && n < 8 ? 8 - n : 0; }
+template <int DT, bool NT = false>
+__device__ __forceinline__ Raw8<DT> load8_row(uint64_t row, uint32_t g, int n) {
+  Raw8<DT> r;
+  for (auto& q : r.v) q = u32x4{0, 0, 0, 0};
+  if (n > 0) r = load8_raw<DT, NT>(row + (8ull * g - missing8(n)) * kEsz<DT>);
   return r;
+}
+template <int DT>
+__device__ __forceinline__ void trim8_row(Raw8<DT>& r, uint32_t dim, int n) {
+  if (dim % 8) move_down8<DT>(r, missing8(n));  // the same for the whole grid
 }
 template <int DT>
 __device__ __forceinline__ void unpack8(const Raw8<DT>& r, float (&f)[8]) {
@@ -305,12 +310,14 @@ __device__ __forceinline__ void store_codes8(uint64_t p, u32x2 b, int n) {
   for (int i = 0; i < 7; ++i)
     if (i < n) *(g_u8*)(p + i) = static_cast<uint8_t>(b[i / 4] >> (8 * (i & 3)));
 }
-// The same of a row of dim >= 8 codes at `row`, as load8_row.
+// The same of a row of dim >= 8 codes at `row`, as load8_row and trim8_row.
 __device__ __forceinline__ u32x2 load_codes8_row(uint64_t row, uint32_t g, int n) {
-  const uint32_t s = n > 0 && n < 8 ? 8 - n : 0;
   u32x2 r = {0, 0};
-  if (n > 0) r = *(gc_u32x2_any1*)(row + 8ull * g - s);
-  return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, r) >> (8 * s));
+  if (n > 0) r = *(gc_u32x2_any1*)(row + 8ull * g - missing8(n));
+  return r;
+}
+__device__ __forceinline__ u32x2 trim_codes8_row(u32x2 b, int n) {
+  return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, b) >> (8 * missing8(n)));
 }
 // Group g of row r of a kept activation, and its block's scale.
 __device__ __forceinline__ u32x2 load_kept8(const Kept& k, uint64_t row, uint32_t g, int n) {

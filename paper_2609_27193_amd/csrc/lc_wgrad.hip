@@ -14,6 +14,8 @@
 // Both operands lie with the tokens, over which the product sums, as rows: a
 // tile goes to LDS as it lies and the transposing LDS reads give each lane the
 // eight tokens of its column that the matrix instruction takes.
+#include <algorithm>
+
 #include "lc_ops_device.h"
 
 namespace lc {
@@ -56,29 +58,19 @@ __device__ __forceinline__ Codes16 load_codes16(const Kept& x, uint64_t row, uin
   return r;
 }
 
-// The same of a row of `cols` >= 16 codes: the last group is read from sixteen
-// before the end and moved down.
-__device__ __forceinline__ Codes16 load_codes16_row(const Kept& x, uint64_t row, uint32_t col, int n) {
-  Codes16 r;
-  r.codes = u32x4{0, 0, 0, 0};
-  r.code = 127;
-  if (n > 0) {
-    const uint32_t s = n < 16 ? 16 - n : 0;
-    r.codes = *(gc_u32x4_any1*)(x.codes + row * x.code_stride + col - s);
-    r.code = *(gc_u8*)(x.scales + row * x.scale_stride + col / kActBlock);
-    uint64_t lo = r.codes[0] | static_cast<uint64_t>(r.codes[1]) << 32, hi = r.codes[2] | static_cast<uint64_t>(r.codes[3]) << 32;
-    if (s & 8) {
-      lo = hi;
-      hi = 0;
-    }
-    const uint32_t bits = s % 8 * 8;
-    if (bits) {
-      lo = lo >> bits | hi << (64 - bits);
-      hi >>= bits;
-    }
-    r.codes = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
+// Sixteen codes moved down by s, zeros behind them.
+__device__ __forceinline__ void move_down16(u32x4& v, uint32_t s) {
+  uint64_t lo = v[0] | static_cast<uint64_t>(v[1]) << 32, hi = v[2] | static_cast<uint64_t>(v[3]) << 32;
+  if (s & 8) {
+    lo = hi;
+    hi = 0;
   }
-  return r;
+  const uint32_t bits = s % 8 * 8;
+  if (bits) {
+    lo = lo >> bits | hi << (64 - bits);
+    hi >>= bits;
+  }
+  v = u32x4{static_cast<uint32_t>(lo), static_cast<uint32_t>(lo >> 32), static_cast<uint32_t>(hi), static_cast<uint32_t>(hi >> 32)};
 }
 
 // Four bytes to four bf16, times 2^(code - 127); exact, and code 255 gives NaN.
@@ -149,7 +141,10 @@ __device__ __forceinline__ void wgrad_place(const WgradTiles& s, uint32_t tile, 
   k0 = k * s.tile;
 }
 // Item b of the grid.  The whole tiles run first, then the parts; each in
-// contiguous eighths for the XCDs.
+// contiguous eighths for the XCDs.  A part's tiles of 256 follow each other, so
+// that an XCD's blocks read the same tokens (16384 tokens x 1024 x 1024: 52.7 us
+// of kernel; a tile's parts after each other 55.5), of 128 a tile's parts (2048 x
+// 1024 x 1024 fp32: 29 us, the other way 34).
 __device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t rows, uint32_t b) {
   WgradItem w;
   w.whole = b < s.full;
@@ -159,11 +154,10 @@ __device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t ro
     w.t_begin = 0;
     w.t_end = rows;
   } else {
-    const uint32_t parts = (s.tiles - s.full) * s.splits;
+    const uint32_t cut = s.tiles - s.full, parts = cut * s.splits;
     const uint32_t i = s.full + parts <= gridDim.x ? remap_xcd(b - s.full, parts) : b - s.full;
-    const uint32_t tile = i / s.splits;
-    w.tile = s.full + tile;
-    w.split = i - tile * s.splits;
+    w.split = s.big ? i / cut : i % s.splits;
+    w.tile = s.full + (s.big ? i % cut : i / s.splits);
     w.t_begin = w.split * s.per_split;
     w.t_end = w.t_begin + s.per_split < rows ? w.t_begin + s.per_split : rows;
   }
@@ -181,12 +175,12 @@ struct WgradCols {
   int in;  // of the eight, that exist
   float scale[8], shift[8];
 };
-__device__ __forceinline__ WgradCols wgrad_cols(const Wgrad& a, uint32_t k) {
+__device__ __forceinline__ WgradCols wgrad_cols(const Wgrad& a, uint32_t k, bool whole) {
   WgradCols c;
   c.k = k;
   c.in = static_cast<int>(a.k) - static_cast<int>(k);
-  load_params8(a.col_scale, a.param_dtype, k / 8, c.in, 1.0f, c.scale);
-  load_params8(a.col_shift, a.param_dtype, k / 8, c.in, 0.0f, c.shift);
+  load_params8(whole ? a.col_scale : 0, a.param_dtype, k / 8, c.in, 1.0f, c.scale);
+  load_params8(whole ? a.col_shift : 0, a.param_dtype, k / 8, c.in, 0.0f, c.shift);
   return c;
 }
 // The whole sums of row n at these columns, into dW.
@@ -229,8 +223,18 @@ __device__ __forceinline__ void wgrad_write_bias(const Wgrad& a, uint64_t n, flo
   store_param(a.dbias, n, a.dw_dtype, sum);
 }
 
-// NARROW: fewer than 8 columns of n or 16 of k, read an element at a time.
-template <int DT, bool SUMS, bool NARROW>
+// The next `rows` of an operand, 32 at most: an offset past the last one's end
+// (and what may be read behind it) reads zeros; past another's end it reads the
+// row behind it, whose columns are not stored.  The hardware looks at four bytes
+// at a time: those that the end divides read zeros, too.
+__device__ __forceinline__ tile_t step_tile(uint64_t base, int rows, uint32_t pitch, uint32_t width) {
+  const uint32_t bytes = static_cast<uint32_t>(rows - 1) * pitch + width;
+  return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0u);
+}
+
+// ANY: rows of any length and stride, read an element at a time where they end;
+// else of 8 columns of n and 16 of k at least, as far as 32-bit offsets reach.
+template <int DT, bool SUMS, bool ANY>
 __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles s) {
   constexpr int P = kPlanes<DT>;
   constexpr uint32_t kIn = 2 * (P + 1) * kStep * kPitch * 2, kOutBytes = 4 * 64 * kOut * 4;
@@ -249,26 +253,50 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
     const int d_in = static_cast<int>(a.n) - static_cast<int>(n0 + 8 * dc);
     const uint32_t xc = tid % 8, xr = tid / 8;
     const int x_in = static_cast<int>(a.k) - static_cast<int>(k0 + 16 * xc);
+    // a group that reaches past its row's end is read from before it, and moved
+    // down on its way to LDS; one that lies past it reads what no one stores
+    const uint32_t d_at = ANY || n0 + 8 * dc + 8 <= a.n ? n0 + 8 * dc : a.n - 8;
+    const uint32_t x_at = ANY || k0 + 16 * xc + 16 <= a.k ? k0 + 16 * xc : a.k - 16;
+    const uint32_t d_move = n0 + 8 * dc - d_at, x_move = k0 + 16 * xc - x_at;
+    const uint32_t s_at = x_in > 0 ? (k0 + 16 * xc) / kActBlock : 0;
+    const uint32_t d_pitch = static_cast<uint32_t>(a.dy.stride * kEsz<DT>), x_pitch = static_cast<uint32_t>(a.x.code_stride);
+    const uint32_t s_pitch = static_cast<uint32_t>(a.x.scale_stride);
+    const uint32_t d_from = dr * d_pitch + d_at * kEsz<DT>, x_from = xr * x_pitch + x_at, s_from = xr * s_pitch + s_at;
     struct Stage {
       Raw8<DT> d[2];
       Codes16 c;
     };
     float sum[8] = {};
+    // Step t, zeros for the rows behind the last: loads without a condition, or
+    // the compiler waits for the newest of them where it needs the oldest.
     auto load = [&](Stage& g, uint64_t t) {
+      if constexpr (ANY) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint64_t r = t + dr + 16 * i;
-        const uint64_t dy = a.dy.data + r * a.dy.stride * kEsz<DT>;
-        const int in = r < t_end ? d_in : 0;
-        if constexpr (NARROW) g.d[i] = load8_raw<DT>(dy + (n0 + 8ull * dc) * kEsz<DT>, in);
-        else g.d[i] = load8_row<DT>(dy, n0 / 8 + dc, a.n, in);
+        for (int i = 0; i < 2; ++i) {
+          const uint64_t r = t + dr + 16 * i;
+          g.d[i] = load8_raw<DT>(a.dy.data + (r * a.dy.stride + d_at) * kEsz<DT>, r < t_end ? d_in : 0);
+        }
+        g.c = load_codes16(a.x, t + xr, x_at, t + xr < t_end ? x_in : 0);
+      } else {
+        const int rows = t + kStep <= t_end ? static_cast<int>(kStep) : t < t_end ? static_cast<int>(t_end - t) : 0;
+        const tile_t td = step_tile(a.dy.data + t * a.dy.stride * kEsz<DT>, rows, d_pitch, a.n * kEsz<DT>);
+        const tile_t tx = step_tile(a.x.codes + t * a.x.code_stride, rows, x_pitch, a.k);
+        const tile_t ts = step_tile(a.x.scales + t * a.x.scale_stride, rows, s_pitch, (a.k + kActBlock - 1) / kActBlock);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int q = 0; q < static_cast<int>(kEsz<DT>) / 2; ++q)
+            g.d[i].v[q] = __builtin_amdgcn_raw_buffer_load_b128(td, d_from + 16 * q, i * 16 * d_pitch, 0);
+        g.c.codes = __builtin_amdgcn_raw_buffer_load_b128(tx, x_from, 0, 0);
+        g.c.code = __builtin_amdgcn_raw_buffer_load_b8(ts, s_from, 0, 0);
       }
-      const uint64_t r = t + xr;
-      const int in = r < t_end ? x_in : 0;
-      if constexpr (NARROW) g.c = load_codes16(a.x, r, k0 + 16 * xc, in);
-      else g.c = load_codes16_row(a.x, r, k0 + 16 * xc, in);
     };
-    auto store = [&](const Stage& g, int buf) {
+    auto store = [&](Stage& g, int buf) {
+      if constexpr (!ANY) {
+        if (a.n % 8)
+          for (auto& d : g.d) move_down8<DT>(d, d_move);
+        if (a.k % 16) move_down16(g.c.codes, x_move);
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t at = (dr + 16 * i) * kPitch + 8 * dc;
@@ -309,18 +337,7 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
     const uint32_t wk = wave % 2 * 64, wn = wave / 2 * 64;
-    // the next step is on its way while one multiplies (two ahead: registers,
-    // and half the waves; 8192 x 4096 x 4096 fp32 990 us, 1078 with two)
-    Stage g;
-    if (t_begin < t_end) {
-      load(g, t_begin);
-      store(g, 0);
-    }
-    __syncthreads();
-    int buf = 0;
-    for (uint64_t t = t_begin; t < t_end; t += kStep) {
-      const bool more = t + kStep < t_end;
-      if (more) load(g, t + kStep);
+    auto multiply = [&](int buf) {
       bf16x8 xf[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) xf[i] = read_cols(xs[buf], wk + 16 * i, lane);
@@ -333,9 +350,39 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
           for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[i], df, acc[i][j], 0, 0, 0);
         }
       }
-      if (more) store(g, buf ^ 1);
+    };
+    // The next kAhead steps' loads are on their way while one multiplies (of
+    // three parts a step, one: 8192 x 4096 x 4096 fp32 850 us, 900 with two).
+    constexpr int kAhead = ANY || P > 1 ? 1 : 3;
+    Stage g[kAhead];
+    if (t_end <= t_begin + kStep) {  // one step at most: nothing else is loaded
+      if (t_begin < t_end) {
+        load(g[0], t_begin);
+        store(g[0], 0);
+        __syncthreads();
+        multiply(0);
+      }
       __syncthreads();
-      buf ^= 1;
+    } else {
+#pragma unroll
+      for (int d = 0; d < kAhead; ++d) load(g[d], t_begin + d * kStep);
+      store(g[0], 0);
+      load(g[0], t_begin + kAhead * kStep);
+      __syncthreads();
+      int buf = 0;
+      for (uint64_t t0 = t_begin; t0 < t_end; t0 += kAhead * kStep) {
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d) {
+          const uint64_t t = t0 + d * kStep;
+          if (t >= t_end) break;
+          multiply(buf);
+          Stage& next = g[(d + 1) % kAhead];
+          if (t + kStep < t_end) store(next, buf ^ 1);
+          load(next, t + (1 + kAhead) * kStep);
+          __syncthreads();
+          buf ^= 1;
+        }
+      }
     }
 
     if constexpr (SUMS) {
@@ -363,7 +410,7 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<f32x4*>(mine + (16 * j + lane % 16) * kOut + 16 * i + lane / 16 * 4) = acc[i][j];
-    const WgradCols cols = wgrad_cols(a, k0 + wk + lane % 8 * 8);
+    const WgradCols cols = wgrad_cols(a, k0 + wk + lane % 8 * 8, w.whole);
 #pragma unroll 2
     for (uint32_t q = lane / 8; q < 64; q += 8) {
       float v[8];
@@ -408,15 +455,6 @@ struct BigStage {
   uint32_t scale[2];
 };
 
-// The next `rows` of an operand, 32 at most: an offset past the last one's end
-// (and what may be read behind it) reads zeros; past another's end it reads the
-// row behind it, whose columns are not stored.  The hardware looks at four bytes
-// at a time: those that the end divides read zeros, too.
-__device__ __forceinline__ tile_t step_tile(uint64_t base, int rows, uint32_t pitch, uint32_t width) {
-  const uint32_t bytes = static_cast<uint32_t>(rows - 1) * pitch + width;
-  return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0u);
-}
-
 __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTiles s) {
   // dY, dY, X, X; at the end the waves' 32 rows of 128
   __shared__ __align__(256) uint8_t lds[4 * 32 * kBigOut * 4 > 4 * kBigBuf ? 4 * 32 * kBigOut * 4 : 4 * kBigBuf];
@@ -440,6 +478,8 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
     x_at[i] = base + 2 * kBigBuf + at + wk * 2;
     dy_at[i] = base + at + wn * 2;
   }
+  // what the tile's rows and columns have besides their products
+  __shared__ __align__(16) float row_sum[kBigTile], row_last[kBigTile], col_scale[kBigTile], col_shift[kBigTile], col_last[kBigTile];
   const uint32_t items = s.full + (s.tiles - s.full) * s.splits;
   for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
     const WgradItem w = wgrad_item(s, a.rows, b);
@@ -549,6 +589,23 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
     BigStage g0, g1;  // the odd steps on their way, and the even ones
     load(g1);
     load(g0);
+    // a wave for each, so that their loads do not wait for one another
+    for (uint32_t i = lane; i < kBigTile; i += 64) {
+      const uint64_t n = n0 + i, k = k0 + i;
+      const bool on_n = n < a.n, on_k = k < a.k;
+      if (wave == 0) {
+        col_scale[i] = a.col_scale && on_k ? load_param(a.col_scale, k, a.param_dtype) : 1.0f;
+      } else if (wave == 1) {
+        col_shift[i] = a.col_shift && on_k ? load_param(a.col_shift, k, a.param_dtype) : 0.0f;
+      } else if (wave == 2) {
+        row_sum[i] = a.col_shift && on_n ? s.sums[n] : 0.0f;
+        if (last) row_last[i] = on_n ? load1<kBf16>(a.dy.data + ((a.rows - 1) * a.dy.stride + n) * 2) : 0.0f;
+      } else if (last) {
+        const uint32_t code = on_k ? *(gc_u8*)(a.x.codes + (a.rows - 1) * a.x.code_stride + k) : 0;
+        const float scale = on_k ? act_scale(load_kept_code(a.x, a.rows - 1, k / 8)) : 0.0f;
+        col_last[i] = __builtin_amdgcn_cvt_f32_fp8(code, 0) * scale;
+      }
+    }
 #pragma unroll
     for (int p = 0; p < 8; ++p) store(g1, 0, p);
     load(g1);
@@ -564,10 +621,17 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
     // out of the registers through LDS, 32 rows of dW a wave at a time, so
     // that a lane has eight neighbours of k (every other eight: see above)
     float* const mine = reinterpret_cast<float*>(lds) + wave * 32 * kBigOut;
-    const WgradCols cols = wgrad_cols(a, k0 + lane % 16 * 16 + wk / 16);
-    float x_last[8] = {};
-    if (last && cols.in > 0)
-      act_decode8(load_kept8(a.x, a.rows - 1, cols.k / 8, cols.in), act_scale(load_kept_code(a.x, a.rows - 1, cols.k / 8)), x_last);
+    const uint32_t lk = lane % 16 * 16 + wk / 16;
+    WgradCols cols;
+    cols.k = k0 + lk;
+    cols.in = static_cast<int>(a.k) - static_cast<int>(cols.k);
+    float x_last[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      cols.scale[e] = col_scale[lk + e];
+      cols.shift[e] = col_shift[lk + e];
+      x_last[e] = last ? col_last[lk + e] : 0.0f;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -577,50 +641,70 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
           const f32x4 v = {acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]};
           *reinterpret_cast<f32x4*>(mine + lane % 32 * kBigOut + 32 * i + 8 * r + lane / 32 * 4) = v;
         }
-#pragma unroll 1
+#pragma unroll 4
       for (uint32_t q = lane / 16; q < 32; q += 4) {
         const uint32_t ln = wn + 32 * j + q;
-        const bool on = n0 + ln < a.n;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = mine[q * kBigOut + lane % 16 * 8 + e];
-        if (last && on) {
-          const float d = load1<kBf16>(a.dy.data + ((a.rows - 1) * a.dy.stride + n0 + ln) * 2);
+        if (last) {
+          const float d = row_last[ln];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(d, x_last[e], v[e]);
         }
-        wgrad_out8(a, s, w, cols, ln, a.col_shift && on ? s.sums[n0 + ln] : 0.0f, v);
+        wgrad_out8(a, s, w, cols, ln, row_sum[ln], v);
       }
     }
     __syncthreads();
   }
 }
 
-// The parts' sums, in order, with the columns' scale and shift.
+// The parts' sums with the columns' scale and shift.  SLICES threads share eight
+// columns of a row of dW: each adds every SLICES-th part, then the first adds the
+// others' sums, in a fixed order.
+template <uint32_t SLICES>
 __global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTiles s) {
-  const uint32_t per_row = s.tile / 8, blocks = s.tile * per_row / kThreads;  // of a tile
+  constexpr uint32_t G = kThreads / SLICES;  // groups of eight columns a block
+  __shared__ float sums[SLICES][9][G];
+  const uint32_t per_row = s.tile / 8, blocks = s.tile * per_row / G;  // of a tile
+  const uint32_t own = threadIdx.x % G, slice = threadIdx.x / G;
   for (uint32_t it = blockIdx.x; it < (s.tiles - s.full) * blocks; it += gridDim.x) {
-    const uint32_t tile = s.full + it / blocks, in_t = it % blocks * kThreads + threadIdx.x;
+    const uint32_t tile = s.full + it / blocks, in_t = it % blocks * G + own;
     const uint32_t ln = in_t / per_row, lk = in_t % per_row * 8;
     uint32_t n0, k0;
     wgrad_place(s, tile, n0, k0);
     const uint64_t n = n0 + ln;
     const int in = static_cast<int>(a.k) - static_cast<int>(k0 + lk);
-    if (n >= a.n || in <= 0) continue;
-    float v[8] = {}, f[8], sum = 0;
-#pragma unroll 8
-    for (uint32_t p = 0; p < s.splits; ++p) {  // a part is a whole tile, also where dW ends
-      unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, tile, p, ln) + lk)), f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += f[e];
-    }
+    const bool on = n < a.n && in > 0;
     const bool bias = a.dbias && !s.big && k0 + lk == 0;
-    if (a.col_shift || bias) {
-#pragma unroll 8
-      for (uint32_t p = 0; p < s.sum_parts; ++p) sum += s.sums[p * static_cast<uint64_t>(a.n) + n];
+    float v[8] = {}, f[8], sum = 0;
+    if (on) {
+#pragma unroll (SLICES > 1 ? 4 : 8)
+      for (uint32_t p = slice; p < s.splits; p += SLICES) {  // a part is a whole tile, also where dW ends
+        unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, tile, p, ln) + lk)), f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += f[e];
+      }
+      if (a.col_shift || bias) {
+#pragma unroll 4
+        for (uint32_t p = slice; p < s.sum_parts; p += SLICES) sum += s.sums[p * static_cast<uint64_t>(a.n) + n];
+      }
     }
-    if (bias) wgrad_write_bias(a, n, sum);
-    wgrad_write8(a, n, wgrad_cols(a, k0 + lk), sum, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[slice][e][own] = v[e];
+    sums[slice][8][own] = sum;
+    __syncthreads();
+    if (slice == 0 && on) {
+#pragma unroll
+      for (uint32_t q = 1; q < SLICES; ++q) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += sums[q][e][own];
+        sum += sums[q][8][own];
+      }
+      if (bias) wgrad_write_bias(a, n, sum);
+      wgrad_write8(a, n, wgrad_cols(a, k0 + lk, true), sum, v);
+    }
+    __syncthreads();
   }
 }
 
@@ -666,13 +750,11 @@ __global__ __launch_bounds__(64) void wgrad_sums_join_kernel(Wgrad a, const floa
 
 // The cut.  More parts shorten what a block takes over the tokens and cost
 // their sums' way through memory.  The figures are measured (us): what a block
-// of 256 columns takes beside its steps 14 (ragged 19), a step of 32 tokens 0.6,
-// with every CU at work 0.85; of 128 columns 7, 0.65 and, two a CU, 1.0; a part's
-// sums there and back 0.105 and 0.018, the join's launch 4 and 0.12 a part.  By
-// it (measured) 4096 tokens x 512 x 512 take 23 (23) in tiles of 128 and 31 (30)
-// of 256, 16000 x 1500 x 2100 147 (134) of 256, and 64 x 14000 x 2000 26 (24) and
-// 31 (34).
-WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big, double* best_us) {
+// of 256 columns takes beside its steps 12 (ragged 17), a step of 32 tokens 0.6,
+// with every CU at work 0.85; of 128 columns 9 (behind another 4), 0.53 and, two
+// a CU, 0.77, of an fp32 dY 1.2 and 1.65; a part's sums there and back 0.105 and
+// 0.018, the join's launch 4 and 0.02 a part.
+WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big, bool wide, double* best_us) {
   WgradTiles s{};
   s.big = big;
   s.ragged = n % 8 != 0 || k % 16 != 0;
@@ -682,17 +764,19 @@ WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big, double* 
   s.tiles = s.tn * s.tk;
   const uint32_t at_once = big ? 256 : 512, rest = s.tiles % at_once;
   const uint64_t rounds = s.tiles / at_once, steps = (rows + kStep - 1) / kStep;
-  const double block_us = !big ? 7.0 : s.ragged ? 19.0 : 14.0, part_us = big ? 0.105 : 0.018;
-  const double whole_us = rounds * (steps * (big ? 0.85 : 1.0) + (big ? block_us : 3.0)) + (big ? 0.0 : block_us);
+  const double block_us = !big ? 9.0 : s.ragged ? 17.0 : 12.0, next_us = big ? block_us : 4.0, part_us = big ? 0.105 : 0.018;
+  const double one_us = big ? 0.6 : wide ? 1.2 : 0.53, all_us = big ? 0.85 : wide ? 1.65 : 0.77;
+  const double whole_us = rounds ? rounds * steps * all_us + block_us + (rounds - 1) * next_us : 0.0;
   uint64_t best = 1;
   *best_us = 1e30;
   // the small kernel splits every tile or none: it takes a whole tile's column
   // sums along, and the parts of a column of tiles have to be alike
-  for (uint64_t splits = 1; splits == 1 || (rest && (big || !rounds) && splits <= at_once / rest && splits <= steps); ++splits) {
+  for (uint64_t splits = 1; splits == 1 || (rest && (big || !rounds) && splits <= at_once / rest && splits <= steps);
+       splits += 1 + splits / 16) {
     const double blocks = static_cast<double>(splits) * rest;
-    const double step_us = big ? 0.6 + 0.25 * blocks / 256 : 0.65 + (blocks > 256 ? 0.35 * (blocks - 256) / 256 : 0.0);
-    const double us = whole_us + (rest ? (steps + splits - 1) / splits * step_us + (big ? block_us : rounds ? 3.0 : 0.0) : 0.0) +
-                      (splits > 1 ? blocks * part_us + 4.0 + 0.12 * splits : 0.0);
+    const double fill = big ? blocks / 256 : blocks > 256 ? (blocks - 256) / 256 : 0.0;  // of the CUs; of their second places
+    const double us = whole_us + (rest ? (steps + splits - 1) / splits * (one_us + (all_us - one_us) * fill) + (rounds ? next_us : block_us) : 0.0) +
+                      (splits > 1 ? blocks * part_us + 4.0 + 0.02 * splits : 0.0);
     if (us < *best_us) {
       *best_us = us;
       best = splits;
@@ -705,11 +789,13 @@ WgradTiles wgrad_tiles(uint64_t rows, uint64_t n, uint64_t k, bool big, double* 
   return s;
 }
 
-// The 256-column kernel takes a bf16 dY, as far as its loads' 32-bit offsets
-// reach.
+// Whether 32 rows lie within 32-bit offsets.
+bool wgrad_in_reach(const Wgrad& a) {
+  return a.dy.stride < (1u << 24) && a.x.code_stride < (1u << 26) && a.x.scale_stride < (1u << 26);
+}
+// The 256-column kernel takes a bf16 dY.
 bool wgrad_may_be_big(const Wgrad& a) {
-  return a.dtype == kBf16 && a.n >= 8 && a.k >= 16 && a.dy.stride < (1u << 25) && a.x.code_stride < (1u << 26) &&
-         a.x.scale_stride < (1u << 26) && a.rows < (1u << 30);
+  return a.dtype == kBf16 && a.n >= 8 && a.k >= 16 && wgrad_in_reach(a) && a.rows < (1u << 30);
 }
 
 uint64_t wgrad_part_bytes(const WgradTiles& s) {
@@ -717,9 +803,15 @@ uint64_t wgrad_part_bytes(const WgradTiles& s) {
 }
 template <int DT>
 hipError_t wgrad_of(const Wgrad& a, const WgradTiles& s, uint32_t grid, bool sums, hipStream_t st) {
-  if (a.n < 8 || a.k < 16)
+  if (a.n < 8 || a.k < 16 || !wgrad_in_reach(a))
     return launch_op(sums ? wgrad_kernel<DT, true, true> : wgrad_kernel<DT, false, true>, grid, kThreads, st, a, s);
   return launch_op(sums ? wgrad_kernel<DT, true, false> : wgrad_kernel<DT, false, false>, grid, kThreads, st, a, s);
+}
+constexpr uint64_t kJoinAlone = 98304;  // groups of eight columns from which a thread adds all parts of one
+template <uint32_t SLICES>
+hipError_t wgrad_join(const Wgrad& a, const WgradTiles& s, hipStream_t st) {
+  const uint32_t blocks = (s.tiles - s.full) * (s.tile * s.tile / 8 * SLICES / kThreads);
+  return launch_op(wgrad_join_kernel<SLICES>, grid_for(blocks, kThreads), kThreads, st, a, s);
 }
 uint64_t wgrad_space(const WgradTiles& s, uint64_t n) {
   return wgrad_part_bytes(s) + (s.sum_parts + (s.big ? kSumParts : 0)) * n * 4;
@@ -730,16 +822,17 @@ uint64_t wgrad_space(const WgradTiles& s, uint64_t n) {
 uint64_t wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k) {
   // which tiles a call takes goes by its types and alignment, too
   double us;
-  const uint64_t big = wgrad_space(wgrad_tiles(rows, n, k, true, &us), n);
-  const uint64_t small = wgrad_space(wgrad_tiles(rows, n, k, false, &us), n);
-  return big > small ? big : small;
+  const uint64_t big = wgrad_space(wgrad_tiles(rows, n, k, true, false, &us), n);
+  const uint64_t narrow = wgrad_space(wgrad_tiles(rows, n, k, false, false, &us), n);
+  const uint64_t wide = wgrad_space(wgrad_tiles(rows, n, k, false, true, &us), n);
+  return std::max(big, std::max(narrow, wide));
 }
 
 hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
   double us, big_us;
-  WgradTiles s = wgrad_tiles(a.rows, a.n, a.k, false, &us);
+  WgradTiles s = wgrad_tiles(a.rows, a.n, a.k, false, a.dtype == kF32, &us);
   if (wgrad_may_be_big(a)) {
-    const WgradTiles big = wgrad_tiles(a.rows, a.n, a.k, true, &big_us);
+    const WgradTiles big = wgrad_tiles(a.rows, a.n, a.k, true, false, &big_us);
     if (big_us <= us) s = big;
   }
   s.part = reinterpret_cast<float*>(a.ws);
@@ -760,8 +853,10 @@ hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
     e = a.dtype == kBf16 ? wgrad_of<kBf16>(a, s, grid, sums, st) : wgrad_of<kF32>(a, s, grid, sums, st);
   }
   if (e != hipSuccess || s.splits == 1) return e;
-  return launch_op(wgrad_join_kernel, grid_for((s.tiles - s.full) * (s.tile * s.tile / 8 / kThreads), kThreads), kThreads,
-                   st, a, s);
+  const uint64_t groups = static_cast<uint64_t>(s.tiles - s.full) * s.tile * s.tile / 8;
+  return s.splits <= 2 || groups >= kJoinAlone ? wgrad_join<1>(a, s, st)
+         : s.splits <= 4                       ? wgrad_join<4>(a, s, st)
+                                               : wgrad_join<8>(a, s, st);
 }
 
 }  // namespace lc

@@ -619,6 +619,26 @@ def test_a_single_rows_strides_are_not_looked_at(n, k, dtype, strides):
     assert torch.equal(back.double(), kept.values())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_wgrad_of_rows_far_apart(dtype):
+    """Rows 2^24 elements and more apart, whose offsets the loads of 32 rows cannot hold in 32 bits."""
+    rows, n, k, stride = 9, 264, 272, (1 << 24) + 8
+    dt, code, _ = DT[dtype]
+    dy = torch.zeros(rows * stride, dtype=dt, device="cuda").view(rows, stride)[:, :n]
+    dy.copy_(torch.randint(-8, 8, (rows, n), generator=gen(2), device="cuda"))
+    codes = torch.zeros(rows * stride, dtype=torch.uint8, device="cuda").view(rows, stride)[:, :k]
+    kept = kept_normal(rows, k, 4)
+    codes.copy_(kept.codes.view)
+    act = LC.saved_act(codes.data_ptr(), kept.scales.addr, rows, k, stride, kept.scales.stride)
+    need = LC.lc_linear_wgrad_workspace(rows, n, k)
+    buf, ws, _ = space(need)
+    dw = torch.empty(n, k, device="cuda")
+    LC.lc_linear_wgrad(LC.matrix(dy.data_ptr(), rows, n, code, stride), act, LC.matrix(dw.data_ptr(), n, k, LC.LC_DT_F32), ws, need,
+                       stream=stream())
+    x, d64 = kept.values(), dy.double()
+    close(dw, d64.t() @ x, (3 * rows + 80) * U32 * (d64.abs().t() @ x.abs()))
+
+
 def test_wgrad_takes_all_bits_of_a_32_bit_gradient():
     """One token and a kept 1.0: the gradient is dy itself, to the last bit, from the largest to the smallest normal."""
     g = gen(9)
