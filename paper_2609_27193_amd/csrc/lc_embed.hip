@@ -90,15 +90,14 @@ __device__ __forceinline__ void fill_rows(const Fill& f, uint64_t block, uint64_
 // ---- sorting the tokens ------------------------------------------------------------
 // Few tokens need no order (embed_direct_kernel, below).  Up to kRankTokens one
 // launch counts, for every token, the tokens that come before it (a smaller row,
-// or the same row at an earlier position); beyond that a radix sort of kDigitBits
-// a pass, two launches a pass.  Of the whole gradient into 32000 x 1024, added to
-// what is there: 4096 tokens 22 us by counts and 32 by passes, 8192 tokens 38 and
-// 31.  Both are bound by latency: 4096 tokens, counted, about 8 us; a pass of
-// 16384 tokens 2.5 to 4.7 and 4.5 to 5.3 us for its two launches.  Their few
-// blocks leave the chip to others, which clear the table meanwhile, rows with a
-// token and without: writing the former twice costs less than the sort's time
-// alone (16384 tokens into 128256 x 2048: 117 us, and 152 where the sums' launch
-// cleared the rows without a token).
+// or the same row at an earlier position); beyond that one block sorts, or, many,
+// a radix sort of kDigitBits a pass, two launches a pass.  All are bound by
+// latency: 4096 tokens, counted, about 8 us; a pass of 16384 tokens 2.5 to 4.7 and
+// 4.5 to 5.3 us for its two launches.  Their few blocks leave the chip to others,
+// which clear the table meanwhile, rows with a token and without: writing the
+// former twice costs less than the sort's time alone (16384 tokens into 128256 x
+// 2048 bf16: 117 us by passes, and 152 where the sums' launch cleared the rows
+// without a token).
 constexpr uint32_t kRankTokens = 4096;
 constexpr uint32_t kRankThreads = 256;
 constexpr uint32_t kRankOwn = 8;  // tokens of a block; its 32 slices of threads share the others
@@ -162,6 +161,21 @@ constexpr uint32_t kSortTiles = 64;
 __host__ __device__ inline uint32_t sort_tile(uint64_t n) {
   const uint64_t per = (n + kSortTiles - 1) / kSortTiles;
   return static_cast<uint32_t>((per + kSortThreads - 1) / kSortThreads * kSortThreads);
+}
+
+// Lanes of the wave that are `on` and have this lane's digit.
+__device__ __forceinline__ uint64_t lanes_of_digit(bool on, uint32_t digit, uint32_t bits) {
+  const uint64_t all = __ballot(on);
+  uint32_t lo = static_cast<uint32_t>(all), hi = static_cast<uint32_t>(all >> 32);
+#pragma unroll
+  for (uint32_t bit = 0; bit < kDigitBits; ++bit) {
+    if (bit >= bits) break;  // the same for the whole grid
+    const uint32_t zero = (digit >> bit & 1) - 1;  // all ones where the bit is not set
+    const uint64_t ones = __ballot(zero == 0);
+    lo &= static_cast<uint32_t>(ones) ^ zero;
+    hi &= static_cast<uint32_t>(ones >> 32) ^ zero;
+  }
+  return static_cast<uint64_t>(hi) << 32 | lo;
 }
 
 // keys null: the tokens themselves, at position i.
@@ -233,13 +247,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a,
       const bool on = i < a.n;
       const uint32_t key = on ? sort_key(a, keys, i) : 0;
       const uint32_t digit = (key >> shift) % kDigits;
-      uint64_t same = __ballot(on);  // lanes of this wave with the same digit
-#pragma unroll
-      for (uint32_t bit = 0; bit < kDigitBits; ++bit) {
-        const bool one = digit >> bit & 1;
-        const uint64_t ones = __ballot(one);
-        same &= one ? ones : ~ones;
-      }
+      const uint64_t same = lanes_of_digit(on, digit, kDigitBits);
       const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
       if (on && rank == 0) wave_count[wave][digit] = __popcll(same);
       __syncthreads();
@@ -261,6 +269,110 @@ __global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a,
 #pragma unroll
       for (uint32_t w = 0; w < kSortWaves; ++w) wave_count[w][tid] = 0;
       __syncthreads();
+    }
+  }
+}
+
+// ---- sorting in one block -------------------------------------------------------------
+// One block sorts alone, in one launch, while the others clear the table: KPT
+// tokens a thread, up to kDigitBits a pass, exchanged through LDS.  A wave has
+// 64 * KPT tokens that follow each other; a token's place within its wave's
+// tokens of a digit comes from ballots and the wave's own counts, so that a pass
+// keeps the order of what is equal.  Bound by that one CU's vector ALU: 13.7 us
+// for 6000 tokens of 2000 rows, 28 for 16384 of 50257, where the passes over all
+// blocks take 24 and 24.  So it sorts up to 8192 tokens (6000 into 2000 x 300
+// fp32, whole, 29 us, by passes 38.6), and twice that where the table takes as long
+// to clear (16384 into 32000 x 4096 bf16 83 us for 88, into 50257 x 1024, 103 MB,
+// 46.5 for 43).
+constexpr uint32_t kBlockThreads = 1024, kBlockWaves = kBlockThreads / 64;
+constexpr uint32_t kBlockTokens = 8 * kBlockThreads;
+constexpr uint64_t kBlockClears = 128ull << 20;  // bytes
+bool sorts_in_block(uint64_t n, uint64_t table_bytes) {
+  return n <= kBlockTokens || (n <= 2 * kBlockTokens && table_bytes >= kBlockClears);
+}
+template <uint32_t KPT>
+__global__ __launch_bounds__(kBlockThreads) void embed_block_sort_kernel(EmbedBwd a, Fill fill, uint32_t passes, uint32_t bits,
+                                                                         uint32_t* keys, uint32_t* pos) {
+  __shared__ uint32_t key_lds[KPT * kBlockThreads];
+  __shared__ uint16_t pos_lds[KPT * kBlockThreads];
+  __shared__ uint16_t count[kBlockWaves][kDigits];  // a wave's tokens of a digit, then where the first of them goes
+  __shared__ uint32_t wave_total[kDigits / 64];
+  static_assert(2 * kBlockTokens <= 1u << 16, "positions and places in 16 bits");
+  if (blockIdx.x > 0) {
+    for (uint64_t b = blockIdx.x - 1; fill.first + b * fill.per < fill.rows; b += gridDim.x - 1) fill_rows(fill, b, 0);
+    return;
+  }
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = static_cast<uint32_t>(a.n);
+  const uint32_t at0 = wave * 64 * KPT + lane;
+  volatile uint16_t* const mine = count[wave];  // other lanes' writes are seen
+  uint32_t key[KPT], from[KPT], place[KPT];
+#pragma unroll
+  for (uint32_t r = 0; r < KPT; ++r) {
+    const uint32_t i = at0 + 64 * r;
+    from[r] = i;
+    key[r] = token_row(a.tokens, a.token64, i < n ? i : n - 1, a.first, a.vocab);
+  }
+  for (uint32_t pass = 0; pass < passes; ++pass) {
+    const uint32_t shift = pass * bits, digits = 1u << bits;
+    for (uint32_t d = lane; d < digits; d += 64) mine[d] = 0;
+#pragma unroll
+    for (uint32_t r = 0; r < KPT; ++r) {
+      const bool on = at0 + 64 * r < n;
+      const uint32_t digit = key[r] >> shift & (digits - 1);
+      const uint64_t same = lanes_of_digit(on, digit, bits);
+      const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+      const uint32_t had = mine[digit];
+      __builtin_amdgcn_wave_barrier();
+      if (on && before == 0) mine[digit] = static_cast<uint16_t>(had + __popcll(same));
+      __builtin_amdgcn_wave_barrier();
+      place[r] = had + before;
+    }
+    __syncthreads();
+    uint32_t total = 0, scan = 0;
+    if (tid < kDigits) {  // whole waves: a thread a digit; behind the last one, counts that no one reads
+#pragma unroll
+      for (uint32_t w = 0; w < kBlockWaves; ++w) {
+        const uint32_t c = count[w][tid];
+        count[w][tid] = static_cast<uint16_t>(total);
+        total += c;
+      }
+      scan = total;
+#pragma unroll
+      for (uint32_t d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(scan, d, 64);
+        if (lane >= d) scan += o;
+      }
+      if (lane == 63) wave_total[wave] = scan;
+    }
+    __syncthreads();
+    if (tid < kDigits) {
+      uint32_t base = scan - total;
+      for (uint32_t w = 0; w < wave; ++w) base += wave_total[w];
+#pragma unroll
+      for (uint32_t w = 0; w < kBlockWaves; ++w) count[w][tid] = static_cast<uint16_t>(count[w][tid] + base);
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < KPT; ++r) {
+      if (at0 + 64 * r >= n) continue;
+      const uint32_t to = count[wave][key[r] >> shift & (digits - 1)] + place[r];
+      key_lds[to] = key[r];
+      pos_lds[to] = static_cast<uint16_t>(from[r]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < KPT; ++r) {  // behind the last token: whatever lies there, and is not used
+      key[r] = key_lds[at0 + 64 * r];
+      from[r] = pos_lds[at0 + 64 * r];
+    }
+    // the next pass's counts are written before its own barriers, and so are its keys after them
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < KPT; ++r) {
+    const uint32_t i = at0 + 64 * r;
+    if (i < n) {
+      keys[i] = key[r];
+      pos[i] = from[r];
     }
   }
 }
@@ -625,7 +737,7 @@ BwdRegions bwd_regions(uint64_t n, uint64_t dim) {
   if (n <= kDirectTokens) return r;
   r.run = sum_run(n, (dim + kSumCols - 1) / kSumCols);
   r.tiles = static_cast<uint32_t>((n + r.run - 1) / r.run);
-  const bool radix = n > kRankTokens;
+  const bool radix = n > kBlockTokens;  // up to twice that, by the table
   const uint64_t list = pad256(n * 4);
   uint64_t at = 0;
   for (int i = 0; i < (radix ? 2 : 1); ++i) {
@@ -724,13 +836,14 @@ hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
   uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(a.ws + r.keys[0]), reinterpret_cast<uint32_t*>(a.ws + r.keys[1])};
   uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(a.ws + r.pos[0]), reinterpret_cast<uint32_t*>(a.ws + r.pos[1])};
   int sorted = 0;
-  if (a.n > kRankTokens) {
+  const Fill table = whole_table_at_once(a);
+  if (!sorts_in_block(a.n, table.rows * table.bytes)) {
     uint32_t* hist = reinterpret_cast<uint32_t*>(a.ws + r.hist);
     const uint32_t tile = sort_tile(a.n);
     const uint64_t tiles = (a.n + tile - 1) / tile;
     uint32_t launches = 0, launch = 0;
     for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += kDigitBits) launches += 2;  // keys 0 to vocab
-    Fill f = whole_table_at_once(a);
+    Fill f = table;
     const uint64_t rows = f.rows, share = (rows / launches + f.per) / f.per * f.per;
     auto next = [&] {  // the launch's share of the table
       f.first = share * launch < rows ? share * launch : rows;
@@ -753,10 +866,17 @@ hipError_t launch_embed_bwd(const EmbedBwd& a, hipStream_t st) {
       from = to;
     }
     sorted = from;
+  } else if (a.n > kRankTokens) {
+    const SortGrid g = sort_grid(1, table, kBlockThreads);
+    uint32_t bits = 1;
+    while (a.vocab >> bits) ++bits;  // keys 0 to vocab
+    const uint32_t passes = (bits + kDigitBits - 1) / kDigitBits;
+    const hipError_t e = launch_op(a.n > kBlockTokens ? embed_block_sort_kernel<16> : embed_block_sort_kernel<8>, g.blocks,
+                                   kBlockThreads, st, a, table, passes, (bits + passes - 1) / passes, keys[0], pos[0]);
+    if (e != hipSuccess) return e;
   } else if (a.n > kDirectTokens) {
-    const Fill f = whole_table_at_once(a);
-    const SortGrid g = sort_grid((a.n + kRankOwn - 1) / kRankOwn, f, kRankThreads);
-    const hipError_t e = launch_op(embed_rank_kernel, g.blocks, kRankThreads, st, a, f, g.fill_from, keys[0], pos[0]);
+    const SortGrid g = sort_grid((a.n + kRankOwn - 1) / kRankOwn, table, kRankThreads);
+    const hipError_t e = launch_op(embed_rank_kernel, g.blocks, kRankThreads, st, a, table, g.fill_from, keys[0], pos[0]);
     if (e != hipSuccess) return e;
   }
   SumArgs s;

@@ -274,6 +274,22 @@ def test_embedding(n, vocab, dim, kind, w, o):
         assert torch.equal(again.view, dw.view)  # the same bits every time
 
 
+@pytest.mark.parametrize("n,vocab,dim,kind", [(4097, 511, 8, "skewed"), (4097, 512, 8, "mixed"), (8192, 3, 16, "mixed"), (8192, 262144, 8, "skewed"),
+                                              (5000, 1, 24, "one"), (12000, 33000, 2048, "skewed"), (16384, 65000, 1040, "mixed")])
+def test_embedding_gradient_sorted_in_one_block(n, vocab, dim, kind):
+    """Around its sizes: gradients of whole numbers, whose sums are exact, so that any token out of place shows."""
+    tokens = some_tokens(n, vocab, 0, n, kind)
+    held = (tokens >= 0) & (tokens < vocab)
+    dout = torch.randint(-3, 4, (n, dim), generator=gen(n), device="cuda").bfloat16()
+    dw = torch.full((vocab, dim), math.nan, device="cuda")
+    need = LC.lc_embedding_backward_workspace(n, dim)
+    buf, ws, _ = space(need)
+    LC.lc_embedding_backward(LC.matrix(dout.data_ptr(), n, dim, LC.LC_DT_BF16), tokens.data_ptr(), LC.LC_IT_I64, n,
+                             LC.matrix(dw.data_ptr(), vocab, dim, LC.LC_DT_F32), ws, need, stream=stream())
+    assert bool((buf[need:] == 0xA5).all())
+    assert torch.equal(dw, torch.zeros(vocab, dim, device="cuda").index_add_(0, tokens[held], dout[held].float()))
+
+
 def test_embedding_gradient_against_differences():
     """The table's gradient is that of sum(dout * out): out is linear in the table, so a difference is exact to rounding."""
     n, vocab, dim, scale = 200, 30, 40, 3.0

@@ -31,7 +31,8 @@ def calls(h):
     V = lambda: at + next(apart)  # noqa: E731
     out = [("embedding", lambda: LC.lc_embedding_forward(M(99, 64), V(), 2, 7, M(7, 64)), ["embed_fwd"])]
     for n, vocab, kernels in [(7, 99, ["direct"]), (2048, 99, ["direct"]), (2049, 99, ["rank", "sum", "join"]),
-                              (4096, 99, ["rank", "sum", "join"]), (4097, 99, ["count", "scatter", "sum", "join"]),
+                              (4096, 99, ["rank", "sum", "join"]), (4097, 99, ["block_sort", "sum", "join"]), (8192, 1 << 18, ["block_sort", "sum", "join"]),
+                              (16384, 1 << 20, ["block_sort", "sum", "join"]), (16385, 1 << 20, ["count", "scatter"] * 3 + ["sum", "join"]),
                               (8193, 512, ["count", "scatter"] * 2 + ["sum", "join"]),
                               (8193, 511, ["count", "scatter", "sum", "join"]),
                               (8193, 1 << 18, ["count", "scatter"] * 3 + ["sum", "join"])]:
