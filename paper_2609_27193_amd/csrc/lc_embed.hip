@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, ui
 struct Fill {
   uint64_t data, pitch, first, rows;  // of the table: its first row, bytes a row; rows first to rows - 1
   uint64_t end;                       // no byte from here on is written
-  uint32_t bytes;                     // of a row that count, even
+  uint64_t bytes;                     // of a row that count, even: up to 2^32
   uint32_t per;
 };
 __host__ inline uint64_t fill_blocks(const Fill& f) { return (f.rows - f.first + f.per - 1) / f.per; }
@@ -80,9 +80,9 @@ __device__ __forceinline__ void fill_rows(const Fill& f, uint64_t block, uint64_
   for (uint32_t i = wave * run; i < (wave + 1) * run && i < f.per && r0 + i < f.rows; ++i) {
     if (skip >> i & 1) continue;
     const uint64_t p = f.data + (r0 + i) * f.pitch;
-    const uint32_t bytes = f.end - p < f.bytes ? static_cast<uint32_t>(f.end - p) : f.bytes;
-    for (uint32_t at = lane * 16; at + 16 <= bytes; at += 64 * 16) st_any(reinterpret_cast<uint8_t*>(p + at), u32x4{0, 0, 0, 0});
-    const uint32_t tail = bytes & ~15u;
+    const uint64_t bytes = f.end - p < f.bytes ? f.end - p : f.bytes;
+    for (uint64_t at = lane * 16; at + 16 <= bytes; at += 64 * 16) st_any(reinterpret_cast<uint8_t*>(p + at), u32x4{0, 0, 0, 0});
+    const uint64_t tail = bytes & ~15ull;
     if (tail + lane * 2 < bytes) *(g_u16*)(p + tail + lane * 2) = 0;
   }
 }
@@ -777,8 +777,7 @@ hipError_t embed_sums(const SumArgs& s, hipStream_t st) {
 
 Fill fill_of(uint64_t data, uint64_t pitch, uint64_t rows, uint64_t bytes) {
   const uint64_t per = bytes < 262144 ? 262144 / bytes : 1;
-  return Fill{data, pitch, 0, rows, data + (rows ? (rows - 1) * pitch + bytes : 0), static_cast<uint32_t>(bytes),
-              static_cast<uint32_t>(per < 64 ? per : 64)};
+  return Fill{data, pitch, 0, rows, data + (rows ? (rows - 1) * pitch + bytes : 0), bytes, static_cast<uint32_t>(per < 64 ? per : 64)};
 }
 Fill whole_table(const EmbedBwd& a) {
   const uint64_t e = a.dw_dtype == kBf16 ? 2 : 4;

@@ -452,7 +452,7 @@ constexpr bool norm_has_shape(uint64_t dim) { return dim >= 8 && dim <= kNormLon
   else F(1024, 2)
 
 // As many blocks as are resident at once, for more only add parts (16384 x
-// 4096 layer norm, 12 waves a CU 85 us, 16 97; RMS norm in bf16, which holds no
+// 4096 layer norm, 12 waves a CU 69 us, 16 81; RMS norm in bf16, which holds no
 // sums of db and narrower rows, 71 and 67).
 NormParts norm_parts(uint64_t rows, uint64_t dim, bool light) {
   uint32_t tpr = kLongThreads, waves = 16;

@@ -661,8 +661,8 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
 
 // The parts' sums with the columns' scale and shift.  SLICES threads share eight
 // columns of a row of dW: each adds every SLICES-th part, then the first adds the
-// others' sums, in a fixed order.
-template <uint32_t SLICES>
+// others' sums, in a fixed order.  AHEAD: parts that a thread has under way.
+template <uint32_t SLICES, uint32_t AHEAD>
 __global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTiles s) {
   constexpr uint32_t G = kThreads / SLICES;  // groups of eight columns a block
   __shared__ float sums[SLICES][9][G];
@@ -679,7 +679,7 @@ __global__ __launch_bounds__(kThreads) void wgrad_join_kernel(Wgrad a, WgradTile
     const bool bias = a.dbias && !s.big && k0 + lk == 0;
     float v[8] = {}, f[8], sum = 0;
     if (on) {
-#pragma unroll (SLICES > 1 ? 4 : 8)
+#pragma unroll (AHEAD)
       for (uint32_t p = slice; p < s.splits; p += SLICES) {  // a part is a whole tile, also where dW ends
         unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(wgrad_part(s, tile, p, ln) + lk)), f);
 #pragma unroll
@@ -808,10 +808,10 @@ hipError_t wgrad_of(const Wgrad& a, const WgradTiles& s, uint32_t grid, bool sum
   return launch_op(sums ? wgrad_kernel<DT, true, false> : wgrad_kernel<DT, false, false>, grid, kThreads, st, a, s);
 }
 constexpr uint64_t kJoinAlone = 98304;  // groups of eight columns from which a thread adds all parts of one
-template <uint32_t SLICES>
+template <uint32_t SLICES, uint32_t AHEAD>
 hipError_t wgrad_join(const Wgrad& a, const WgradTiles& s, hipStream_t st) {
   const uint32_t blocks = (s.tiles - s.full) * (s.tile * s.tile / 8 * SLICES / kThreads);
-  return launch_op(wgrad_join_kernel<SLICES>, grid_for(blocks, kThreads), kThreads, st, a, s);
+  return launch_op(wgrad_join_kernel<SLICES, AHEAD>, grid_for(blocks, kThreads), kThreads, st, a, s);
 }
 uint64_t wgrad_space(const WgradTiles& s, uint64_t n) {
   return wgrad_part_bytes(s) + (s.sum_parts + (s.big ? kSumParts : 0)) * n * 4;
@@ -854,9 +854,9 @@ hipError_t launch_wgrad(const Wgrad& a, hipStream_t st) {
   }
   if (e != hipSuccess || s.splits == 1) return e;
   const uint64_t groups = static_cast<uint64_t>(s.tiles - s.full) * s.tile * s.tile / 8;
-  return s.splits <= 2 || groups >= kJoinAlone ? wgrad_join<1>(a, s, st)
-         : s.splits <= 4                       ? wgrad_join<4>(a, s, st)
-                                               : wgrad_join<8>(a, s, st);
+  if (s.splits <= 2) return wgrad_join<1, 2>(a, s, st);
+  if (groups >= kJoinAlone) return s.splits <= 4 ? wgrad_join<1, 4>(a, s, st) : wgrad_join<1, 8>(a, s, st);
+  return s.splits <= 4 ? wgrad_join<4, 1>(a, s, st) : wgrad_join<8, 4>(a, s, st);
 }
 
 }  // namespace lc
