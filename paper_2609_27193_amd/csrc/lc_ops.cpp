@@ -207,7 +207,7 @@ extern "C" lc_status lc_embedding_forward(const lc_matrix* weight, const void* t
 }
 
 extern "C" uint64_t lc_embedding_backward_workspace(uint64_t n_tokens, uint64_t cols) {
-  return n_tokens > kMaxRows || cols > kMaxCols ? 0 : embed_bwd_workspace(n_tokens, cols);
+  return n_tokens > kMaxRows || cols == 0 || cols > kMaxCols ? 0 : embed_bwd_workspace(n_tokens, cols);
 }
 
 extern "C" lc_status lc_embedding_backward(const lc_matrix* dout, const void* tokens, int32_t token_dtype,

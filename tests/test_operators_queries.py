@@ -1,0 +1,29 @@
+"""The workspace queries of the training operators, at sizes that no call takes (CPU)."""
+import subprocess
+import sys
+
+import pytest
+
+from tests.conftest import ROOT
+
+
+@pytest.mark.parametrize("query,sizes", [("lc_embedding_backward_workspace", (5000, 0)), ("lc_embedding_backward_workspace", (2049, 0)),
+                                         ("lc_embedding_backward_workspace", (1 << 31, 0)), ("lc_embedding_backward_workspace", (0, 0)),
+                                         ("lc_embedding_backward_workspace", ((1 << 31) + 1, 8)), ("lc_embedding_backward_workspace", (5000, (1 << 30) + 1)),
+                                         ("lc_embedding_backward_workspace", ((1 << 64) - 1, (1 << 64) - 1)),
+                                         ("lc_norm_backward_workspace", (5000, 0)), ("lc_norm_backward_workspace", (0, 0)),
+                                         ("lc_norm_backward_workspace", ((1 << 64) - 1, (1 << 64) - 1)),
+                                         ("lc_linear_wgrad_workspace", (5000, 0, 8)), ("lc_linear_wgrad_workspace", (5000, 8, 0)),
+                                         ("lc_linear_wgrad_workspace", (0, 0, 0)), ("lc_linear_wgrad_workspace", ((1 << 64) - 1,) * 3)])
+def test_nothing_is_needed_beyond_the_limits(query, sizes):
+    """In a child process: a query must not end the program."""
+    r = subprocess.run([sys.executable, "-c", f"from paper_2609_27193_amd import layercheck as LC; print(LC.{query}{sizes})"],
+                       cwd=ROOT, capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0 and r.stdout.split()[-1] == "0", (r.returncode, r.stdout, r.stderr)
+
+
+@pytest.mark.parametrize("n,cols", [(1 << 31, 1 << 30), (1 << 31, 1), (2049, 1 << 30)])
+def test_the_largest_sizes_have_one(n, cols):
+    from paper_2609_27193_amd import layercheck as LC
+    assert LC.lc_embedding_backward_workspace(n, cols) >= 8 * n
+    assert LC.lc_norm_backward_workspace(n, cols) >= 8 * cols
