@@ -452,14 +452,15 @@ lc_status lc_destroy(lc_ctx *c);
  * they allocate nothing, so they may be captured into a HIP graph.  Arguments
  * are checked first (LC_ERR_INVALID_ARG, nothing enqueued): sizes, types,
  * alignment, and that no array that is written overlaps another one (columns
- * of one buffer beside each other are fine).  As with the gradients of the
- * optimizer steps, addresses are checked for NULL and alignment and not
- * looked up: a wrong one faults on the GPU.  A workspace is 16-byte aligned
- * and at least as large as the _workspace call says for the same sizes
- * (LC_ERR_CAPACITY if smaller; the _workspace calls give 0 for sizes beyond
- * the limits, and where no workspace is needed); its contents need not be
- * kept between calls.  Sums are fp32 or wider and their order is fixed, so a
- * call gives the same bits every time. */
+ * of one buffer beside each other are fine, and so is a vector or a single row
+ * between the rows of an array; arrays of two strides must lie behind each
+ * other).  As with the gradients of the optimizer steps, addresses are checked
+ * for NULL and alignment and not looked up: a wrong one faults on the GPU.  A
+ * workspace is 16-byte aligned and at least as large as the _workspace call says
+ * for the same sizes (LC_ERR_CAPACITY if smaller; the _workspace calls give 0
+ * for sizes beyond the limits, and where no workspace is needed); its contents
+ * need not be kept between calls.  Sums are fp32 or wider and their order is
+ * fixed, so a call gives the same bits every time. */
 
 /* Rows of elements in device memory: element (r, c) at data + (r * stride + c)
  * elements.  At most 2^31 rows of 2^30 columns; data is aligned to its element

@@ -87,11 +87,12 @@ bool overlap(const Area& a, const Area& b) {
   if (!a.rows || !b.rows) return false;
   const uint64_t a_end = a.base + (a.rows - 1) * a.pitch + a.width, b_end = b.base + (b.rows - 1) * b.pitch + b.width;
   if (a_end <= b.base || b_end <= a.base) return false;
-  if (a.rows > 1 && b.rows > 1 && a.pitch == b.pitch) {  // columns beside each other in one buffer
-    const uint64_t off = b.base >= a.base ? (b.base - a.base) % a.pitch : (a.pitch - (a.base - b.base) % a.pitch) % a.pitch;
-    return off < a.width || off + b.width > a.pitch;
-  }
-  return true;
+  if (a.rows == 1 && b.rows == 1) return true;
+  // columns beside each other in one buffer; a single row or a vector has the pitch of the rows beside it
+  const uint64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+  if (b.rows > 1 && b.pitch != pitch) return true;
+  const uint64_t off = b.base >= a.base ? (b.base - a.base) % pitch : (pitch - (a.base - b.base) % pitch) % pitch;
+  return off < a.width || off + b.width > pitch;
 }
 
 // The first n_out areas are written.
