@@ -231,6 +231,13 @@ __device__ __forceinline__ tile_t step_tile(uint64_t base, int rows, uint32_t pi
   const uint32_t bytes = static_cast<uint32_t>(rows - 1) * pitch + width;
   return make_tile(reinterpret_cast<const void*>(base), rows > 0 ? bytes : 0u);
 }
+// The whole offset is in the operand that the bounds check covers; the scalar
+// one is left at zero, for it need not count there.
+template <typename T>
+__device__ __forceinline__ T ld_step(tile_t t, uint32_t off) {
+  if constexpr (sizeof(T) == 16) return __builtin_amdgcn_raw_buffer_load_b128(t, off, 0, 0);
+  else return __builtin_amdgcn_raw_buffer_load_b8(t, off, 0, 0);
+}
 
 // ANY: rows of any length and stride, read an element at a time where they end;
 // else of 8 columns of n and 16 of k at least, as far as 32-bit offsets reach.
@@ -286,9 +293,9 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int q = 0; q < static_cast<int>(kEsz<DT>) / 2; ++q)
-            g.d[i].v[q] = __builtin_amdgcn_raw_buffer_load_b128(td, d_from + 16 * q, i * 16 * d_pitch, 0);
-        g.c.codes = __builtin_amdgcn_raw_buffer_load_b128(tx, x_from, 0, 0);
-        g.c.code = __builtin_amdgcn_raw_buffer_load_b8(ts, s_from, 0, 0);
+            g.d[i].v[q] = ld_step<u32x4>(td, d_from + i * 16 * d_pitch + 16 * q);
+        g.c.codes = ld_step<u32x4>(tx, x_from);
+        g.c.code = ld_step<uint8_t>(ts, s_from);
       }
     };
     auto store = [&](Stage& g, int buf) {
@@ -515,11 +522,11 @@ __global__ __launch_bounds__(kThreads, 1) void wgrad_big_kernel(Wgrad a, WgradTi
       const auto there = [&](uint32_t row, uint32_t from) { return !RAGGED || static_cast<int>(row) < rows ? from : kNowhere; };
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        g.dy[i] = __builtin_amdgcn_raw_buffer_load_b128(td, there(dr + 8 * i, dy_from + i * 8 * dy_pitch), 0, 0);
+        g.dy[i] = ld_step<u32x4>(td, there(dr + 8 * i, dy_from + i * 8 * dy_pitch));
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        g.x[i] = __builtin_amdgcn_raw_buffer_load_b128(tx, there(xr + 16 * i, x_from + i * 16 * x_pitch), 0, 0);
-        g.scale[i] = __builtin_amdgcn_raw_buffer_load_b8(ts, s_from, i * 16 * s_pitch, 0);
+        g.x[i] = ld_step<u32x4>(tx, there(xr + 16 * i, x_from + i * 16 * x_pitch));
+        g.scale[i] = ld_step<uint8_t>(ts, s_from + i * 16 * s_pitch);
       }
     };
     // a step's share in eight writes, a half step's operands in eight reads

@@ -6,7 +6,7 @@ import sys
 
 from paper_2609_27193_amd.build_lib import LIB
 from tests.test_host_calls import DEVICE, ROOT, hip, standin  # noqa: F401 (a fixture)
-from tests.wgrad_cases import RAGGED
+from tests.wgrad_cases import ALIGNED, RAGGED, SMALL
 
 
 def routes():
@@ -14,9 +14,9 @@ def routes():
     h = hip()
     at = h.standin_alloc(1 << 20, DEVICE)
     a = [at + (i + 1 << 38) for i in range(6)]  # never read
-    for (rows, n, k), kernels in RAGGED:
+    for dtype, (rows, n, k), kernels in [(LC.LC_DT_BF16, *c) for c in ALIGNED + RAGGED + SMALL] + [(LC.LC_DT_F32, *c) for c in SMALL]:
         h.standin_clear()
-        LC.lc_linear_wgrad(LC.matrix(a[0], rows, n, LC.LC_DT_BF16), LC.saved_act(a[1], a[2], rows, k),
+        LC.lc_linear_wgrad(LC.matrix(a[0], rows, n, dtype), LC.saved_act(a[1], a[2], rows, k),
                            LC.matrix(a[3], n, k, LC.LC_DT_F32), a[4], LC.lc_linear_wgrad_workspace(rows, n, k))
         got = h.words()
         assert len(got) == len(kernels) and all(w in g for w, g in zip(kernels, got)), ((rows, n, k), got)

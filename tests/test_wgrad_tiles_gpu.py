@@ -1,4 +1,4 @@
-"""The weight gradient's tiles of 256 columns at the sizes that take them, with what must not be read made of NaN: the rows
+"""The weight gradient at sizes that take each of its kernels, with what must not be read made of NaN: the rows
 behind the last one, the gaps between rows and what lies before the first.
 
 dY and the kept X are whole numbers (X times a power of two), and no sum of theirs reaches 2^24: every sum is exact in any
@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from paper_2609_27193_amd import layercheck as LC
-from tests.wgrad_cases import RAGGED
+from tests.wgrad_cases import ALIGNED, RAGGED, SMALL
 
 pytestmark = pytest.mark.gpu
 
@@ -40,12 +40,12 @@ def code_of(numbers):
 class Case:
     """dY and X of a size; X is `x` times 2^(scale - 127)."""
 
-    def __init__(self, rows, n, k, pad, off, scale):
+    def __init__(self, rows, n, k, pad, off, scale, dtype=torch.bfloat16):
         g = torch.Generator(device="cuda").manual_seed(rows + n + k)
         self.rows, self.n, self.k, self.power = rows, n, k, 2.0 ** (scale - 127)
         self.d = torch.randint(-3, 4, (rows, n), generator=g, device="cuda")
         self.x = torch.randint(1, 16, (rows, k), generator=g, device="cuda") * (torch.randint(0, 2, (rows, k), generator=g, device="cuda") * 2 - 1)
-        self.dy = among_nan(self.d.bfloat16(), math.nan, pad, off)
+        self.dy = among_nan(self.d.to(dtype), math.nan, pad, off)
         self.codes = among_nan(code_of(self.x), 127, pad, off)
         self.scales = among_nan(torch.full((rows, -(-k // 32)), scale, dtype=torch.uint8, device="cuda"), 255, pad, off)
 
@@ -53,7 +53,7 @@ class Case:
         need = LC.lc_linear_wgrad_workspace(self.rows, self.n, self.k)
         space = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN, where a part is not written
         dw = torch.full((self.n, self.k), math.nan, device="cuda")
-        LC.lc_linear_wgrad(LC.matrix(self.dy[1], self.rows, self.n, BF, self.dy[2]),
+        LC.lc_linear_wgrad(LC.matrix(self.dy[1], self.rows, self.n, BF if self.dy[0].dtype == torch.bfloat16 else F32, self.dy[2]),
                            LC.saved_act(self.codes[1], self.scales[1], self.rows, self.k, self.codes[2], self.scales[2]),
                            LC.matrix(dw.data_ptr(), self.n, self.k, F32), space.data_ptr(), need,
                            stream=torch.cuda.current_stream().cuda_stream, **kw)
@@ -64,6 +64,21 @@ class Case:
 
 
 PLACES = [(0, 0), (0, 1), (3, 1), (24, 8)]
+
+
+@pytest.mark.parametrize("rows,n,k", [size for size, _ in ALIGNED])
+@pytest.mark.parametrize("pad,off", PLACES)
+def test_whole_groups(rows, n, k, pad, off):
+    c = Case(rows, n, k, pad, off, 130)
+    assert torch.equal(c.wgrad().double(), c.reference())
+
+
+@pytest.mark.parametrize("rows,n,k", [size for size, _ in SMALL])
+@pytest.mark.parametrize("pad,off", PLACES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_tiles_of_128(rows, n, k, pad, off, dtype):
+    c = Case(rows, n, k, pad, off, 120, dtype)
+    assert torch.equal(c.wgrad().double(), c.reference())
 
 
 @pytest.mark.parametrize("rows,n,k", [size for size, _ in RAGGED])

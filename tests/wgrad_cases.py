@@ -1,5 +1,23 @@
 """Sizes of the linear weight gradient by the kernels that they take: (rows, n, k) of a bf16 dY, and the launches."""
 
+# whole groups of 16 bytes, in tiles of 256: steps of 32 tokens that end with 8, 1, 31 and 32, whole and in parts
+ALIGNED = [
+    ((200, 4096, 4096), ["big"]),
+    ((513, 2568, 4096), ["big"]),
+    ((2079, 4096, 2304), ["big"]),
+    ((4097, 2048, 3008), ["big", "join_kernelILj1ELj2E"]),
+    ((8192, 1288, 2304), ["big", "join_kernelILj1ELj4E"]),
+    ((16385, 1024, 1024), ["big", "join_kernelILj1ELj8E"]),
+]
+
+# tiles of 128, of either type: from one token and one column on
+SMALL = [
+    ((1, 1, 1), ["wgrad_kernel"]), ((1, 8, 16), ["wgrad_kernel"]), ((2, 9, 17), ["wgrad_kernel"]),
+    ((15, 200, 208), ["wgrad_kernel"]), ((17, 130, 140), ["wgrad_kernel"]), ((33, 257, 130), ["wgrad_kernel"]),
+    ((63, 7, 300), ["wgrad_kernel"]), ((95, 300, 15), ["wgrad_kernel"]),
+    ((1000, 40, 1030), ["wgrad_kernel", "join"]), ((4099, 129, 257), ["wgrad_kernel", "join"]),
+]
+
 RAGGED = [
     # whole sums; the last token behind 6 whole steps and 7 tokens, behind 16 whole steps, and behind 64
     ((200, 4091, 4095), ["big"]),
