@@ -27,7 +27,11 @@ EPS = 1e-5
 
 
 def view(t):
-    """The library's view of a two-dimensional tensor."""
+    """The library's view of a two-dimensional tensor, whose rows lie apart and whose columns lie side by side."""
+    if t.dim() != 2 or t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{t.dim()} dimensions of {t.dtype}: a matrix in bf16 or fp32 is needed")
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"strides of {t.stride()} for {tuple(t.shape)}: rows of neighbouring columns are needed")
     return LC.matrix(t.data_ptr(), t.shape[0], t.shape[1], BF if t.dtype == torch.bfloat16 else F32, t.stride(0))
 
 
