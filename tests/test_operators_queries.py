@@ -1,9 +1,11 @@
-"""The workspace queries of the training operators, at sizes that no call takes (CPU)."""
+"""The workspace queries of the training operators, at sizes that no call takes, and their checks under sanitizers (CPU)."""
+import os
 import subprocess
 import sys
 
 import pytest
 
+from paper_2609_27193_amd.build_lib import SANITIZED_LIB, sanitizer_runtime
 from tests.conftest import ROOT
 
 
@@ -27,3 +29,17 @@ def test_the_largest_sizes_have_one(n, cols):
     from paper_2609_27193_amd import layercheck as LC
     assert LC.lc_embedding_backward_workspace(n, cols) >= 8 * n
     assert LC.lc_norm_backward_workspace(n, cols) >= 8 * cols
+
+
+def test_checks_and_queries_under_host_sanitizers():
+    rt = sanitizer_runtime()
+    if not os.path.exists(SANITIZED_LIB) or not rt:
+        pytest.skip("the host-sanitized library is built by __graft_entry__.build()")
+    env = dict(os.environ, LD_PRELOAD=rt, LAYERCHECK_LIB=SANITIZED_LIB, ASAN_OPTIONS="detect_leaks=0:halt_on_error=1:abort_on_error=1",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-p", "no:cacheprovider", "-m", "not gpu", "-k", "not sanitizers",
+                        "tests/test_operators_abi.py", "tests/test_operators_apart.py", "tests/test_operators_queries.py"],
+                       cwd=ROOT, env=env, capture_output=True, text=True, timeout=600)
+    tail = (r.stdout + r.stderr)[-4000:]
+    assert r.returncode == 0, tail
+    assert "ERROR: AddressSanitizer" not in tail and "runtime error:" not in tail, tail

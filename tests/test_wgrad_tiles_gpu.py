@@ -153,6 +153,21 @@ def test_scales_at_both_ends(rows, n, k, dtype):
     assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
 
 
+@pytest.mark.parametrize("n,k", [(4096, 4096), (2565, 4095), (9, 17)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_no_tokens(n, k, dtype):
+    """Zeros, or what is there; dY and X have no rows and need no address."""
+    need = LC.lc_linear_wgrad_workspace(0, n, k)
+    space = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    scale, shift = torch.full((k,), 2.0, device="cuda"), torch.full((k,), 3.0, device="cuda")
+    for accumulate, before, after in ((False, math.nan, 0.0), (True, 5.0, 5.0)):
+        dw, db = torch.full((n, k), before, device="cuda"), torch.full((n,), before, device="cuda")
+        LC.lc_linear_wgrad(LC.matrix(0, 0, n, dtype), LC.saved_act(0, 0, 0, k), LC.matrix(dw.data_ptr(), n, k, F32),
+                           space.data_ptr(), need, col_scale=scale.data_ptr(), col_shift=shift.data_ptr(), dbias=db.data_ptr(),
+                           accumulate=accumulate, stream=torch.cuda.current_stream().cuda_stream)
+        assert bool((dw == after).all()) and bool((db == after).all())
+
+
 def test_grids_capped_at_forty_blocks():
     """Blocks that take several tiles, and several parts, after each other."""
     if not os.path.exists(GRID_CAPPED_LIB):
