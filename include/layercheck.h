@@ -487,9 +487,12 @@ lc_status lc_embedding_forward(const lc_matrix *weight, const void *tokens, int3
 
 /* dweight[v] = scale * sum of dout[t] over the t whose token is v + first_token
  * (accumulate 1: added to what dweight holds; 0: dweight is written in full,
- * zeros in rows that no token has).  The tokens are sorted, a row's sum runs
- * in the order of its positions in fp32 and is rounded once.  Tokens outside
- * the rows of dweight add nothing.  dout: n_tokens x dim, dweight: vocabulary
+ * zeros in rows that no token has).  A row's sum is fp32 and is rounded to
+ * dweight's type once.  Its tokens are taken by their positions, in runs that
+ * go by n_tokens, dim and the row's place among the sorted tokens, and the
+ * runs' sums are added in a fixed order: the same bits every time, and not
+ * those of one sum from the first position to the last.  Tokens outside the
+ * rows of dweight add nothing.  dout: n_tokens x dim, dweight: vocabulary
  * rows x dim, either of both dtypes. */
 uint64_t lc_embedding_backward_workspace(uint64_t n_tokens, uint64_t cols);
 lc_status lc_embedding_backward(const lc_matrix *dout, const void *tokens, int32_t token_dtype, uint64_t n_tokens,
@@ -560,7 +563,10 @@ lc_status lc_norm_backward(const lc_norm_params *params, const lc_matrix *dy, co
  *   dbias[n] (+)= sum over rows t of dy[t][n]
  * dy: rows x n, saved: rows x k, dweight: n x k, dbias: [n] of dweight's dtype
  * or NULL; col_scale and col_shift: [k] of param_dtype, each may be NULL (1, 0).
- * Products are exact (an fp32 dy enters with all its 24 bits), sums fp32. */
+ * Products of dy and X are exact (an fp32 dy enters with all its 24 bits; of X,
+ * what is below 2^-126 enters as bf16 holds it), sums fp32: dy * X is summed,
+ * then multiplied by col_scale, and the sum of dy by col_shift is added.  Where
+ * X * col_scale and col_shift cancel, the error stays that of the two sums. */
 uint64_t lc_linear_wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k);
 lc_status lc_linear_wgrad(const lc_matrix *dy, const lc_saved_act *saved, const void *col_scale,
                           const void *col_shift, int32_t param_dtype, const lc_matrix *dweight, void *dbias,

@@ -9,7 +9,9 @@ namespace {
 
 constexpr uint32_t kActThreads = 256;
 // Groups that a thread has in flight (saved and read back, us, of one, two, four
-// and eight; bf16): 8192 x 14336: 135, 133, 131, 127; 65536 x 1024: 79, 78, 79, 122.
+// and eight): 8192 x 14336 bf16 126, 124, 119, 114; 8192 x 8192 fp32 100, 96, 91,
+// 91; 65536 x 1024 bf16 73, 70, 76, 119.  Two: up to 2048
+// columns a thread has one, and the places held for more cost waves.
 constexpr int kActVecs = 2;
 
 // `lanes` threads (a power of two, 4 at least) take a row.

@@ -4,9 +4,9 @@
 //   dW[v] (+)= scale * sum over t with token[t] - first = v of dout[t]
 //
 // Both are bound by memory; of the gradient's, most is the table itself, which
-// is written whole.  The gradient sorts the tokens and sums a row's in the order
-// of their positions, in fp32: the result does not depend on how blocks are
-// scheduled.
+// is written whole.  The gradient sorts the tokens by row and position and sums
+// a row's in fp32, in runs whose bounds and order go by the sizes and the sorted
+// tokens alone: the result does not depend on how blocks are scheduled.
 #include "lc_ops_device.h"
 
 namespace lc {
@@ -25,9 +25,9 @@ constexpr uint32_t kEmbedThreads = 256;
 constexpr int kEmbedVecs = 4;  // groups of eight that a thread has in flight
 
 // `lanes` threads (a power of two) take one token's row, 8 elements each at a
-// time.  Bound by memory, 16384 rows of 4096 out of 128256 in bf16: 33 us, 8 TB/s
+// time.  Bound by memory, 16384 rows of 4096 out of 128256 in bf16: 32.4 us, 8 TB/s
 // with the rows that come again out of the caches; the output goes past them
-// (through them 38.6 us).
+// (through them 34.7 us).
 template <int WDT, int ODT>
 __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, uint32_t lanes_log2) {
   const uint32_t lanes = 1u << lanes_log2, per_block = kEmbedThreads >> lanes_log2;
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(EmbedFwd a, ui
 // ---- clearing the table -------------------------------------------------------------
 // A block clears `per` rows, about 256 KB and 64 of them at most, or those of
 // them that are not in `skip`; a wave's rows follow each other (16384 tokens into
-// 128256 x 2048 bf16, whole: 117 us, the waves' rows in turn 122).
+// 128256 x 2048 bf16, whole: 112 us, the waves' rows in turn 116).
 struct Fill {
   uint64_t data, pitch, first, rows;  // of the table: its first row, bytes a row; rows first to rows - 1
   uint64_t end;                       // no byte from here on is written
@@ -96,8 +96,8 @@ __device__ __forceinline__ void fill_rows(const Fill& f, uint64_t block, uint64_
 // 4.5 to 5.3 us for its two launches.  Their few blocks leave the chip to others,
 // which clear the table meanwhile, rows with a token and without: writing the
 // former twice costs less than the sort's time alone (16384 tokens into 128256 x
-// 2048 bf16: 117 us by passes, and 152 where the sums' launch cleared the rows
-// without a token).
+// 2048 bf16, sorted by passes: 117 us, and 152 where the sums' launch cleared the
+// rows without a token; one block sorts these now, 112).
 constexpr uint32_t kRankTokens = 4096;
 constexpr uint32_t kRankThreads = 256;
 constexpr uint32_t kRankOwn = 8;  // tokens of a block; its 32 slices of threads share the others
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_scatter_kernel(EmbedBwd a,
 // for 6000 tokens of 2000 rows, 28 for 16384 of 50257, where the passes over all
 // blocks take 24 and 24.  So it sorts up to 8192 tokens (6000 into 2000 x 300
 // fp32, whole, 29 us, by passes 38.6), and twice that where the table takes as long
-// to clear (16384 into 32000 x 4096 bf16 83 us for 88, into 50257 x 1024, 103 MB,
+// to clear (16384 into 32000 x 4096 bf16 83 us for 89, into 50257 x 1024, 103 MB,
 // 46.5 for 43).
 constexpr uint32_t kBlockThreads = 1024, kBlockWaves = kBlockThreads / 64;
 constexpr uint32_t kBlockTokens = 8 * kBlockThreads;
@@ -389,8 +389,8 @@ constexpr uint32_t kSumCols = 512;
 
 // Sorted positions of a tile: more leave fewer parts to join, fewer leave more
 // waves; 16 at least, and beyond that some 512 tiles, or 2048 waves of few columns
-// (131072 tokens into 32000 x 2048, all of one row: 2048 tiles 218 us, 512 154;
-// 16384 tokens' rows as often as words: 123 and 122).
+// (131072 tokens into 32000 x 2048, all of one row: 2048 tiles 223 us, 512 153, as
+// often as words 191 and 183; 16384 into 128256 x 2048 113 and 112).
 __host__ inline uint32_t sum_run(uint64_t n, uint64_t chunks) {
   const uint64_t tiles = chunks < 4 ? 2048 / chunks : 512;
   uint64_t r = 16;

@@ -243,8 +243,12 @@ __device__ __forceinline__ void normed8(const NormIn<DT, KEPT>& in, int n, float
 }
 
 // A block keeps its columns' weights and sums in registers and takes its turn
-// at the rows.  (The next row's loads under way meanwhile, for fewer blocks a
-// CU: no faster up to 4096 columns, 16384 columns 102.8 us for 72.9.)
+// at the rows.  The next row's loads in registers meanwhile, for fewer blocks a
+// CU, cost more than they hide (bf16, us: 16384 x 4096 RMS norm from kept rows 75
+// for 65, layer norm 71 for 69; 4096 x 16384 layer norm 92 for 79; 8192 x 8192
+// 74 for 75).  dx goes through the caches, where what follows may find it.  Past
+// them, of 16384 x 4096 from five sets of arrays in turn: from x 78.0 us for 74.5,
+// from kept rows 66.9 for 68.5, of one set over and over 79 for 75 and 65 for 65.
 template <int DT, bool LAYER, bool KEPT, int TPR, int NV>
 __global__ __launch_bounds__(kNormThreads<TPR>) void norm_bwd_kernel(NormBwd a, uint32_t parts) {
   constexpr uint32_t RPB = kNormThreads<TPR> / TPR;
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void norm_bwd_kernel(NormBwd a, 
   const uint32_t t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   const float inv_dim = 1.0f / static_cast<float>(a.dim);
   // The weights in LDS where registers for them would spill (128 a thread of 1024;
-  // 4096 x 16384 layer norm in bf16 108 us with the spills, 78 without).
+  // 4096 x 16384 layer norm in bf16 110 us with the spills, 79 without).
   constexpr bool kWeightsInLds = LAYER && TPR == 1024;
   __shared__ __align__(16) float w_lds[kWeightsInLds ? NV * TPR * 8 : 1];
   float w_reg[kWeightsInLds ? 1 : NV][8], dw[NV][8] = {}, db[LAYER ? NV : 1][8] = {};
@@ -438,8 +442,9 @@ __global__ __launch_bounds__(kJoinCols * kJoinSlices) void norm_join_kernel(Norm
 
 // Threads a row and groups of eight a thread, the smallest shape that holds a
 // row of `dim` elements; other rows take the kernels for any length.  Measured
-// on 16384 x 4096 (bf16, RMS, rows kept; us forward / backward): 256 threads
-// of 2 groups 65 / 71, 128 of 4 70 / 126, a wave of 8 94 / 136.
+// on 16384 x 4096 (bf16, RMS, rows kept; us forward with the rows read back /
+// backward): 256 threads of 2 groups 99 / 65, 128 of 4 103 / 77, a wave of 8
+// 124 / 103.
 constexpr uint32_t kNormLongest = 16384;
 constexpr bool norm_has_shape(uint64_t dim) { return dim >= 8 && dim <= kNormLongest; }
 #define LC_NORM_SHAPES(F)          \
@@ -452,8 +457,8 @@ constexpr bool norm_has_shape(uint64_t dim) { return dim >= 8 && dim <= kNormLon
   else F(1024, 2)
 
 // As many blocks as are resident at once, for more only add parts (16384 x
-// 4096 layer norm, 12 waves a CU 69 us, 16 81; RMS norm in bf16, which holds no
-// sums of db and narrower rows, 71 and 67).
+// 4096 layer norm in bf16, 12 waves a CU 69 us, 16 81; RMS norm, which holds no
+// sums of db, 66 and 65).
 NormParts norm_parts(uint64_t rows, uint64_t dim, bool light) {
   uint32_t tpr = kLongThreads, waves = 16;
   if (norm_has_shape(dim)) {
@@ -467,7 +472,7 @@ NormParts norm_parts(uint64_t rows, uint64_t dim, bool light) {
   const uint64_t items = (rows + p.rpb - 1) / p.rpb;
   const auto blocks_of = [&](uint32_t w) -> uint64_t { return 256 * (w > block_waves ? w / block_waves : 1); };
   // up to four rows a block the parts weigh more (1024 x 4096 RMS norm in bf16, 16
-  // waves a CU 17.7 us, 8 14.4)
+  // waves a CU 18.0 us of kernels, 8 14.6)
   const uint64_t most = blocks_of(waves > 8 && items <= 4 * blocks_of(8) ? 8 : waves);
   const uint64_t turns = (items + most - 1) / most;
   // few turns are dealt out evenly: 1025 over 768 blocks as two each for 513

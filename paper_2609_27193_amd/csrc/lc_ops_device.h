@@ -23,11 +23,14 @@ __host__ hipError_t launch_op(void (*kernel)(P...), dim3 grid, uint32_t threads,
 
 constexpr int kBf16 = 1;
 constexpr int kF32 = 2;
-// Rows that a kernel reads or writes once go past the caches where that is
-// faster, which is so for bf16, a lane's 16 bytes in one access (16384 x 4096,
-// us): norm with rows kept 65.8, its gradient 71.3, rows read back 36.7; streamed
-// 59.5, 69.4, 29.6.  Of fp32, whose 32 bytes a lane come in two halves, the norm
-// takes 114 and streamed 124, rows read back 64 and 99.
+// Rows in bf16 that a kernel reads or writes once go past the caches, a lane's 16
+// bytes in one access (the norm gradient's dx does not, see there).  16384 x 4096
+// from five sets of arrays in turn, us through the caches and past them: norm 55.3
+// and 52.6, with rows kept and read back 99.5 and 93.4, its gradient from x 83.2
+// and 74.5, from kept rows 72.3 and 68.5, rows kept and read back 70.0 and 66.5.
+// (Of one set over and over, what a cache still holds makes up for it: the norm
+// alone takes 43 and 50.)  fp32 rows, whose 32 bytes a lane come in two halves,
+// go through them (the norm 101 us, past them 107).
 template <int DT>
 constexpr bool kStreams = DT == kBf16;
 template <int DT>
@@ -198,8 +201,8 @@ __device__ __forceinline__ int in_group(uint32_t dim, uint32_t g) {
 }
 
 // Item `it` of a kernel whose blocks take rows: runs of 32 items per XCD, so that
-// neighbours meet in one L2 (65536 x 1024 kept in 8 bits 39.9 us, in runs 34.4;
-// 16384 x 4096 alike).  Beyond the dispatch limit, in order.
+// neighbours meet in one L2 (65536 x 1024 kept in 8 bits and read back 76.0 us, in
+// runs 70.4; rows of 4096, and norms, alike).  Beyond the dispatch limit, in order.
 __device__ __forceinline__ uint64_t row_item(uint64_t it, uint64_t items) {
   return items <= gridDim.x ? remap_xcd_runs<32>(static_cast<uint32_t>(it), static_cast<uint32_t>(items)) : it;
 }

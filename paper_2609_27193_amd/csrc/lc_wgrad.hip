@@ -7,9 +7,11 @@
 //
 // so the columns' scale and shift cost the main loop nothing.  Bound by the
 // matrix cores: 2 n k flops a token.  A kept element is 4 significant bits
-// times a power of two, so it is exact in bf16; a bf16 dY enters as it is, an
-// fp32 dY as the sum of three bf16 parts (8 of its 24 bits each), which keeps
-// every product exact.  Sums are fp32.
+// times a power of two, so it is exact in bf16 (below 2^-126 as far as its
+// subnormals hold it); a bf16 dY enters as it is, an fp32 dY as the sum of three
+// bf16 parts (8 of its 24 bits each), which keeps every product exact.  Sums are
+// fp32; scale and shift are applied to the two sums, so where X * scale and shift
+// cancel the error stays that of each.
 //
 // Both operands lie with the tokens, over which the product sums, as rows: a
 // tile goes to LDS as it lies and the transposing LDS reads give each lane the
@@ -142,9 +144,9 @@ __device__ __forceinline__ void wgrad_place(const WgradTiles& s, uint32_t tile, 
 }
 // Item b of the grid.  The whole tiles run first, then the parts; each in
 // contiguous eighths for the XCDs.  A part's tiles of 256 follow each other, so
-// that an XCD's blocks read the same tokens (16384 tokens x 1024 x 1024: 52.7 us
-// of kernel; a tile's parts after each other 55.5), of 128 a tile's parts (2048 x
-// 1024 x 1024 fp32: 29 us, the other way 34).
+// that an XCD's blocks read the same tokens (16384 tokens x 1024 x 1024: 62.3 us;
+// a tile's parts after each other 67), of 128 a tile's parts (2048 x 1024 x 1024
+// fp32: 33.8 us, the other way 36.9).
 __device__ __forceinline__ WgradItem wgrad_item(const WgradTiles& s, uint64_t rows, uint32_t b) {
   WgradItem w;
   w.whole = b < s.full;
@@ -359,7 +361,8 @@ __global__ __launch_bounds__(kThreads, 2) void wgrad_kernel(Wgrad a, WgradTiles 
       }
     };
     // The next kAhead steps' loads are on their way while one multiplies (of
-    // three parts a step, one: 8192 x 4096 x 4096 fp32 850 us, 900 with two).
+    // three parts a step, one: 2048 x 1024 x 1024 fp32 33.8 us, with two 35.7;
+    // 8192 x 4096 x 4096 867 and 868).
     constexpr int kAhead = ANY || P > 1 ? 1 : 3;
     Stage g[kAhead];
     if (t_end <= t_begin + kStep) {  // one step at most: nothing else is loaded
