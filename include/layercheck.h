@@ -321,6 +321,28 @@ typedef struct {
 lc_status lc_sgd_step_score(lc_ctx *c, int64_t step, const void *const *grads, int32_t grad_dtype,
                             const uint8_t *decay_mask, const lc_sgd_params *p);
 
+/* Hyper-parameters of one mixed step. */
+typedef struct {
+  lc_adamw_params adamw;     /* of the segments that ortho_mask leaves            */
+  double ortho_lr;           /* learning rate of the others, >= 0                 */
+  double ortho_weight_decay; /* their decoupled decay where decay_mask, >= 0      */
+} lc_muon_params;
+
+/* The optimizer step of a training that orthogonalises the updates of its
+ * matrices (lc_orthogonalize) and leaves the rest, embeddings, head, norms and
+ * biases, to AdamW.  A segment with ortho_mask 1 takes its entry of `grads` as the
+ * update o, in fp32 with one rounding per operation:
+ *   p_new = p * (1 - ortho_lr ortho_wd) - ortho_lr * o     (the decay only where decay_mask)
+ * and its moments are not touched: its exp_avg is the momentum that lc_orthogonalize
+ * keeps (so the records hold it), its exp_avg_sq is not in use.  A segment with
+ * ortho_mask 0 takes the step of lc_adamw_step_score.  The drift comes from both.
+ *   ortho_mask: host array [n_segments] of 0/1
+ * The other arguments, call sequence and errors as lc_adamw_step_score, whose bits
+ * this call gives with an ortho_mask of zeros, and those of lc_sgd_step_score with
+ * one of ones.  The layout has Adam moments.  Asynchronous. */
+lc_status lc_muon_step_score(lc_ctx *c, int64_t step, const void *const *grads, int32_t grad_dtype,
+                             const uint8_t *ortho_mask, const uint8_t *decay_mask, const lc_muon_params *p);
+
 /* ---- Persistence store (Section 3.5: reconstruction from persisted metadata) --
  * A directory of version files plus an append-only manifest recording the
  * persistence history: per version its step, its layer mask and its payload
@@ -557,6 +579,33 @@ lc_status lc_norm_backward(const lc_norm_params *params, const lc_matrix *dy, co
                            const float *rstd, const lc_saved_act *saved, const lc_matrix *dx, void *dweight,
                            void *dbias, int32_t grad_dtype, int32_t accumulate, void *workspace,
                            uint64_t workspace_bytes, void *stream);
+
+/* The norm of a block's input with the residual's addition before it:
+ *   h = x + residual, and mean, rstd, n and y of h as lc_norm_forward's of x.
+ * The sum is formed in fp32 and normalised so; h receives it in residual's dtype
+ * (NULL: it is not written).  residual and h are of x's dtype, or LC_DT_F32 beside
+ * bf16 layers.  y (x's shape and dtype) and y_saved, its 8-bit form, receive the
+ * result, each may be NULL, not both; y_saved is taken from the fp32 values, not
+ * from y.  `saved` (or NULL) keeps the normalised rows n, as in lc_norm_forward.
+ * With y_saved, lc_linear_wgrad takes y for the layer that follows (no col_scale
+ * and col_shift). */
+lc_status lc_residual_norm_forward(const lc_norm_params *params, const lc_matrix *x, const lc_matrix *residual,
+                                   const lc_matrix *h, const lc_matrix *y, float *mean, float *rstd,
+                                   const lc_saved_act *saved, const lc_saved_act *y_saved, void *stream);
+
+/* Its gradient.  dy is that of y; dh, the one that arrives at h beside the norm, is
+ * added:
+ *   dx = dresidual = dh + rstd * (g - mean(g) - n * mean(g * n))
+ *   dweight (+)= sum over rows of dy * n,  dbias (+)= sum over rows of dy
+ * with g, mean(g), n and the workspace (lc_norm_backward_workspace) as in
+ * lc_norm_backward, and exactly one of h and saved.  dh, h and dresidual are of one
+ * dtype: dy's, or LC_DT_F32.  dx is of dy's dtype.  Both are one gradient, in two
+ * types where these differ; each may be NULL, as may dweight and dbias. */
+lc_status lc_residual_norm_backward(const lc_norm_params *params, const lc_matrix *dy, const lc_matrix *dh,
+                                    const lc_matrix *h, const float *mean, const float *rstd,
+                                    const lc_saved_act *saved, const lc_matrix *dx, const lc_matrix *dresidual,
+                                    void *dweight, void *dbias, int32_t grad_dtype, int32_t accumulate,
+                                    void *workspace, uint64_t workspace_bytes, void *stream);
 
 /* The weight gradient of y = X W^T + bias, with X kept in 8 bits:
  *   dweight[n][k] (+)= sum over rows t of dy[t][n] * (X[t][k] * col_scale[k] + col_shift[k])

@@ -155,9 +155,11 @@ struct OptSeg {
 };
 
 // Per-call part: gradient address and weight-decay flag of each segment.
+constexpr uint32_t kGradDecay = 1;  // weight decay applies
+constexpr uint32_t kGradOrtho = 2;  // an orthogonalised update (the mixed step)
 struct GradSeg {
   uint64_t grad;
-  uint32_t decay;
+  uint32_t flags;
   uint32_t vec_ok;  // gradient aligned to 4 elements at element 0
 };
 
@@ -179,6 +181,12 @@ struct AdamScalars {
 // fp32 scalars of one SGD step: lr and the decoupled decay factor 1 - lr wd.
 struct SgdScalars {
   float lr, decay;
+};
+
+// Of one mixed step.
+struct MuonScalars {
+  AdamScalars adamw;
+  SgdScalars ortho;
 };
 
 // Written by the select kernel to pinned host memory, followed by the 0/1 mask
@@ -293,5 +301,7 @@ hipError_t launch_adamw(const DeviceTables& t, const InlineGrads& grads, int gra
                         const AdamScalars& sc, hipStream_t st);
 hipError_t launch_sgd(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
                       const SgdScalars& sc, hipStream_t st);
+hipError_t launch_muon(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
+                       const MuonScalars& sc, hipStream_t st);
 
 }  // namespace lc

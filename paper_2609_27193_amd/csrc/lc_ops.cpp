@@ -352,6 +352,155 @@ extern "C" lc_status lc_norm_backward(const lc_norm_params* params, const lc_mat
   return launched("lc_norm_backward", launch_norm_bwd(a, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+lc_status check_res_dtypes(int dtype, int res_dtype) {
+  // a bf16 stream beside fp32 layers would lose what the layers add
+  return res_dtype == dtype || res_dtype == LC_DT_F32 ? LC_OK
+                                                      : fail(LC_ERR_INVALID_ARG, "the residual must have x's dtype or LC_DT_F32");
+}
+}  // namespace
+
+extern "C" lc_status lc_residual_norm_forward(const lc_norm_params* params, const lc_matrix* x, const lc_matrix* residual,
+                                              const lc_matrix* h, const lc_matrix* y, float* mean, float* rstd,
+                                              const lc_saved_act* saved, const lc_saved_act* y_saved, void* stream) {
+  lc::TraceRange trace_("lc_residual_norm_forward");
+  LC_CHECK(check_norm(params));
+  LC_CHECK(check_matrix("x", x));
+  LC_CHECK(check_matrix("residual", residual));
+  LC_CHECK(check_shape("residual", residual->rows, residual->cols, x->rows, x->cols));
+  LC_CHECK(check_res_dtypes(x->dtype, residual->dtype));
+  if (h) {
+    LC_CHECK(check_matrix("h", h));
+    LC_CHECK(check_shape("h", h->rows, h->cols, x->rows, x->cols));
+    if (h->dtype != residual->dtype) return fail(LC_ERR_INVALID_ARG, "h has another dtype than residual");
+  }
+  if (!y && !y_saved) return fail(LC_ERR_INVALID_ARG, "y or y_saved must be given");
+  if (y) {
+    LC_CHECK(check_matrix("y", y));
+    LC_CHECK(check_shape("y", y->rows, y->cols, x->rows, x->cols));
+    if (y->dtype != x->dtype) return fail(LC_ERR_INVALID_ARG, "y has another dtype than x");
+  }
+  if (mean && params->kind == LC_NORM_RMS) return fail(LC_ERR_INVALID_ARG, "LC_NORM_RMS has no mean");
+  LC_CHECK(check_vector("mean", mean, 4));
+  LC_CHECK(check_vector("rstd", rstd, 4));
+  if (saved) {
+    LC_CHECK(check_saved("saved", saved));
+    LC_CHECK(check_shape("saved", saved->rows, saved->cols, x->rows, x->cols));
+  }
+  if (y_saved) {
+    LC_CHECK(check_saved("y_saved", y_saved));
+    LC_CHECK(check_shape("y_saved", y_saved->rows, y_saved->cols, x->rows, x->cols));
+  }
+  const uint64_t param_bytes = x->cols * esz_of(params->param_dtype);
+  Area y_codes = codes_of(y_saved), y_scales = scales_of(y_saved);
+  y_codes.name = "y_saved's codes";
+  y_scales.name = "y_saved's scales";
+  const Area areas[] = {area_of("h", h), area_of("y", y), flat("mean", mean, x->rows * 4), flat("rstd", rstd, x->rows * 4),
+                        codes_of(saved), scales_of(saved), y_codes, y_scales, area_of("x", x),
+                        area_of("residual", residual), flat("weight", params->weight, param_bytes),
+                        flat("bias", params->bias, param_bytes)};
+  LC_CHECK(check_apart(areas, 8));
+  LC_CHECK(check_stream(stream));
+  ResNormFwd a{};
+  a.x = rows_of(x);
+  a.y = rows_of(y);
+  a.kept = kept_of(saved);
+  a.weight = addr(params->weight);
+  a.bias = addr(params->bias);
+  a.mean = mean;
+  a.rstd = rstd;
+  a.rows = x->rows;
+  a.dim = static_cast<uint32_t>(x->cols);
+  a.eps = static_cast<float>(params->eps);
+  a.dtype = x->dtype;
+  a.param_dtype = params->param_dtype;
+  a.layer = params->kind == LC_NORM_LAYER;
+  a.res = rows_of(residual);
+  a.h = rows_of(h);
+  a.y8 = kept_of(y_saved);
+  a.res_dtype = residual->dtype;
+  return launched("lc_residual_norm_forward", launch_res_norm_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+extern "C" lc_status lc_residual_norm_backward(const lc_norm_params* params, const lc_matrix* dy, const lc_matrix* dh,
+                                               const lc_matrix* h, const float* mean, const float* rstd,
+                                               const lc_saved_act* saved, const lc_matrix* dx,
+                                               const lc_matrix* dresidual, void* dweight, void* dbias,
+                                               int32_t grad_dtype, int32_t accumulate, void* workspace,
+                                               uint64_t workspace_bytes, void* stream) {
+  lc::TraceRange trace_("lc_residual_norm_backward");
+  LC_CHECK(check_norm(params));
+  LC_CHECK(check_matrix("dy", dy));
+  LC_CHECK(check_matrix("dh", dh));
+  LC_CHECK(check_shape("dh", dh->rows, dh->cols, dy->rows, dy->cols));
+  LC_CHECK(check_res_dtypes(dy->dtype, dh->dtype));
+  if ((h != nullptr) == (saved != nullptr)) return fail(LC_ERR_INVALID_ARG, "exactly one of h and saved must be given");
+  if (h) {
+    LC_CHECK(check_matrix("h", h));
+    LC_CHECK(check_shape("h", h->rows, h->cols, dy->rows, dy->cols));
+    if (h->dtype != dh->dtype) return fail(LC_ERR_INVALID_ARG, "h has another dtype than dh");
+  } else {
+    LC_CHECK(check_saved("saved", saved));
+    LC_CHECK(check_shape("saved", saved->rows, saved->cols, dy->rows, dy->cols));
+  }
+  const bool wants_mean = h && params->kind == LC_NORM_LAYER;
+  if (!wants_mean && mean) return fail(LC_ERR_INVALID_ARG, "mean goes with h and LC_NORM_LAYER only");
+  if (dy->rows && ((wants_mean && !mean) || !rstd)) return fail(LC_ERR_INVALID_ARG, "mean or rstd is NULL");
+  LC_CHECK(check_vector("mean", mean, 4));
+  LC_CHECK(check_vector("rstd", rstd, 4));
+  if (dx) {
+    LC_CHECK(check_matrix("dx", dx));
+    LC_CHECK(check_shape("dx", dx->rows, dx->cols, dy->rows, dy->cols));
+    if (dx->dtype != dy->dtype) return fail(LC_ERR_INVALID_ARG, "dx has another dtype than dy");
+  }
+  if (dresidual) {
+    LC_CHECK(check_matrix("dresidual", dresidual));
+    LC_CHECK(check_shape("dresidual", dresidual->rows, dresidual->cols, dy->rows, dy->cols));
+    if (dresidual->dtype != dh->dtype) return fail(LC_ERR_INVALID_ARG, "dresidual has another dtype than dh");
+  }
+  if (dbias && params->kind == LC_NORM_RMS) return fail(LC_ERR_INVALID_ARG, "LC_NORM_RMS has no bias");
+  LC_CHECK(check_flag("accumulate", accumulate));
+  const bool grads = dweight || dbias;
+  if (grads) {
+    if (!dtype_ok(grad_dtype)) return fail(LC_ERR_INVALID_ARG, "unknown gradient dtype %d", grad_dtype);
+    LC_CHECK(check_vector("dweight", dweight, esz_of(grad_dtype)));
+    LC_CHECK(check_vector("dbias", dbias, esz_of(grad_dtype)));
+  }
+  const uint64_t need = grads ? norm_bwd_workspace(dy->rows, dy->cols) : 0;
+  LC_CHECK(check_space(workspace, workspace_bytes, need));
+  const uint64_t param_bytes = dy->cols * esz_of(params->param_dtype);
+  const uint64_t grad_bytes = grads ? dy->cols * esz_of(grad_dtype) : 0;
+  const Area areas[] = {area_of("dx", dx), area_of("dresidual", dresidual), flat("dweight", dweight, grad_bytes),
+                        flat("dbias", dbias, grad_bytes), flat("workspace", workspace, need), area_of("dy", dy),
+                        area_of("dh", dh), area_of("h", h), codes_of(saved), scales_of(saved),
+                        flat("mean", mean, dy->rows * 4), flat("rstd", rstd, dy->rows * 4),
+                        flat("weight", params->weight, param_bytes)};
+  LC_CHECK(check_apart(areas, 5));
+  LC_CHECK(check_stream(stream));
+  ResNormBwd a{};
+  a.dy = rows_of(dy);
+  a.x = rows_of(h);
+  a.dx = rows_of(dx);
+  a.kept = kept_of(saved);
+  a.weight = addr(params->weight);
+  a.mean = mean;
+  a.rstd = rstd;
+  a.part = grads ? static_cast<float*>(workspace) : nullptr;
+  a.rows = dy->rows;
+  a.dim = static_cast<uint32_t>(dy->cols);
+  a.dtype = dy->dtype;
+  a.param_dtype = params->param_dtype;
+  a.layer = params->kind == LC_NORM_LAYER;
+  a.dweight = addr(dweight);
+  a.dbias = addr(dbias);
+  a.grad_dtype = grad_dtype;
+  a.accumulate = accumulate;
+  a.dh = rows_of(dh);
+  a.dres = rows_of(dresidual);
+  a.res_dtype = dh->dtype;
+  return launched("lc_residual_norm_backward", launch_res_norm_bwd(a, static_cast<hipStream_t>(stream)));
+}
+
 extern "C" lc_status lc_act_save(const lc_matrix* x, const lc_saved_act* saved, void* stream) {
   lc::TraceRange trace_("lc_act_save");
   LC_CHECK(check_matrix("x", x));

@@ -1,6 +1,7 @@
 // Arguments and launchers of the training operators (embedding, norm, kept
 // activations, linear weight gradient), shared by their entry points
-// (lc_ops.cpp) and their kernels (lc_embed.hip, lc_norm.hip, lc_wgrad.hip).
+// (lc_ops.cpp) and their kernels (lc_embed.hip, lc_norm.hip, lc_resnorm.hip,
+// lc_act.hip, lc_wgrad.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -79,6 +80,21 @@ struct NormBwd {
 };
 uint64_t norm_bwd_workspace(uint64_t rows, uint64_t dim);
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t st);
+
+// The norm of x + res; x, y and weight as above (y.data 0: not written).
+struct ResNormFwd : NormFwd {
+  Rows res, h;    // h.data 0: the sum is not written
+  Kept y8;        // codes 0: y is not written in 8 bits
+  int res_dtype;  // of res and h
+};
+hipError_t launch_res_norm_fwd(const ResNormFwd& a, hipStream_t st);
+
+// Its gradient; `x` is the sum h.
+struct ResNormBwd : NormBwd {
+  Rows dh, dres;  // dres.data 0: none
+  int res_dtype;  // of h, dh and dres
+};
+hipError_t launch_res_norm_bwd(const ResNormBwd& a, hipStream_t st);
 
 struct ActCopy {
   Rows x;  // the activation, read or written

@@ -1,11 +1,13 @@
 // HIP kernels of the optimizer steps that yield the drift statistic (Section
 // 3.4: the drift is taken from the optimizer's own update): AdamW, as the
-// paper trains, and plain SGD, which Section 4.7 notes the method carries
-// over to.  One pass over the optimizer state per step; per chunk of the
-// score layout the kernel updates the parameters and writes the Eq. 1
-// partial sums of |p_new - p| and |p|, which the finalize kernel turns into
-// u and Delta.  Streaming rules as in lc_kernels.hip (full chunks through
-// buffer resources, ragged ones through global pointers).
+// paper trains, plain SGD, which Section 4.7 notes the method carries over
+// to, and a mixed step, in which segments with an orthogonalised update take
+// it as SGD takes a gradient and the others take AdamW.  One pass over the
+// optimizer state per step; per chunk of the score layout the kernel updates
+// the parameters and writes the Eq. 1 partial sums of |p_new - p| and |p|,
+// which the finalize kernel turns into u and Delta.  Streaming rules as in
+// lc_kernels.hip (full chunks through buffer resources, ragged ones through
+// global pointers).
 #include "lc_device.h"
 
 namespace lc {
@@ -13,6 +15,7 @@ namespace {
 
 constexpr int kAdamW = 0;
 constexpr int kSGD = 1;
+constexpr int kMuon = 2;  // each segment either of the two
 
 // Threads per block: a block takes its whole tile in one burst of loads, so
 // 512 threads of two groups for the 4096 elements of a bf16 chunk (256 threads
@@ -244,7 +247,7 @@ __device__ __forceinline__ void optim_elem(const OptSeg& sg, const GradSeg& gs, 
   const float po = MASTER ? ((const g_f32*)sg.master)[e]
                           : w_load<WDT>(reinterpret_cast<const uint8_t*>(sg.w), e);
   const float gv = g_load<GDT>(reinterpret_cast<const uint8_t*>(gs.grad), e);
-  const bool decay = gs.decay != 0;
+  const bool decay = (gs.flags & kGradDecay) != 0;
   float x;
   if constexpr (OPT == kAdamW) {
     g_f32* mp = (g_f32*)sg.m + e;
@@ -272,20 +275,16 @@ struct OptTables {
 };
 
 template <int OPT, int WDT, int GDT, bool MASTER, typename SC>
-__device__ __forceinline__ void optim_chunk(const OptTables& t, const InlineGrads& ig, const SC& sc, uint32_t c) {
+__device__ __forceinline__ void optim_chunk_of(const OptTables& t, const OptSeg& sg, const GradSeg& gs, const SC& sc,
+                                               uint32_t c) {
   constexpr uint32_t WSZ = WDT == 1 ? 2 : 4, GSZ = GDT == 1 ? 2 : 4;
   constexpr uint32_t CE = kChunkBytes / WSZ;  // elements per chunk (the score chunks)
   const uint32_t tid = threadIdx.x;
-  const uint32_t si = t.chunk_seg[c];
-  const OptSeg sg = t.opt_segs[si];
-  // a constant either way, so that the lookup stays a scalar load
-  const c_GradSeg* gt = (const c_GradSeg*)(t.grad_segs ? t.grad_segs : ig.g);
-  const GradSeg gs{gt[si].grad, gt[si].decay, gt[si].vec_ok};
   const uint32_t k = c - sg.chunk_begin;
   const uint64_t e0 = static_cast<uint64_t>(k) * CE + sg.head;  // the chunk's tile
   const uint64_t rem = sg.numel > e0 ? sg.numel - e0 : 0;
   const uint32_t n = rem < CE ? static_cast<uint32_t>(rem) : CE;
-  const bool decay = gs.decay != 0;
+  const bool decay = (gs.flags & kGradDecay) != 0;
   const bool pairs = sg.form == kOptPairs && gs.vec_ok;
   ChunkPtrs cp;
   cp.w = reinterpret_cast<uint8_t*>(sg.w) + e0 * WSZ;
@@ -313,6 +312,21 @@ __device__ __forceinline__ void optim_chunk(const OptTables& t, const InlineGrad
   if (k == 0 && tid < sg.head && tid < sg.numel) optim_elem<OPT, WDT, GDT, MASTER>(sg, gs, sc, tid, a, b);
   block_sum2<kOptThreads<WDT, MASTER>>(a, b);
   if (tid == kOptThreads<WDT, MASTER> - 1) t.partials[c] = make_double2(a, b);
+}
+
+template <int OPT, int WDT, int GDT, bool MASTER, typename SC>
+__device__ __forceinline__ void optim_chunk(const OptTables& t, const InlineGrads& ig, const SC& sc, uint32_t c) {
+  const uint32_t si = t.chunk_seg[c];
+  const OptSeg sg = t.opt_segs[si];
+  // a constant either way, so that the lookup stays a scalar load
+  const c_GradSeg* gt = (const c_GradSeg*)(t.grad_segs ? t.grad_segs : ig.g);
+  const GradSeg gs{gt[si].grad, gt[si].flags, gt[si].vec_ok};
+  if constexpr (OPT == kMuon) {  // the same for the whole block
+    if (gs.flags & kGradOrtho) optim_chunk_of<kSGD, WDT, GDT, MASTER>(t, sg, gs, sc.ortho, c);
+    else optim_chunk_of<kAdamW, WDT, GDT, MASTER>(t, sg, gs, sc.adamw, c);
+  } else {
+    optim_chunk_of<OPT, WDT, GDT, MASTER>(t, sg, gs, sc, c);
+  }
 }
 
 template <int OPT, int WDT, int GDT, bool MASTER, bool LOOP, typename SC>
@@ -356,7 +370,7 @@ void launch_optim_t(const DeviceTables& t, const InlineGrads& ig, const SC& sc, 
   const uint32_t g = grid_for(t.n_chunks, kOptThreads<WDT, MASTER>);
   constexpr uint32_t CE = kChunkBytes / (WDT == 1 ? 2 : 4);
   constexpr uint32_t wsz = WDT == 1 ? 2 : 4;
-  constexpr uint32_t tile = CE * ((MASTER ? 8 + wsz : 2 * wsz) + (OPT == kAdamW ? 16 : 0) + (GDT == 1 ? 2 : 4));
+  constexpr uint32_t tile = CE * ((MASTER ? 8 + wsz : 2 * wsz) + (OPT == kSGD ? 0 : 16) + (GDT == 1 ? 2 : 4));
   constexpr uint32_t fit = (kOptBytesPerCU + tile / 2) / tile;
   constexpr uint32_t blocks = LC_OPT_BLOCKS_PER_CU ? LC_OPT_BLOCKS_PER_CU
                               : tile >= kOptBytesPerCU ? 1 : fit < 2 ? 2 : fit;
@@ -388,6 +402,12 @@ void launch_optim(const DeviceTables& t, const InlineGrads& ig, int grad_dtype, 
 hipError_t launch_adamw(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
                         const AdamScalars& sc, hipStream_t st) {
   launch_optim<kAdamW>(t, grads, grad_dtype, has_master, sc, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_muon(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
+                       const MuonScalars& sc, hipStream_t st) {
+  launch_optim<kMuon>(t, grads, grad_dtype, has_master, sc, st);
   return hipGetLastError();
 }
 

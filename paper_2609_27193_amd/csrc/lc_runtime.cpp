@@ -947,7 +947,7 @@ namespace {
 // table, its way to the device, and the call-order state afterwards (the
 // caller launches its kernel between the two halves).
 lc_status optimizer_begin(lc_ctx* c, int64_t step, const void* const* grads, int32_t grad_dtype,
-                          const uint8_t* decay_mask) {
+                          const uint8_t* decay_mask, const uint8_t* ortho_mask = nullptr) {
   if (!grads) return fail(LC_ERR_INVALID_ARG, "grads must be non-NULL");
   if (grad_dtype != LC_DT_BF16 && grad_dtype != LC_DT_F32)
     return fail(LC_ERR_INVALID_ARG, "unknown gradient dtype %d", grad_dtype);
@@ -964,6 +964,7 @@ lc_status optimizer_begin(lc_ctx* c, int64_t step, const void* const* grads, int
     if (!g) return fail(LC_ERR_INVALID_ARG, "gradient of segment %zu is NULL", i);
     if (g % gsz) return fail(LC_ERR_INVALID_ARG, "gradient of segment %zu is misaligned", i);
     if (decay_mask && decay_mask[i] > 1) return fail(LC_ERR_INVALID_ARG, "decay_mask must be 0/1");
+    if (ortho_mask && ortho_mask[i] > 1) return fail(LC_ERR_INVALID_ARG, "ortho_mask must be 0/1");
   }
   const bool fetched = ns > kInlineGrads;
   // the pinned table may still feed the previous call's fetch (a stream that
@@ -974,7 +975,7 @@ lc_status optimizer_begin(lc_ctx* c, int64_t step, const void* const* grads, int
   for (size_t i = 0; i < ns; ++i) {
     const uint64_t g = reinterpret_cast<uint64_t>(grads[i]);
     table[i].grad = g;
-    table[i].decay = decay_mask ? decay_mask[i] : 1u;
+    table[i].flags = (!decay_mask || decay_mask[i] ? kGradDecay : 0u) | (ortho_mask && ortho_mask[i] ? kGradOrtho : 0u);
     table[i].vec_ok = g % (4 * gsz) == 0 ? 1u : 0u;
   }
   if (fetched) {
@@ -998,16 +999,8 @@ lc_status optimizer_end(lc_ctx* c, int64_t step) {
   return LC_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-lc_status lc_adamw_step_score(lc_ctx* c, int64_t step, const void* const* grads, int32_t grad_dtype,
-                              const uint8_t* decay_mask, const lc_adamw_params* p) {
-  lc::TraceRange trace_("lc_adamw_step_score");
-  lc_status st = check_ctx(c);
-  if (st != LC_OK) return st;
-  if (!p) return fail(LC_ERR_INVALID_ARG, "params must be non-NULL");
+// The values of one AdamW step, and its scalars.
+lc_status check_adamw(const lc_adamw_params* p) {
   if (!(p->lr >= 0.0) || !std::isfinite(p->lr)) return fail(LC_ERR_INVALID_ARG, "lr must be finite and >= 0");
   if (!(p->beta1 >= 0.0 && p->beta1 < 1.0) || !(p->beta2 >= 0.0 && p->beta2 < 1.0))
     return fail(LC_ERR_INVALID_ARG, "betas must lie in [0, 1)");
@@ -1015,9 +1008,9 @@ lc_status lc_adamw_step_score(lc_ctx* c, int64_t step, const void* const* grads,
   if (!(p->weight_decay >= 0.0) || !std::isfinite(p->weight_decay))
     return fail(LC_ERR_INVALID_ARG, "weight_decay must be finite and >= 0");
   if (p->adam_step < 1) return fail(LC_ERR_INVALID_ARG, "adam_step must be >= 1");
-  if (!c->L.has_moments) return fail(LC_ERR_BAD_STATE, "the layout has no Adam moments");
-  st = optimizer_begin(c, step, grads, grad_dtype, decay_mask);
-  if (st != LC_OK) return st;
+  return LC_OK;
+}
+AdamScalars adamw_scalars(const lc_adamw_params* p) {
   const double t = static_cast<double>(p->adam_step);
   AdamScalars sc;
   sc.b1 = static_cast<float>(p->beta1);
@@ -1029,6 +1022,25 @@ lc_status lc_adamw_step_score(lc_ctx* c, int64_t step, const void* const* grads,
   sc.eps = static_cast<float>(p->eps);
   sc.lr = static_cast<float>(p->lr);
   sc.decay = static_cast<float>(1.0 - p->lr * p->weight_decay);
+  return sc;
+}
+
+}  // namespace
+
+extern "C" {
+
+lc_status lc_adamw_step_score(lc_ctx* c, int64_t step, const void* const* grads, int32_t grad_dtype,
+                              const uint8_t* decay_mask, const lc_adamw_params* p) {
+  lc::TraceRange trace_("lc_adamw_step_score");
+  lc_status st = check_ctx(c);
+  if (st != LC_OK) return st;
+  if (!p) return fail(LC_ERR_INVALID_ARG, "params must be non-NULL");
+  st = check_adamw(p);
+  if (st != LC_OK) return st;
+  if (!c->L.has_moments) return fail(LC_ERR_BAD_STATE, "the layout has no Adam moments");
+  st = optimizer_begin(c, step, grads, grad_dtype, decay_mask);
+  if (st != LC_OK) return st;
+  const AdamScalars sc = adamw_scalars(p);
   LC_HIP(c, launch_adamw(c->dt, c->inline_grads, grad_dtype, c->L.has_master ? 1 : 0, sc, c->stream));
   return optimizer_end(c, step);
 }
@@ -1048,6 +1060,30 @@ lc_status lc_sgd_step_score(lc_ctx* c, int64_t step, const void* const* grads, i
   sc.lr = static_cast<float>(p->lr);
   sc.decay = static_cast<float>(1.0 - p->lr * p->weight_decay);
   LC_HIP(c, launch_sgd(c->dt, c->inline_grads, grad_dtype, c->L.has_master ? 1 : 0, sc, c->stream));
+  return optimizer_end(c, step);
+}
+
+lc_status lc_muon_step_score(lc_ctx* c, int64_t step, const void* const* grads, int32_t grad_dtype,
+                             const uint8_t* ortho_mask, const uint8_t* decay_mask, const lc_muon_params* p) {
+  lc::TraceRange trace_("lc_muon_step_score");
+  lc_status st = check_ctx(c);
+  if (st != LC_OK) return st;
+  if (!p) return fail(LC_ERR_INVALID_ARG, "params must be non-NULL");
+  if (!ortho_mask) return fail(LC_ERR_INVALID_ARG, "ortho_mask must be non-NULL");
+  st = check_adamw(&p->adamw);
+  if (st != LC_OK) return st;
+  if (!(p->ortho_lr >= 0.0) || !std::isfinite(p->ortho_lr))
+    return fail(LC_ERR_INVALID_ARG, "ortho_lr must be finite and >= 0");
+  if (!(p->ortho_weight_decay >= 0.0) || !std::isfinite(p->ortho_weight_decay))
+    return fail(LC_ERR_INVALID_ARG, "ortho_weight_decay must be finite and >= 0");
+  if (!c->L.has_moments) return fail(LC_ERR_BAD_STATE, "the layout has no Adam moments");
+  st = optimizer_begin(c, step, grads, grad_dtype, decay_mask, ortho_mask);
+  if (st != LC_OK) return st;
+  MuonScalars sc;
+  sc.adamw = adamw_scalars(&p->adamw);
+  sc.ortho.lr = static_cast<float>(p->ortho_lr);
+  sc.ortho.decay = static_cast<float>(1.0 - p->ortho_lr * p->ortho_weight_decay);
+  LC_HIP(c, launch_muon(c->dt, c->inline_grads, grad_dtype, c->L.has_master ? 1 : 0, sc, c->stream));
   return optimizer_end(c, step);
 }
 

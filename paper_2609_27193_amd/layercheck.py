@@ -37,7 +37,7 @@ EXPORTED = ("lc_query_build", "lc_query_layout", "lc_init_layout", "lc_score_lay
             "lc_read_state", "lc_record_bytes", "lc_destroy", "lc_last_error", "lc_score_layers_static",
             "lc_embedding_forward", "lc_embedding_backward", "lc_embedding_backward_workspace", "lc_act_save",
             "lc_act_load", "lc_norm_forward", "lc_norm_backward", "lc_norm_backward_workspace", "lc_linear_wgrad",
-            "lc_linear_wgrad_workspace")
+            "lc_linear_wgrad_workspace", "lc_residual_norm_forward", "lc_residual_norm_backward", "lc_muon_step_score")
 
 
 class lc_segment(C.Structure):
@@ -81,6 +81,10 @@ class lc_adamw_params(C.Structure):
 
 class lc_sgd_params(C.Structure):
     _fields_ = [("lr", C.c_double), ("weight_decay", C.c_double)]
+
+
+class lc_muon_params(C.Structure):
+    _fields_ = [("adamw", lc_adamw_params), ("ortho_lr", C.c_double), ("ortho_weight_decay", C.c_double)]
 
 
 class lc_matrix(C.Structure):
@@ -130,6 +134,8 @@ def load_library(path: str = LIB_PATH):
                                               P(lc_adamw_params)]),
             "lc_sgd_step_score": (C.c_int, [C.c_void_p, C.c_int64, P(C.c_void_p), C.c_int32, P(C.c_uint8),
                                             P(lc_sgd_params)]),
+            "lc_muon_step_score": (C.c_int, [C.c_void_p, C.c_int64, P(C.c_void_p), C.c_int32, P(C.c_uint8), P(C.c_uint8),
+                                             P(lc_muon_params)]),
             "lc_store_open": (C.c_int, [C.c_char_p, C.c_uint32, P(C.c_uint64), C.c_uint64, P(C.c_void_p)]),
             "lc_store_append": (C.c_int, [C.c_void_p, C.c_int64, P(C.c_uint8), C.c_void_p, C.c_uint64,
                                           C.c_void_p]),
@@ -160,6 +166,11 @@ def load_library(path: str = LIB_PATH):
             "lc_norm_backward": (C.c_int, [P(lc_norm_params), P(lc_matrix), P(lc_matrix), C.c_void_p, C.c_void_p,
                                            P(lc_saved_act), P(lc_matrix), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                            C.c_void_p, C.c_uint64, C.c_void_p]),
+            "lc_residual_norm_forward": (C.c_int, [P(lc_norm_params), P(lc_matrix), P(lc_matrix), P(lc_matrix), P(lc_matrix),
+                                                   C.c_void_p, C.c_void_p, P(lc_saved_act), P(lc_saved_act), C.c_void_p]),
+            "lc_residual_norm_backward": (C.c_int, [P(lc_norm_params), P(lc_matrix), P(lc_matrix), P(lc_matrix), C.c_void_p,
+                                                    C.c_void_p, P(lc_saved_act), P(lc_matrix), P(lc_matrix), C.c_void_p,
+                                                    C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
             "lc_linear_wgrad_workspace": (C.c_uint64, [C.c_uint64, C.c_uint64, C.c_uint64]),
             "lc_linear_wgrad": (C.c_int, [P(lc_matrix), P(lc_saved_act), C.c_void_p, C.c_void_p, C.c_int32,
                                           P(lc_matrix), C.c_void_p, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
@@ -325,6 +336,23 @@ def lc_sgd_step_score(ctx, step: int, grads: Sequence[int], grad_dtype: int, lr:
     _check(load_library().lc_sgd_step_score(ctx, step, g, grad_dtype, dm, C.byref(prm)), "lc_sgd_step_score")
 
 
+def _mask(flags: Sequence[int]):
+    """A mask of 0/1, and what keeps its memory."""
+    a = np.ascontiguousarray(flags, dtype=np.uint8)
+    return a.ctypes.data_as(C.POINTER(C.c_uint8)), a
+
+
+def lc_muon_step_score(ctx, step: int, grads: Sequence[int], grad_dtype: int, ortho_mask: Sequence[int], lr: float,
+                       beta1: float, beta2: float, eps: float, weight_decay: float, adam_step: int, ortho_lr: float,
+                       ortho_weight_decay: float = 0.0, decay_mask: Optional[Sequence[int]] = None) -> None:
+    """grads: one device address per segment, in layout order: an update where ``ortho_mask``, else a gradient."""
+    g = _addresses(grads)
+    om, _ortho = _mask(ortho_mask)
+    dm, _decay = (None, None) if decay_mask is None else _mask(decay_mask)
+    prm = lc_muon_params(lc_adamw_params(lr, beta1, beta2, eps, weight_decay, adam_step), ortho_lr, ortho_weight_decay)
+    _check(load_library().lc_muon_step_score(ctx, step, g, grad_dtype, om, dm, C.byref(prm)), "lc_muon_step_score")
+
+
 class Store:
     """Persistence store (a directory of version files and a manifest)."""
 
@@ -484,6 +512,25 @@ def lc_norm_backward(params: lc_norm_params, dy: lc_matrix, rstd: int, dx: Optio
     _check(load_library().lc_norm_backward(params, dy, x, mean or None, rstd or None, saved, dx, dweight or None,
                                            dbias or None, grad_dtype, int(accumulate), workspace or None,
                                            workspace_bytes, stream or None), "lc_norm_backward")
+
+
+def lc_residual_norm_forward(params: lc_norm_params, x: lc_matrix, residual: lc_matrix, h: Optional[lc_matrix],
+                             y: Optional[lc_matrix] = None, mean: Optional[int] = None, rstd: Optional[int] = None,
+                             saved: Optional[lc_saved_act] = None, y_saved: Optional[lc_saved_act] = None,
+                             stream: int = 0) -> None:
+    _check(load_library().lc_residual_norm_forward(params, x, residual, h, y, mean or None, rstd or None, saved, y_saved,
+                                                   stream or None), "lc_residual_norm_forward")
+
+
+def lc_residual_norm_backward(params: lc_norm_params, dy: lc_matrix, dh: lc_matrix, rstd: int, dx: Optional[lc_matrix],
+                              dresidual: Optional[lc_matrix], dweight: Optional[int], dbias: Optional[int], grad_dtype: int,
+                              workspace: int, workspace_bytes: int, h: Optional[lc_matrix] = None, mean: Optional[int] = None,
+                              saved: Optional[lc_saved_act] = None, accumulate: bool = False, stream: int = 0) -> None:
+    """The normalised rows come from ``h`` (with ``mean`` for LC_NORM_LAYER) or from ``saved``."""
+    _check(load_library().lc_residual_norm_backward(params, dy, dh, h, mean or None, rstd or None, saved, dx, dresidual,
+                                                    dweight or None, dbias or None, grad_dtype, int(accumulate),
+                                                    workspace or None, workspace_bytes, stream or None),
+           "lc_residual_norm_backward")
 
 
 def lc_linear_wgrad_workspace(rows: int, n: int, k: int) -> int:
