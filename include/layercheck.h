@@ -621,6 +621,39 @@ lc_status lc_linear_wgrad(const lc_matrix *dy, const lc_saved_act *saved, const 
                           const void *col_shift, int32_t param_dtype, const lc_matrix *dweight, void *dbias,
                           int32_t accumulate, void *workspace, uint64_t workspace_bytes, void *stream);
 
+typedef struct {
+  uint32_t steps;      /* Newton-Schulz steps, 1 to 32                             */
+  int32_t nesterov;    /* 0 or 1                                                   */
+  double momentum;     /* mu, in [0, 1); not looked at without momenta             */
+  double eps;          /* added to the norm, finite and >= 0 (e.g. 1e-7)           */
+  double scale;        /* of the result, finite (e.g. 0.2 sqrt(max(rows, cols)))   */
+  const double *coefs; /* host [steps][3]: a, b, c of each step; NULL: 3.4445,
+                          -4.7750, 2.0315 for every one                            */
+} lc_orthogonalize_params;
+
+/* The update of an optimizer that orthogonalises it, for up to 64 matrices of one
+ * shape (each side at most 65536).  For each, in fp32 or wider,
+ *   buf <- g + mu * buf;  u = g + mu * buf (nesterov) or buf;  X = u / (|u| + eps)
+ *   steps times:  A = X X^T,  X <- a X + (b A + c A A) X
+ *   out = scale * X
+ * with |u| the square root of the sum of u's squares (in 64 bits) and, of a matrix
+ * with more rows than columns, X^T in X's place.  Without momenta (NULL) u = g.  The
+ * gradients are of one dtype, the momenta fp32 (the exp_avg of their segments, so
+ * that records hold them; strides as in memory), the results of one dtype: with
+ * LC_DT_BF16 the steps hold X, A and their products' operands to 11 bits, about what
+ * a gradient in bf16 holds of itself, with LC_DT_F32 to 22 bits, in three times the
+ * products.  Errors are relative to the largest singular value, and the steps raise
+ * the small ones by up to `a` each.  Coefficients that let a singular value grow
+ * beyond 2^30 are refused.  A matrix of zeros gives zeros; one that holds an infinity
+ * or a NaN gives NaN throughout (its momentum holds them where they were), and the
+ * matrices beside it are as ever.  The results are what lc_muon_step_score takes.
+ * The workspace is that of the matrices which are worked on at once, and goes by the
+ * results' dtype. */
+uint64_t lc_orthogonalize_workspace(uint32_t n_matrices, uint64_t rows, uint64_t cols, int32_t out_dtype);
+lc_status lc_orthogonalize(const lc_orthogonalize_params *params, uint32_t n_matrices, const lc_matrix *grads,
+                           const lc_matrix *momenta, const lc_matrix *out, void *workspace, uint64_t workspace_bytes,
+                           void *stream);
+
 /* Message for the last failing call on this thread ("" if none). */
 const char *lc_last_error(void);
 

@@ -13,7 +13,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblayercheck.so")
 SOURCES = ["lc_runtime.cpp", "lc_store.cpp", "lc_kernels.hip", "lc_optim.hip", "lc_noalloc.hip",
-           "lc_ops.cpp", "lc_embed.hip", "lc_norm.hip", "lc_resnorm.hip", "lc_act.hip", "lc_wgrad.hip"]
+           "lc_ops.cpp", "lc_embed.hip", "lc_norm.hip", "lc_resnorm.hip", "lc_act.hip", "lc_wgrad.hip",
+           "lc_ortho.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

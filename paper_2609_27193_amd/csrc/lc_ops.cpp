@@ -1,9 +1,10 @@
-// Entry points of the training operators: embedding, norms, kept activations
-// and the linear weight gradient.  Host only: everything is checked before
+// Entry points of the training operators: embedding, norms, kept activations,
+// the linear weight gradient and the orthogonalised update.  Host only: everything is checked before
 // anything is enqueued, and the workspace is the caller's, so a call allocates
 // nothing and may be captured into a graph.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "layercheck.h"
@@ -570,4 +571,108 @@ extern "C" lc_status lc_linear_wgrad(const lc_matrix* dy, const lc_saved_act* sa
   a.accumulate = accumulate;
   a.ws = static_cast<uint8_t*>(workspace);
   return launched("lc_linear_wgrad", launch_wgrad(a, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+constexpr double kOrthoDefault[3] = {3.4445, -4.7750, 2.0315};
+constexpr uint32_t kOrthoSteps = 32;
+
+lc_status check_ortho(const lc_orthogonalize_params* p, double (&coefs)[3 * kOrthoSteps]) {
+  if (!p) return fail(LC_ERR_INVALID_ARG, "params is NULL");
+  if (p->steps < 1 || p->steps > kOrthoSteps) return fail(LC_ERR_INVALID_ARG, "steps must lie in [1, %u]", kOrthoSteps);
+  LC_CHECK(check_flag("nesterov", p->nesterov));
+  if (!(p->momentum >= 0.0 && p->momentum < 1.0)) return fail(LC_ERR_INVALID_ARG, "momentum must lie in [0, 1)");
+  if (!(p->eps >= 0.0) || !std::isfinite(p->eps)) return fail(LC_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (!std::isfinite(static_cast<float>(p->scale))) return fail(LC_ERR_INVALID_ARG, "scale must be finite");
+  for (uint32_t i = 0; i < 3 * p->steps; ++i) {
+    coefs[i] = p->coefs ? p->coefs[i] : kOrthoDefault[i % 3];
+    if (!std::isfinite(coefs[i])) return fail(LC_ERR_INVALID_ARG, "coefs must be finite");
+  }
+  if (!ortho_in_range(p->steps, coefs)) return fail(LC_ERR_INVALID_ARG, "coefs make a singular value larger than 2^30");
+  return LC_OK;
+}
+
+// The matrices of one argument: alike, of sides that the kernels reckon with.
+lc_status check_matrices(const char* name, const lc_matrix* m, uint32_t n, const lc_matrix& like, Rows* rows, Area* areas) {
+  for (uint32_t i = 0; i < n; ++i) {
+    LC_CHECK(check_matrix(name, m + i));
+    LC_CHECK(check_shape(name, m[i].rows, m[i].cols, like.rows, like.cols));
+    if (m[i].dtype != m[0].dtype) return fail(LC_ERR_INVALID_ARG, "%s: the matrices have different dtypes", name);
+    rows[i] = rows_of(m + i);
+    areas[i] = area_of(name, m + i);
+  }
+  return LC_OK;
+}
+
+}  // namespace
+
+extern "C" uint64_t lc_orthogonalize_workspace(uint32_t n_matrices, uint64_t rows, uint64_t cols, int32_t out_dtype) {
+  if (n_matrices == 0 || n_matrices > kOrthoMost || rows == 0 || cols == 0 || rows > kOrthoLongest || cols > kOrthoLongest ||
+      !dtype_ok(out_dtype))
+    return 0;
+  return ortho_workspace(n_matrices, rows, cols, out_dtype);
+}
+
+extern "C" lc_status lc_orthogonalize(const lc_orthogonalize_params* params, uint32_t n_matrices, const lc_matrix* grads,
+                                      const lc_matrix* momenta, const lc_matrix* out, void* workspace,
+                                      uint64_t workspace_bytes, void* stream) {
+  lc::TraceRange trace_("lc_orthogonalize");
+  double coefs[3 * kOrthoSteps];
+  LC_CHECK(check_ortho(params, coefs));
+  if (n_matrices > kOrthoMost) return fail(LC_ERR_INVALID_ARG, "%u matrices, at most %u", n_matrices, kOrthoMost);
+  if (n_matrices == 0) return LC_OK;
+  if (!grads || !out) return fail(LC_ERR_INVALID_ARG, "grads or out is NULL");
+  Rows g[kOrthoMost], m[kOrthoMost], o[kOrthoMost];
+  Area areas[3 * kOrthoMost + 1];
+  uint32_t n_areas = 0;  // what is written first
+  LC_CHECK(check_matrix("grads", grads));
+  const lc_matrix& like = grads[0];
+  if (like.rows > kOrthoLongest || like.cols > kOrthoLongest)
+    return fail(LC_ERR_INVALID_ARG, "matrices of %llu x %llu: at most %llu on a side", static_cast<unsigned long long>(like.rows),
+                static_cast<unsigned long long>(like.cols), static_cast<unsigned long long>(kOrthoLongest));
+  LC_CHECK(check_matrices("out", out, n_matrices, like, o, areas));
+  n_areas += n_matrices;
+  if (momenta) {
+    LC_CHECK(check_matrices("momenta", momenta, n_matrices, like, m, areas + n_areas));
+    if (momenta[0].dtype != LC_DT_F32) return fail(LC_ERR_INVALID_ARG, "momenta must be of LC_DT_F32");
+    n_areas += n_matrices;
+  }
+  const uint64_t need = lc_orthogonalize_workspace(n_matrices, like.rows, like.cols, out[0].dtype);
+  LC_CHECK(check_space(workspace, workspace_bytes, need));
+  areas[n_areas++] = flat("workspace", workspace, need);
+  const uint32_t written = n_areas;
+  LC_CHECK(check_matrices("grads", grads, n_matrices, like, g, areas + n_areas));
+  n_areas += n_matrices;
+  // by their addresses: an area is held against those that begin before its end
+  uint32_t order[3 * kOrthoMost + 1];
+  for (uint32_t i = 0; i < n_areas; ++i) order[i] = i;
+  std::sort(order, order + n_areas, [&](uint32_t a, uint32_t b) { return areas[a].base < areas[b].base; });
+  for (uint32_t i = 0; i < n_areas; ++i) {
+    const Area& a = areas[order[i]];
+    if (!a.rows) continue;
+    const uint64_t end = a.base + (a.rows - 1) * a.pitch + a.width;
+    for (uint32_t j = i + 1; j < n_areas && areas[order[j]].base < end; ++j)
+      if ((order[i] < written || order[j] < written) && overlap(a, areas[order[j]]))
+        return fail(LC_ERR_INVALID_ARG, "%s and %s overlap in memory", a.name, areas[order[j]].name);
+  }
+  LC_CHECK(check_stream(stream));
+  if (like.rows == 0) return LC_OK;
+  Ortho a{};
+  a.grads = g;
+  a.momenta = momenta ? m : nullptr;
+  a.outs = o;
+  a.count = n_matrices;
+  a.steps = params->steps;
+  a.rows = like.rows;
+  a.cols = like.cols;
+  a.coefs = coefs;
+  a.momentum = params->momentum;
+  a.eps = params->eps;
+  a.scale = params->scale;
+  a.nesterov = params->nesterov;
+  a.dtype = like.dtype;
+  a.out_dtype = out[0].dtype;
+  a.ws = static_cast<uint8_t*>(workspace);
+  return launched("lc_orthogonalize", launch_ortho(a, static_cast<hipStream_t>(stream)));
 }

@@ -119,4 +119,23 @@ struct Wgrad {
 uint64_t wgrad_workspace(uint64_t rows, uint64_t n, uint64_t k);
 hipError_t launch_wgrad(const Wgrad& a, hipStream_t st);
 
+// Momentum and Newton-Schulz steps of matrices of one shape.
+constexpr uint32_t kOrthoMost = 64;             // matrices a call
+constexpr uint64_t kOrthoLongest = 1 << 16;     // of a side
+constexpr double kOrthoLargest = 1.0 * (1 << 30);  // that the steps may make a singular value
+struct Ortho {
+  const Rows* grads;
+  const Rows* momenta;  // null: none
+  const Rows* outs;
+  uint32_t count, steps;
+  uint64_t rows, cols;
+  const double* coefs;  // [steps][3]
+  double momentum, eps, scale;
+  int nesterov, dtype, out_dtype;
+  uint8_t* ws;
+};
+bool ortho_in_range(uint32_t steps, const double* coefs);
+uint64_t ortho_workspace(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype);
+hipError_t launch_ortho(const Ortho& a, hipStream_t st);
+
 }  // namespace lc

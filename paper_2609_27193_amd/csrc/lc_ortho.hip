@@ -1,0 +1,748 @@
+// Momentum and Newton-Schulz steps for matrices of one shape:
+//
+//   buf <- g + mu buf,  u = g + mu buf (Nesterov) or buf,  X = u / (|u| + eps)
+//   a step:  A = X X^T,  B = b A + c A A,  X <- a X + B X
+//
+// on the shorter side (a tall matrix is transposed on its way in and out), m rows
+// of n.  Bound by the matrix cores: 4 m^2 n + 2 m^3 flops a step, of which the
+// halves of A and A A below the diagonal are written from those above.
+//
+// X, A and B are held in fp16, times a power of two that keeps their largest
+// possible element, which is bounded by the largest singular value that the steps'
+// polynomials allow, at 2^15 or less: 11 bits of every element, where bf16 at the
+// same rate keeps 8.  A result in fp32 takes each as the sum of two such planes, 22
+// bits, and a product as three (the fourth is below the last bit).  An error of one
+// rounding (2^-12 of an element) is spread over all singular directions; the
+// smaller ones, which the steps raise by up to `a` each, carry it along: 256 x 1024
+// of normal elements, five steps of 3.4445, -4.775, 2.0315: 1.4e-3 of the result's
+// norm, a bf16 result's rounding itself 1.7e-3; bf16 throughout 1.2e-2; two planes
+// 2.6e-7, fp32 throughout 1.7e-7.  Sums, norms and the momentum are fp32 or wider.
+//
+// Inside, sides are padded to multiples of 64 with zeros, which stay zeros.
+#include <algorithm>
+#include <cmath>
+
+#include "lc_ops_device.h"
+
+namespace lc {
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef const __attribute__((address_space(3))) f16x8 lds_f16x8;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) float lds_f32;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+constexpr uint32_t kThreads = 256;  // four waves
+constexpr uint32_t kPad = 64;       // of both sides
+constexpr uint32_t kStep = 64;      // of the sum, in LDS at a time
+constexpr uint32_t kNormBlocks = 256;  // of one matrix, at most
+
+// ---- the update and its norm -----------------------------------------------------------
+// Matrix z of the group: where its gradient and momentum are.
+struct OrthoIn {
+  uint64_t g[kOrthoMost], g_stride[kOrthoMost];
+  uint64_t buf[kOrthoMost], buf_stride[kOrthoMost];  // buf[0] 0: no momentum
+  uint32_t rows, cols;
+  float mu;
+  int nesterov;
+};
+// Eight elements of u from column c on, out of the gradient and the momentum as
+// it is (OLD) or already is.  The new momentum is left in b.
+template <int DT, bool OLD>
+__device__ __forceinline__ void update8(const OrthoIn& a, uint32_t z, uint32_t row, uint32_t c, int n, float (&u)[8],
+                                        float (&b)[8]) {
+  unpack8<DT>(load8_raw<DT>(a.g[z] + (row * a.g_stride[z] + c) * kEsz<DT>, n), u);
+  if (!a.buf[0]) return;
+  unpack8<kF32>(load8_raw<kF32>(a.buf[z] + (row * a.buf_stride[z] + c) * 4, n), b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (OLD) b[e] = __builtin_fmaf(a.mu, b[e], u[e]);
+    u[e] = a.nesterov ? __builtin_fmaf(a.mu, b[e], u[e]) : b[e];
+  }
+}
+
+__device__ __forceinline__ double block_sum(double v, double (&red)[kThreads / 64]) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (uint32_t w = 1; w < kThreads / 64; ++w) v += red[w];
+  return v;
+}
+
+// The new momentum, and the squares of u summed in 64 bits: a gradient's elements
+// may be as small as their squares are no fp32 numbers.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void ortho_norm_kernel(OrthoIn a, double* sums) {
+  __shared__ double red[kThreads / 64];
+  const uint32_t z = blockIdx.y, groups = (a.cols + 7) / 8;
+  const uint64_t items = static_cast<uint64_t>(a.rows) * groups;
+  double s = 0;
+  for (uint64_t i = blockIdx.x * kThreads + threadIdx.x; i < items; i += gridDim.x * kThreads) {
+    const uint32_t row = static_cast<uint32_t>(i / groups), c = static_cast<uint32_t>(i % groups) * 8;
+    const int n = static_cast<int>(a.cols - c);
+    float u[8], b[8];
+    update8<DT, true>(a, z, row, c, n, u, b);
+    if (a.buf[0]) store8<kF32>(a.buf[z] + (row * a.buf_stride[z] + c) * 4, b, n);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += e < n ? static_cast<double>(u[e]) * u[e] : 0.0;
+  }
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) sums[z * gridDim.x + blockIdx.x] = s;
+}
+
+// fp16 planes of eight neighbours: the value's, and of two the rest's times 2^11.
+constexpr float kRestUp = 2048.0f;
+__device__ __forceinline__ void store_planes8(uint64_t p, uint64_t plane, const float (&v)[8]) {
+  u32x4 hi, lo;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f16x2 h = {static_cast<_Float16>(v[e]), static_cast<_Float16>(v[e + 1])};
+    hi[e / 2] = __builtin_bit_cast(uint32_t, h);
+    const f16x2 l = {static_cast<_Float16>((v[e] - static_cast<float>(h[0])) * kRestUp),
+                     static_cast<_Float16>((v[e + 1] - static_cast<float>(h[1])) * kRestUp)};
+    lo[e / 2] = __builtin_bit_cast(uint32_t, l);
+  }
+  *(g_u32x4*)p = hi;
+  if (plane) *(g_u32x4*)(p + plane) = lo;
+}
+typedef const __attribute__((address_space(1))) u32x4 gc_u32x4;
+// Two elements of a plane to fp32.
+__device__ __forceinline__ f32x2 halves(uint32_t w) {
+  const f16x2 h = __builtin_bit_cast(f16x2, w);
+  return f32x2{static_cast<float>(h[0]), static_cast<float>(h[1])};
+}
+__device__ __forceinline__ void load_planes8(uint64_t p, uint64_t plane, float (&v)[8]) {
+  const u32x4 hi = *(gc_u32x4*)p;
+  u32x4 lo = {0, 0, 0, 0};
+  if (plane) lo = *(gc_u32x4*)(p + plane);
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f32x2 h = halves(hi[e / 2]), l = halves(lo[e / 2]);
+    v[e] = __builtin_fmaf(l[0], 1.0f / kRestUp, h[0]);
+    v[e + 1] = __builtin_fmaf(l[1], 1.0f / kRestUp, h[1]);
+  }
+}
+
+// X of the group: u over its norm, m x n, padded.
+struct OrthoX {
+  uint64_t x, plane, next;  // the first matrix's first plane; bytes to the second plane (0: none), to the next matrix
+  uint32_t m, n;            // padded
+  double eps, power;        // what X is held times
+};
+// Blocks of 64 x 64 of a matrix: a tall one goes through LDS.
+template <int DT, bool TALL>
+__global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX o, const double* sums, uint32_t n_sums) {
+  __shared__ double red[kThreads / 64];
+  __shared__ float tile[TALL ? 64 : 1][65];
+  const uint32_t z = blockIdx.y;
+  double s = 0;
+  for (uint32_t i = threadIdx.x; i < n_sums; i += kThreads) s += sums[z * n_sums + i];
+  const double norm = sqrt(block_sum(s, red));
+  // a matrix of zeros stays one; of what is not finite, the whole becomes NaN
+  const double by = norm < __builtin_inf() ? (norm > 0 ? o.power / (norm + o.eps) : 0.0) : __builtin_nan("");
+  const uint32_t across = (TALL ? o.m : o.n) / 64;  // of the gradient's columns
+  const uint32_t tiles = (o.m / 64) * (o.n / 64);
+  const uint64_t base = o.x + z * o.next;
+  for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const uint32_t r0 = t / across * 64, c0 = t % across * 64;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t lr = threadIdx.x / 8 + 32 * h, lc = threadIdx.x % 8 * 8, row = r0 + lr, c = c0 + lc;
+      const int n = row < a.rows ? static_cast<int>(a.cols) - static_cast<int>(c) : 0;
+      float u[8] = {}, b[8];
+      if (n > 0) update8<DT, false>(a, z, row, c, n, u, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = e < n ? static_cast<float>(u[e] * by) : 0.0f;
+      if constexpr (TALL) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[lr][lc + e] = u[e];
+      } else {
+        store_planes8(base + (static_cast<uint64_t>(row) * o.n + c) * 2, o.plane, u);
+      }
+    }
+    if constexpr (TALL) {
+      __syncthreads();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t lc = threadIdx.x / 8 + 32 * h, lr = threadIdx.x % 8 * 8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[lr + e][lc];
+        store_planes8(base + (static_cast<uint64_t>(c0 + lc) * o.n + r0 + lr) * 2, o.plane, v);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ---- the products --------------------------------------------------------------------------
+// D[i][j] = f_acc * sum over k of L[i][k] R'[k][j] + f_aux * aux[i][j], of planes of
+// fp16.  A symmetric one (SYM) takes R' = R^T, with R's rows along the sum as L's, and
+// computes the tiles on and above the diagonal; else R' = R.
+struct OrthoProduct {
+  uint64_t left, right, aux, out;              // of the group's first matrix
+  uint64_t left_plane, right_plane, out_plane; // bytes to the second plane; 0: one plane (aux: as out)
+  uint64_t left_next, right_next, out_next;    // bytes to the next matrix (aux: as out)
+  uint32_t left_pitch, right_pitch, out_pitch; // bytes from row to row (aux: as out)
+  uint32_t rows, cols, k;                      // multiples of 64
+  uint32_t ti, tj, tiles, count;               // tiles down, across and of a matrix; matrices
+  uint32_t splits, split_k;                    // parts of the sum and its steps a part
+  float f_acc, f_aux;
+  float* part;                                 // [count * tiles][splits][T][T], splits > 1
+};
+// Where a group's last products go: the caller's matrices.
+struct OrthoOut {
+  uint64_t data[kOrthoMost], stride[kOrthoMost];
+  uint32_t m, n;  // of X, without its padding
+  int dtype, tall;
+};
+
+__device__ __forceinline__ void ortho_place(const OrthoProduct& p, bool sym, uint32_t t, uint32_t& i, uint32_t& j) {
+  if (sym) {  // columns of the upper triangle
+    j = static_cast<uint32_t>((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while ((j + 1) * (j + 2) / 2 <= t) ++j;
+    while (j * (j + 1) / 2 > t) --j;
+    i = t - j * (j + 1) / 2;
+  } else {  // eight tiles down by all across
+    const uint32_t group = t / (8 * p.tj), in_g = t - group * 8 * p.tj;
+    const uint32_t high = p.ti - group * 8 < 8 ? p.ti - group * 8 : 8;
+    j = in_g / high;
+    i = group * 8 + in_g % high;
+  }
+}
+
+constexpr int kVmcnt0 = 0x0F70;
+
+// A lane's 16 bytes to LDS, the wave's 64 after each other.  The whole offset is in
+// the operand that the bounds check covers.
+__device__ __forceinline__ void load_lds(tile_t t, uint8_t* to, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(t, (lds_void*)to, 16, off, 0, 0, 0);
+}
+
+// Eight neighbours of row i of D from column j on, in the user's type.
+__device__ __forceinline__ void ortho_out8(const OrthoOut& o, uint32_t z, uint64_t row, uint32_t col, int n, const float (&v)[8]) {
+  if (n <= 0) return;
+  const uint64_t at = row * o.stride[z] + col;
+  if (o.dtype == kBf16) store8<kBf16>(o.data[z] + 2 * at, v, n);
+  else store8<kF32>(o.data[z] + 4 * at, v, n);
+}
+
+constexpr int kSym = 0, kMid = 1, kLast = 2;
+
+// T x T of D a block, four waves of T/2 x T/2, two LDS buffers of a step each that
+// the loads write by themselves.
+//
+// LDS: a row of an operand's step is 128 bytes along the sum (L, and R of SYM), its
+// 16-byte pieces at c ^ row % 8; or, of R as it lies, T columns of one k, its 32-byte
+// slots moved up by k % 4, which spreads the four rows that a transposing read takes.
+// PLANES: of each operand.
+template <int MODE, int T, int PLANES>
+__global__ __launch_bounds__(kThreads, T == 256 ? 1 : 2) void ortho_product_kernel(OrthoProduct p, OrthoOut o) {
+  constexpr bool SYM = MODE == kSym;
+  constexpr uint32_t NF = T / 64;             // 32-wide pieces of a wave's side
+  constexpr uint32_t kOperand = T * kStep * 2;  // bytes
+  constexpr uint32_t kLoads = T / 32;         // of an operand, a thread
+  constexpr uint32_t kSlots = T / 16;         // of 32 bytes in a row of R as it lies
+  constexpr uint32_t kOut = T / 2 + 4;        // floats from row to row on their way out
+  constexpr uint32_t kSlab = 32 * kOut * 4;
+  constexpr uint32_t kStage = 2 * kOperand > 2 * kSlab ? 2 * kOperand : 2 * kSlab;
+  __shared__ __align__(1024) uint8_t stage0[kStage];
+  __shared__ __align__(1024) uint8_t stage1[kStage];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t items = p.count * p.tiles * p.splits;
+  for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
+    const uint32_t item = items <= gridDim.x ? remap_xcd(b, items) : b;
+    const uint32_t split = item % p.splits, tile = item / p.splits, z = tile / p.tiles;
+    uint32_t ti, tj;
+    ortho_place(p, SYM, tile % p.tiles, ti, tj);
+    const uint32_t i0 = ti * T, j0 = tj * T;
+    // the steps of this part
+    const uint32_t k_begin = split * p.split_k, k_all = p.k / kStep;
+    const uint32_t k_end = k_begin + p.split_k < k_all ? k_begin + p.split_k : k_all;
+    uint32_t pass = 0, next_k = 0, last_pass = 0;
+    const uint64_t left = p.left + z * p.left_next + static_cast<uint64_t>(i0) * p.left_pitch;
+    const uint64_t right = p.right + z * p.right_next + (SYM ? static_cast<uint64_t>(j0) * p.right_pitch : 2ull * j0);
+    const uint32_t left_rows = p.rows - i0 < T ? p.rows - i0 : T, right_rows = p.cols - j0 < T ? p.cols - j0 : T;
+    const uint32_t left_at = (wave * 8 + lane / 8) * p.left_pitch + (lane % 8 ^ lane / 8) * 16;
+    uint32_t right_at[kLoads];
+#pragma unroll
+    for (uint32_t q = 0; q < kLoads; ++q) {
+      if constexpr (SYM) {
+        right_at[q] = (q * 32 + wave * 8 + lane / 8) * p.right_pitch + (lane % 8 ^ lane / 8) * 16;
+      } else {
+        const uint32_t piece = (q * 4 + wave) * 64 + lane, row = piece / (2 * kSlots), pos = piece % (2 * kSlots);
+        right_at[q] = row * p.right_pitch + ((pos / 2 + kSlots - row % 4) % kSlots * 2 + pos % 2) * 16;
+      }
+    }
+    // Nothing is read behind an operand: rows and columns that are not there are
+    // not stored, whatever LDS holds for them.
+    auto load = [&](uint8_t* stage) {
+      const bool on = pass < last_pass;
+      const uint64_t l = left + (pass == 0 ? p.left_plane : 0) + next_k * 128ull;
+      const uint64_t r = right + (pass == 1 ? p.right_plane : 0) + (SYM ? next_k * 128ull : next_k * 64ull * p.right_pitch);
+      const tile_t tl = make_tile(reinterpret_cast<const void*>(l), on ? left_rows * p.left_pitch - next_k * 128 : 0);
+      const tile_t tr = make_tile(reinterpret_cast<const void*>(r), !on ? 0 : SYM ? right_rows * p.right_pitch - next_k * 128
+                                                                                  : kStep * p.right_pitch - 2 * j0);
+#pragma unroll
+      for (uint32_t q = 0; q < kLoads; ++q)
+        load_lds(tl, stage + (q * 4 + wave) * 1024, left_at + q * 32 * p.left_pitch);
+#pragma unroll
+      for (uint32_t q = 0; q < kLoads; ++q) load_lds(tr, stage + kOperand + (q * 4 + wave) * 1024, right_at[q]);
+      if (++next_k == k_end) {
+        next_k = k_begin;
+        ++pass;
+      }
+    };
+    // operands of 16 of the sum
+    const uint32_t wi = wave % 2 * (T / 2), wj = wave / 2 * (T / 2);
+    f16x8 lf[2][NF], rf[2][NF];
+    const uint32_t x4 = lane % 16 / 4;
+    uint32_t tr_at[NF];
+#pragma unroll
+    for (uint32_t f = 0; f < NF; ++f)
+      tr_at[f] = kOperand + (lane / 32 * 8 + x4) * (T * 2) + (wj / 16 + 2 * f + lane / 16 % 2 + x4) % kSlots * 32 + lane % 4 * 8;
+    auto fetch = [&](uint8_t* stage, uint32_t to, uint32_t sub) {
+      const uint32_t piece = ((2 * sub + lane / 32) ^ (lane % 8)) * 16;
+#pragma unroll
+      for (uint32_t f = 0; f < NF; ++f) {
+        if constexpr (SYM) {
+          rf[to][f] = *(lds_f16x8*)(stage + kOperand + (wj + 32 * f + lane % 32) * 128 + piece);
+        } else {
+          uint8_t* const at = stage + tr_at[f] + sub * 16 * T * 2;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * T * 2));
+          rf[to][f] = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+      }
+#pragma unroll
+      for (uint32_t f = 0; f < NF; ++f) lf[to][f] = *(lds_f16x8*)(stage + (wi + 32 * f + lane % 32) * 128 + piece);
+    };
+    f32x16 acc[NF][NF];  // [j][i] pieces of 32: a lane holds four runs of 4 of j for one i
+#pragma unroll
+    for (uint32_t j = 0; j < NF; ++j)
+#pragma unroll
+      for (uint32_t i = 0; i < NF; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[j][i][e] = 0;
+    auto multiply = [&](uint32_t of) {
+#pragma unroll
+      for (uint32_t j = 0; j < NF; ++j)
+#pragma unroll
+        for (uint32_t i = 0; i < NF; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(rf[of][j], lf[of][i], acc[j][i], 0, 0, 0);
+    };
+    // One step out of `cur`: the next operands are read while the ones before them
+    // multiply, and the step behind the next goes into `cur` when all waves have it
+    // in registers.
+    auto step = [&](uint8_t* cur, uint8_t* nxt) {
+      fetch(cur, 1, 1);
+      multiply(0);
+      fetch(cur, 0, 2);
+      multiply(1);
+      fetch(cur, 1, 3);
+      multiply(0);
+      __builtin_amdgcn_s_waitcnt(kVmcnt0);
+      __syncthreads();
+      fetch(nxt, 0, 0);
+      load(cur);
+      multiply(1);
+    };
+    // first the products of a second plane, of either side, then those of the first
+#pragma unroll 1
+    for (uint32_t big = PLANES == 2 ? 0 : 1; big < 2; ++big) {
+      pass = big ? 2 : 0;
+      last_pass = big ? 3 : 2;
+      next_k = k_begin;
+      const uint32_t steps = (k_end - k_begin) * (last_pass - pass);
+      load(stage0);
+      load(stage1);
+      __builtin_amdgcn_s_waitcnt(kVmcnt0);
+      __syncthreads();
+      fetch(stage0, 0, 0);
+      for (uint32_t s = 0; s < steps / 2; ++s) {
+        step(stage0, stage1);
+        step(stage1, stage0);
+      }
+      if (steps % 2) step(stage0, stage1);
+      __builtin_amdgcn_s_waitcnt(kVmcnt0);
+      __syncthreads();
+      if (PLANES == 2 && !big) {
+#pragma unroll
+        for (uint32_t j = 0; j < NF; ++j)
+#pragma unroll
+          for (uint32_t i = 0; i < NF; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[j][i][e] *= 1.0f / kRestUp;
+      }
+    }
+
+    // out through LDS, 32 rows a wave at a time
+    lds_f32* const mine = (lds_f32*)((wave < 2 ? stage0 : stage1) + wave % 2 * kSlab);
+    constexpr uint32_t kGroups = T / 16;  // of eight columns in a wave's row
+    const uint64_t out = p.out + z * p.out_next, aux = p.aux + z * p.out_next;
+#pragma unroll
+    for (uint32_t f = 0; f < NF; ++f) {
+#pragma unroll
+      for (uint32_t j = 0; j < NF; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *(lds_f32x4*)(mine + lane % 32 * kOut + 32 * j + 8 * r + lane / 32 * 4) =
+              f32x4{acc[j][f][4 * r], acc[j][f][4 * r + 1], acc[j][f][4 * r + 2], acc[j][f][4 * r + 3]};
+      const uint32_t row0 = i0 + wi + 32 * f, col0 = j0 + wj;
+      if (p.splits > 1) {
+        float* const to = p.part + (static_cast<uint64_t>(tile) * p.splits + split) * (T * T) + (wi + 32 * f) * T + wj;
+        for (uint32_t g = lane; g < 32 * kGroups; g += 64) {
+          const uint32_t q = g / kGroups, c = g % kGroups * 8;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            *(f32x4*)(to + q * T + c + 4 * h) = *(lds_f32x4*)(mine + q * kOut + c + 4 * h);
+        }
+        continue;
+      }
+      const bool turned = SYM ? ti != tj : MODE == kLast && o.tall;
+      for (uint32_t g = lane; g < 32 * kGroups; g += 64) {
+        const uint32_t q = g / kGroups, c = g % kGroups * 8, row = row0 + q, col = col0 + c;
+        float v[8], x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + c + e] * p.f_acc;
+        if (row < p.rows && col < p.cols) {
+          const uint64_t at = static_cast<uint64_t>(row) * p.out_pitch + 2 * col;
+          if (p.aux) {
+            load_planes8(aux + at, p.out_plane, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(p.f_aux, x[e], v[e]);
+          }
+          if (MODE != kLast) store_planes8(out + at, p.out_plane, v);
+          else if (!o.tall && row < o.m) ortho_out8(o, z, row, col, static_cast<int>(o.n) - static_cast<int>(col), v);
+        }
+        if (turned) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mine[q * kOut + c + e] = v[e];
+        }
+      }
+      if (turned) {  // column j of the slab: 32 neighbours of row j of the other side
+        for (uint32_t g = lane; g < 4 * (T / 2); g += 64) {
+          const uint32_t j = g % (T / 2), c = g / (T / 2) * 8, row = col0 + j, col = row0 + c;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = mine[(c + e) * kOut + j];
+          if (MODE == kLast) {
+            if (row < o.n) ortho_out8(o, z, row, col, static_cast<int>(o.m) - static_cast<int>(col), v);
+          } else if (row < p.cols && col < p.rows) {
+            store_planes8(out + static_cast<uint64_t>(row) * p.out_pitch + 2 * col, p.out_plane, v);
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The parts' sums of a symmetric product, in order, to both sides of the diagonal.
+__global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoProduct p, uint32_t side) {
+  __shared__ float sums[64][65];
+  const uint32_t per_tile = (side / 64) * (side / 64);
+  const uint32_t items = p.count * p.tiles * per_tile;
+  for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const uint32_t tile = it / per_tile, z = tile / p.tiles, sub = it % per_tile;
+    const uint32_t si = sub / (side / 64) * 64, sj = sub % (side / 64) * 64;
+    uint32_t ti, tj;
+    ortho_place(p, true, tile % p.tiles, ti, tj);
+    const uint32_t i0 = ti * side + si, j0 = tj * side + sj;
+    const uint64_t out = p.out + z * p.out_next, aux = p.aux + z * p.out_next;
+    const float* const part = p.part + static_cast<uint64_t>(tile) * p.splits * side * side;
+    const bool on = i0 < p.rows && j0 < p.cols;
+    for (uint32_t g = threadIdx.x; on && g < 64 * 8; g += kThreads) {
+      const uint32_t q = g / 8, c = g % 8 * 8;
+      float v[8] = {}, x[8];
+      for (uint32_t s = 0; s < p.splits; ++s) {
+        unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(part + (static_cast<uint64_t>(s) * side + si + q) * side + sj + c)), x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+      }
+      const uint64_t at = static_cast<uint64_t>(i0 + q) * p.out_pitch + 2 * (j0 + c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= p.f_acc;
+      if (p.aux) {
+        load_planes8(aux + at, p.out_plane, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(p.f_aux, x[e], v[e]);
+      }
+      store_planes8(out + at, p.out_plane, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums[q][c + e] = v[e];
+    }
+    __syncthreads();
+    for (uint32_t g = threadIdx.x; on && ti != tj && g < 64 * 8; g += kThreads) {
+      const uint32_t j = g / 8, c = g % 8 * 8;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = sums[c + e][j];
+      store_planes8(out + static_cast<uint64_t>(j0 + j) * p.out_pitch + 2 * (i0 + c), p.out_plane, v);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- the plan ------------------------------------------------------------------------------
+uint64_t padded(uint64_t x) { return (x + kPad - 1) / kPad * kPad; }
+
+// How the products of a shape are cut.
+struct OrthoCut {
+  uint32_t side, ti, tj, tiles, splits, split_k;
+};
+OrthoCut ortho_cut(uint64_t rows, uint64_t cols, uint64_t k, uint32_t count, bool sym, bool may_split) {
+  OrthoCut c{};
+  c.side = 64;
+  for (uint32_t side : {256u, 128u}) {
+    const uint64_t ti = (rows + side - 1) / side, tj = (cols + side - 1) / side;
+    if ((sym ? ti * (ti + 1) / 2 : ti * tj) * count >= (side == 256 ? 256u : 200u)) {
+      c.side = side;
+      break;
+    }
+  }
+  c.ti = static_cast<uint32_t>((rows + c.side - 1) / c.side);
+  c.tj = static_cast<uint32_t>((cols + c.side - 1) / c.side);
+  c.tiles = sym ? c.ti * (c.ti + 1) / 2 : c.ti * c.tj;
+  const uint32_t steps = static_cast<uint32_t>(k / kStep);
+  uint32_t splits = 1;
+  if (may_split && c.tiles * count < 256) splits = std::min(256 / (c.tiles * count), std::max(1u, steps / 4));
+  c.split_k = (steps + splits - 1) / splits;
+  c.splits = (steps + c.split_k - 1) / c.split_k;
+  return c;
+}
+uint64_t ortho_part_bytes(const OrthoCut& c, uint32_t count) {
+  return c.splits > 1 ? static_cast<uint64_t>(c.tiles) * count * c.splits * c.side * c.side * 4 : 0;
+}
+
+// Matrices at once and their place in the workspace.
+struct OrthoPlan {
+  uint64_t m, n;  // padded
+  bool tall;
+  uint32_t planes, group;
+  uint64_t x_bytes, a_bytes;  // of one matrix, all planes
+  uint64_t sums, x0, x1, a, b, part, bytes;  // offsets, and the whole
+  OrthoCut gram, poly, mid;
+};
+OrthoPlan ortho_plan(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype) {
+  OrthoPlan p{};
+  p.tall = rows > cols;
+  p.m = padded(p.tall ? cols : rows);
+  p.n = padded(p.tall ? rows : cols);
+  p.planes = out_dtype == kF32 ? 2 : 1;
+  p.x_bytes = p.m * p.n * 2 * p.planes;
+  p.a_bytes = p.m * p.m * 2 * p.planes;
+  // as many as keep the chip at work: a round of 256 tiles, four times
+  const uint64_t tiles = ((p.m + 255) / 256) * ((p.m + 255) / 256);
+  p.group = static_cast<uint32_t>(std::min<uint64_t>(count, std::max<uint64_t>(1, 1024 / tiles)));
+  p.gram = ortho_cut(p.m, p.m, p.n, p.group, true, true);
+  p.poly = ortho_cut(p.m, p.m, p.m, p.group, true, true);
+  p.mid = ortho_cut(p.m, p.n, p.m, p.group, false, false);
+  p.sums = 0;
+  p.x0 = kOrthoMost * kNormBlocks * 8;
+  p.x1 = p.x0 + p.group * p.x_bytes;
+  p.a = p.x1 + p.group * p.x_bytes;
+  p.b = p.a + p.group * p.a_bytes;
+  p.part = p.b + p.group * p.a_bytes;
+  p.bytes = p.part + std::max(ortho_part_bytes(p.gram, p.group), ortho_part_bytes(p.poly, p.group));
+  return p;
+}
+
+// The power of two that brings `bound` to 2^14 .. 2^15.
+int exponent_for(double bound) {
+  if (!(bound > 0)) return 0;
+  int e;
+  std::frexp(bound, &e);  // bound < 2^e
+  return 15 - e;
+}
+double largest(double x, double a, double b, double c) { return std::fabs(x * (a + x * x * (b + x * x * c))); }
+// The largest |a s + b s^3 + c s^5| of s in [0, top].
+double ortho_bound(double top, const double* k) {
+  double best = largest(top, k[0], k[1], k[2]);
+  // its slope is a + 3 b q + 5 c q^2, q = s^2
+  const double a = 5 * k[2], b = 3 * k[1], c = k[0];
+  double roots[2];
+  int n = 0;
+  if (a != 0) {
+    const double d = b * b - 4 * a * c;
+    if (d >= 0) {
+      roots[n++] = (-b + std::sqrt(d)) / (2 * a);
+      roots[n++] = (-b - std::sqrt(d)) / (2 * a);
+    }
+  } else if (b != 0) {
+    roots[n++] = -c / b;
+  }
+  for (int i = 0; i < n; ++i)
+    if (roots[i] > 0 && roots[i] < top * top) best = std::max(best, largest(std::sqrt(roots[i]), k[0], k[1], k[2]));
+  return best;
+}
+// The same of |b q + c q^2|, q in [0, top].
+double ortho_bound_b(double top, double b, double c) {
+  double best = std::fabs(top * (b + top * c));
+  if (c != 0) {
+    const double q = -b / (2 * c);
+    if (q > 0 && q < top) best = std::max(best, std::fabs(q * (b + q * c)));
+  }
+  return best;
+}
+constexpr double kSlack = 1.02;  // what roundings may add to a bound
+
+template <int MODE, int PLANES>
+hipError_t product_of(const OrthoProduct& p, const OrthoOut& o, uint32_t side, hipStream_t st) {
+  const uint32_t grid = grid_for(static_cast<uint64_t>(p.count) * p.tiles * p.splits, kThreads);
+  if (side == 256) return launch_op(ortho_product_kernel<MODE, 256, PLANES>, grid, kThreads, st, p, o);
+  if (side == 128) return launch_op(ortho_product_kernel<MODE, 128, PLANES>, grid, kThreads, st, p, o);
+  return launch_op(ortho_product_kernel<MODE, 64, PLANES>, grid, kThreads, st, p, o);
+}
+template <int MODE>
+hipError_t product(const OrthoProduct& p, const OrthoOut& o, uint32_t side, hipStream_t st) {
+  const hipError_t e = p.left_plane ? product_of<MODE, 2>(p, o, side, st) : product_of<MODE, 1>(p, o, side, st);
+  if (e != hipSuccess || p.splits == 1) return e;
+  const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * (side / 64) * (side / 64);
+  return launch_op(ortho_join_kernel, grid_for(items, kThreads), kThreads, st, p, side);
+}
+
+void set_cut(OrthoProduct& p, const OrthoCut& c) {
+  p.ti = c.ti;
+  p.tj = c.tj;
+  p.tiles = c.tiles;
+  p.splits = c.splits;
+  p.split_k = c.split_k;
+}
+
+}  // namespace
+
+bool ortho_in_range(uint32_t steps, const double* coefs) {
+  double x = 1.0;
+  for (uint32_t s = 0; s < steps; ++s) {
+    const double* const k = coefs + 3 * s;
+    const double q = x * x * kSlack;
+    x = ortho_bound(x, k) * kSlack;
+    if (!(x < kOrthoLargest) || !(ortho_bound_b(q, k[1], k[2]) < kOrthoLargest) || !(q < kOrthoLargest)) return false;
+  }
+  return true;
+}
+
+uint64_t ortho_workspace(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype) {
+  return ortho_plan(count, rows, cols, out_dtype).bytes;
+}
+
+hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
+  const OrthoPlan plan = ortho_plan(a.count, a.rows, a.cols, a.out_dtype);
+  const uint64_t ws = reinterpret_cast<uint64_t>(a.ws);
+  double* const sums = reinterpret_cast<double*>(ws + plan.sums);
+  float* const part = reinterpret_cast<float*>(ws + plan.part);
+  const uint32_t x_pitch = static_cast<uint32_t>(plan.n * 2), a_pitch = static_cast<uint32_t>(plan.m * 2);
+  const uint64_t x_plane = plan.planes == 2 ? plan.m * plan.n * 2 : 0, a_plane = plan.planes == 2 ? plan.m * plan.m * 2 : 0;
+  for (uint32_t z0 = 0; z0 < a.count; z0 += plan.group) {
+    const uint32_t count = std::min(plan.group, a.count - z0);
+    OrthoIn in{};
+    OrthoOut out{};
+    for (uint32_t z = 0; z < count; ++z) {
+      in.g[z] = a.grads[z0 + z].data;
+      in.g_stride[z] = a.grads[z0 + z].stride;
+      in.buf[z] = a.momenta ? a.momenta[z0 + z].data : 0;
+      in.buf_stride[z] = a.momenta ? a.momenta[z0 + z].stride : 0;
+      out.data[z] = a.outs[z0 + z].data;
+      out.stride[z] = a.outs[z0 + z].stride;
+    }
+    in.rows = static_cast<uint32_t>(a.rows);
+    in.cols = static_cast<uint32_t>(a.cols);
+    in.mu = static_cast<float>(a.momentum);
+    in.nesterov = a.nesterov;
+    out.m = static_cast<uint32_t>(std::min(a.rows, a.cols));
+    out.n = static_cast<uint32_t>(std::max(a.rows, a.cols));
+    out.dtype = a.out_dtype;
+    out.tall = plan.tall;
+    const uint64_t groups = a.rows * ((a.cols + 7) / 8);
+    uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>(kNormBlocks, (groups + kThreads - 1) / kThreads));
+    if (LC_MAX_GRID_BLOCKS > 0 && blocks > LC_MAX_GRID_BLOCKS) blocks = LC_MAX_GRID_BLOCKS;
+    hipError_t e = launch_op(a.dtype == kBf16 ? ortho_norm_kernel<kBf16> : ortho_norm_kernel<kF32>, dim3(blocks, count), kThreads, st, in, sums);
+    if (e != hipSuccess) return e;
+    double bound = 1.0;
+    int ex = exponent_for(bound * kSlack);
+    uint64_t x = ws + plan.x0, other = ws + plan.x1;
+    const OrthoX ox{x, x_plane, plan.x_bytes, static_cast<uint32_t>(plan.m), static_cast<uint32_t>(plan.n), a.eps, std::ldexp(1.0, ex)};
+    const dim3 load_grid(grid_for((plan.m / 64) * (plan.n / 64), kThreads), count);
+    if (a.dtype == kBf16) e = launch_op(plan.tall ? ortho_load_kernel<kBf16, true> : ortho_load_kernel<kBf16, false>, load_grid, kThreads, st, in, ox, sums, blocks);
+    else e = launch_op(plan.tall ? ortho_load_kernel<kF32, true> : ortho_load_kernel<kF32, false>, load_grid, kThreads, st, in, ox, sums, blocks);
+    if (e != hipSuccess) return e;
+    for (uint32_t s = 0; s < a.steps; ++s) {
+      const double* const k = a.coefs + 3 * s;
+      const double bound_a = bound * bound * kSlack;
+      const int ea = exponent_for(bound_a);
+      OrthoProduct p{};  // A = X X^T
+      p.left = p.right = x;
+      p.left_plane = p.right_plane = x_plane;
+      p.left_next = p.right_next = plan.x_bytes;
+      p.left_pitch = p.right_pitch = x_pitch;
+      p.out = ws + plan.a;
+      p.out_plane = a_plane;
+      p.out_next = plan.a_bytes;
+      p.out_pitch = a_pitch;
+      p.rows = p.cols = static_cast<uint32_t>(plan.m);
+      p.k = static_cast<uint32_t>(plan.n);
+      p.count = count;
+      p.part = part;
+      p.f_acc = static_cast<float>(std::ldexp(1.0, ea - 2 * ex));
+      set_cut(p, plan.gram);
+      if ((e = product<kSym>(p, out, plan.gram.side, st)) != hipSuccess) return e;
+      uint64_t left = p.out;
+      int el = ea;
+      double by = k[1];  // of A X; B = b A needs no product of its own
+      if (k[2] != 0) {   // B = b A + c A A
+        const int eb = exponent_for(ortho_bound_b(bound_a, k[1], k[2]) * kSlack);
+        p.left = p.right = p.aux = ws + plan.a;
+        p.left_plane = p.right_plane = a_plane;
+        p.left_next = p.right_next = plan.a_bytes;
+        p.left_pitch = p.right_pitch = a_pitch;
+        p.out = ws + plan.b;
+        p.k = static_cast<uint32_t>(plan.m);
+        p.f_acc = static_cast<float>(std::ldexp(k[2], eb - 2 * ea));
+        p.f_aux = static_cast<float>(std::ldexp(k[1], eb - ea));
+        set_cut(p, plan.poly);
+        if ((e = product<kSym>(p, out, plan.poly.side, st)) != hipSuccess) return e;
+        left = p.out;
+        el = eb;
+        by = 1.0;
+      }
+      bound = ortho_bound(bound, k) * kSlack;
+      const bool last = s + 1 == a.steps;
+      const int eo = last ? 0 : exponent_for(bound);
+      const double scale = last ? a.scale : 1.0;
+      p.left = left;  // X <- a X + B X
+      p.left_plane = a_plane;
+      p.left_next = plan.a_bytes;
+      p.left_pitch = a_pitch;
+      p.right = p.aux = x;
+      p.right_plane = x_plane;
+      p.right_next = plan.x_bytes;
+      p.right_pitch = x_pitch;
+      p.out = other;
+      p.out_plane = x_plane;
+      p.out_next = plan.x_bytes;
+      p.out_pitch = x_pitch;
+      p.cols = static_cast<uint32_t>(plan.n);
+      p.k = static_cast<uint32_t>(plan.m);
+      p.f_acc = static_cast<float>(std::ldexp(by * scale, eo - el - ex));
+      p.f_aux = static_cast<float>(std::ldexp(k[0] * scale, eo - ex));
+      set_cut(p, plan.mid);
+      e = last ? product<kLast>(p, out, plan.mid.side, st) : product<kMid>(p, out, plan.mid.side, st);
+      if (e != hipSuccess) return e;
+      std::swap(x, other);
+      ex = eo;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace lc

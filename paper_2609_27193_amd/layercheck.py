@@ -37,7 +37,8 @@ EXPORTED = ("lc_query_build", "lc_query_layout", "lc_init_layout", "lc_score_lay
             "lc_read_state", "lc_record_bytes", "lc_destroy", "lc_last_error", "lc_score_layers_static",
             "lc_embedding_forward", "lc_embedding_backward", "lc_embedding_backward_workspace", "lc_act_save",
             "lc_act_load", "lc_norm_forward", "lc_norm_backward", "lc_norm_backward_workspace", "lc_linear_wgrad",
-            "lc_linear_wgrad_workspace", "lc_residual_norm_forward", "lc_residual_norm_backward", "lc_muon_step_score")
+            "lc_linear_wgrad_workspace", "lc_residual_norm_forward", "lc_residual_norm_backward", "lc_muon_step_score",
+            "lc_orthogonalize", "lc_orthogonalize_workspace")
 
 
 class lc_segment(C.Structure):
@@ -100,6 +101,11 @@ class lc_saved_act(C.Structure):
 class lc_norm_params(C.Structure):
     _fields_ = [("kind", C.c_int32), ("param_dtype", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p),
                 ("eps", C.c_double)]
+
+
+class lc_orthogonalize_params(C.Structure):
+    _fields_ = [("steps", C.c_uint32), ("nesterov", C.c_int32), ("momentum", C.c_double), ("eps", C.c_double),
+                ("scale", C.c_double), ("coefs", C.POINTER(C.c_double))]
 
 
 class LCError(RuntimeError):
@@ -172,6 +178,9 @@ def load_library(path: str = LIB_PATH):
                                                     C.c_void_p, P(lc_saved_act), P(lc_matrix), P(lc_matrix), C.c_void_p,
                                                     C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
             "lc_linear_wgrad_workspace": (C.c_uint64, [C.c_uint64, C.c_uint64, C.c_uint64]),
+            "lc_orthogonalize_workspace": (C.c_uint64, [C.c_uint32, C.c_uint64, C.c_uint64, C.c_int32]),
+            "lc_orthogonalize": (C.c_int, [P(lc_orthogonalize_params), C.c_uint32, P(lc_matrix), P(lc_matrix), P(lc_matrix),
+                                           C.c_void_p, C.c_uint64, C.c_void_p]),
             "lc_linear_wgrad": (C.c_int, [P(lc_matrix), P(lc_saved_act), C.c_void_p, C.c_void_p, C.c_int32,
                                           P(lc_matrix), C.c_void_p, C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]),
         }
@@ -543,6 +552,32 @@ def lc_linear_wgrad(dy: lc_matrix, saved: lc_saved_act, dweight: lc_matrix, work
     _check(load_library().lc_linear_wgrad(dy, saved, col_scale or None, col_shift or None, param_dtype, dweight,
                                           dbias or None, int(accumulate), workspace or None, workspace_bytes,
                                           stream or None), "lc_linear_wgrad")
+
+
+def orthogonalize_params(steps: int, coefs: Optional[Sequence] = None, momentum: float = 0.0, nesterov: bool = False,
+                         eps: float = 1e-7, scale: float = 1.0) -> lc_orthogonalize_params:
+    """``coefs``: (a, b, c) of every step, or one such triple for each; None: the library's."""
+    p = lc_orthogonalize_params(steps, int(nesterov), momentum, eps, scale, None)
+    if coefs is not None:
+        flat = [float(x) for t in coefs for x in t] if hasattr(coefs[0], "__len__") else [float(x) for x in coefs] * steps
+        if len(flat) != 3 * steps:
+            raise ValueError(f"{len(flat)} coefficients for {steps} steps of three")
+        p.coefs = C.cast((C.c_double * len(flat))(*flat), C.POINTER(C.c_double))
+    return p
+
+
+def lc_orthogonalize_workspace(n_matrices: int, rows: int, cols: int, out_dtype: int) -> int:
+    return load_library().lc_orthogonalize_workspace(n_matrices, rows, cols, out_dtype)
+
+
+def lc_orthogonalize(params: lc_orthogonalize_params, grads: Sequence[lc_matrix], out: Sequence[lc_matrix], workspace: int,
+                     workspace_bytes: int, momenta: Optional[Sequence[lc_matrix]] = None, stream: int = 0) -> None:
+    n = len(grads)
+    if len(out) != n or (momenta is not None and len(momenta) != n):
+        raise ValueError("grads, out and momenta differ in number")
+    many = lc_matrix * n
+    _check(load_library().lc_orthogonalize(params, n, many(*grads), None if momenta is None else many(*momenta), many(*out),
+                                           workspace or None, workspace_bytes, stream or None), "lc_orthogonalize")
 
 
 def lc_record_bytes(ctx, layer: int) -> int:

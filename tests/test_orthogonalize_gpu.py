@@ -1,0 +1,369 @@
+"""The orthogonalised update against its formula in 64 bits.
+
+Where every product and sum is a whole number that the planes hold (11 bits each), the result has to be equal bit for bit:
+matrices of -1, 0 and 1 with 4^k entries that are not zero have a norm of 2^k.  That test holds all indices, paddings, planes and
+orders.  The roundings are held by bounds: HALF = 2^-11 for a rounding to one plane, TWO = 2^-22 for two of them (the rest of a
+plane's rounding, rounded again; TWO leaves twice that), U32 = 2^-24 for an fp32 operation."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_27193_amd import layercheck as LC
+from tests.test_operators_gpu import DT, U32, Guarded, close, gen, space, stream
+
+pytestmark = pytest.mark.gpu
+
+HALF, TWO = 2.0 ** -11, 2.0 ** -21  # two planes: 2^-22, and as much again
+# The first X is held times 2^14 (its bound 1.02 lies between 1 and 2), and fp16 has steps of 2^-24 at the least: half of one is
+# what one plane cuts off; the second holds the rest times 2^11.
+DENORMAL = 2.0 ** (-25 - 14)
+STEEP, CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
+
+
+def call(grads, out_dtype, steps=5, coefs=None, momenta=None, momentum=0.95, nesterov=False, eps=0.0, scale=1.0, pad=0, off=0):
+    """Guarded results of Guarded gradients; what lies around them and behind the workspace is looked at."""
+    n, rows, cols = len(grads), grads[0].rows, grads[0].cols
+    outs = [Guarded(rows, cols, DT[out_dtype][0], pad, off) for _ in grads]
+    need = LC.lc_orthogonalize_workspace(n, rows, cols, DT[out_dtype][1])
+    buf, ws, _ = space(need)
+    prm = LC.orthogonalize_params(steps, coefs, momentum, nesterov, eps, scale)
+    LC.lc_orthogonalize(prm, [g.matrix() for g in grads], [o.matrix() for o in outs], ws, need,
+                        momenta=None if momenta is None else [m.matrix() for m in momenta], stream=stream())
+    assert bool((buf[need:] == 0xA5).all())
+    assert all(t.intact() for t in grads + outs + (momenta or []))
+    return outs
+
+
+def formula(u, steps, coefs, eps=0.0, scale=1.0):
+    x = u.double() / (torch.linalg.vector_norm(u.double()) + eps)
+    tall = x.shape[0] > x.shape[1]
+    x = (x.t() if tall else x).contiguous()
+    for _ in range(steps):
+        a = x @ x.t().contiguous()
+        x = coefs[0] * x + (coefs[1] * a + coefs[2] * (a @ a)) @ x
+    return (x.t() if tall else x) * scale
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (3, 5), (63, 65), (64, 64), (65, 200), (130, 129), (200, 1000), (1000, 96), (257, 513), (700, 650)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("kind", ["plain", "momentum", "nesterov"])
+@pytest.mark.parametrize("pad,off", [(0, 0), (5, 3)])
+def test_update_norm_and_places(rows, cols, dtype, out, kind, pad, off):
+    """One step of a = 1, b = c = 0: u over its norm, an element at a time."""
+    g = gen(rows * 31 + cols)
+    n, mu = 3, 0.95
+    size = 10.0 ** torch.randint(-6, 3, (1,), generator=g, device="cuda").item()
+    grads = [Guarded(rows, cols, DT[dtype][0], pad, off, torch.randn(rows, cols, generator=g, device="cuda") * size) for _ in range(n)]
+    bufs = None if kind == "plain" else [Guarded(rows, cols, torch.float32, pad, off, torch.randn(rows, cols, generator=g, device="cuda") * size)
+                                         for _ in range(n)]
+    before = None if bufs is None else [b.view.clone() for b in bufs]
+    outs = call(grads, out, 1, (1, 0, 0), bufs, mu, kind == "nesterov", 1e-3 * size, 0.25, pad, off)
+    m32 = torch.tensor(mu).double().item()  # what the kernel multiplies by
+    for z in range(n):
+        u = grads[z].view.double()
+        u_tol = torch.zeros_like(u)
+        if bufs is not None:
+            new = u + m32 * before[z].double()
+            close(bufs[z].view, new, U32 * new.abs())
+            kept = bufs[z].view.double()  # the momentum as it is kept enters
+            u, u_tol = (u + m32 * kept, U32 * (u + m32 * kept).abs()) if kind == "nesterov" else (kept, u_tol)
+        norm = torch.linalg.vector_norm(u)
+        want = 0.25 * u / (norm + 1e-3 * size)
+        held = TWO if out == "f32" else HALF
+        # the norm is of 64 bits; X is one fp32 rounding, then the planes', then the factor's, then the result's
+        close(outs[z].view, want, (held + DT[out][2] + 6 * U32) * want.abs() + 0.25 * u_tol / norm + 0.25 * DENORMAL)
+
+
+def whole(rows, cols, log4, seed, dtype, pad=0, off=0):
+    """A matrix of -1, 0, 1 whose norm is 2^log4."""
+    g = gen(seed)
+    flat = torch.zeros(rows * cols, device="cuda")
+    at = torch.randperm(rows * cols, generator=g, device="cuda")[:4 ** log4]
+    flat[at] = torch.randint(0, 2, (4 ** log4,), generator=g, device="cuda").float() * 2 - 1
+    return Guarded(rows, cols, DT[dtype][0], pad, off, flat.view(rows, cols))
+
+
+# rows, cols, log4, matrices: dense ones, whose A A takes both planes, and thin ones
+WHOLE = [(64, 256, 7, 2), (256, 64, 7, 1), (100, 700, 8, 3), (129, 130, 6, 2), (1, 300, 4, 1), (5, 4096, 7, 2), (2000, 33, 8, 2),
+         (40, 9000, 9, 1), (513, 1100, 9, 1), (1030, 770, 9, 2), (300, 40000, 9, 1), (2050, 1900, 10, 1), (1500, 1500, 10, 4)]
+
+
+@pytest.mark.parametrize("rows,cols,log4,n", WHOLE)
+@pytest.mark.parametrize("coefs", [(1.0, 1.0, 0.0), (2.0, -1.0, 1.0), (0.0, 0.0, 1.0)])
+@pytest.mark.parametrize("pad,off", [(0, 0), (3, 1)])
+def test_whole_numbers_come_out_exactly(rows, cols, log4, n, coefs, pad, off):
+    """One step in fp32: X is -1, 0, 1 (times 2^-log4), whose second plane is zero.  A's whole numbers fit both planes (22 bits);
+    up to 2^11 they fit one, and then A A is exact in fp32 too.  Where b A and A A, which are of different units, do not fit the
+    planes together, or the result fp32, their bounds are left."""
+    grads = [whole(rows, cols, log4, s, "f32", pad, off) for s in range(n)]
+    outs = call(grads, "f32", 1, coefs, pad=pad, off=off)
+    for g, o in zip(grads, outs):
+        x = g.view.double()
+        x = (x.t() if rows > cols else x).contiguous()
+        a = x @ x.t().contiguous()
+        # X in units of 2^-log4, A of 4^-log4, B of that or, with A A, its square
+        unit = 4.0 ** log4
+        power = unit ** 2 if coefs[2] else unit
+        aa, b_a = a @ a * coefs[2], a * coefs[1] * (unit if coefs[2] else 1.0)
+        b = b_a + aa
+        want = coefs[0] * power * x + b @ x
+        exact = want.abs().max() < 2.0 ** 24 and b.abs().max() < 2.0 ** 22 and a.abs().max() <= (2.0 ** 11 if coefs[2] else 2.0 ** 22)
+        size = (b_a.abs() + abs(coefs[2]) * (a.abs() @ a.abs())) @ x.abs()
+        tol = 0.0 if exact else (4 * TWO + 8 * U32) * size + 4 * U32 * want.abs()
+        assert exact or coefs[2] != 0
+        back = lambda t: (t.t() if rows > cols else t) / power * 2.0 ** -log4  # noqa: E731
+        if exact:
+            assert torch.equal(o.view.double(), back(want))
+        else:
+            close(o.view, back(want), back(tol))
+
+
+@pytest.mark.parametrize("rows,cols,log4,n", [(64, 256, 5, 3), (700, 90, 5, 2), (300, 300, 5, 2), (1300, 1200, 6, 1), (40, 9000, 6, 2),
+                                              (4100, 4096, 6, 5)])
+def test_whole_numbers_in_one_plane(rows, cols, log4, n):
+    """Thin matrices, whose A, and mostly A A, stays below 2^11: a bf16 result is then the exact one, rounded once."""
+    grads = [whole(rows, cols, log4, 50 + s, "bf16") for s in range(n)]
+    for coefs in ((1.0, 1.0, 0.0), (0.0, 0.0, 1.0)):
+        outs = call(grads, "bf16", 1, coefs)
+        for g, o in zip(grads, outs):
+            x = g.view.double()
+            x = (x.t() if rows > cols else x).contiguous()
+            a = x @ x.t().contiguous()
+            b = a @ a if coefs[2] else a
+            unit = 4.0 ** log4
+            if coefs[2] and b.abs().max() > 2048:
+                continue
+            assert b.abs().max() <= 2048
+            want = (coefs[0] * x + b @ x / unit if not coefs[2] else b @ x / unit ** 2) * 2.0 ** -log4
+            want = want.t() if rows > cols else want
+            assert torch.equal(o.view, want.float().to(torch.bfloat16))  # a sum of whole numbers below 2^24: exact in fp32
+
+
+@pytest.mark.parametrize("rows,cols", [(3, 5), (64, 64), (65, 300), (400, 129), (520, 520), (96, 5000)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("coefs", [STEEP, CUBIC])
+def test_one_step_an_element_at_a_time(rows, cols, out, coefs):
+    """First-order bounds, formed from absolute values: what each rounding does to what follows from it."""
+    g = gen(rows + cols)
+    grad = Guarded(rows, cols, torch.float32, value=torch.randn(rows, cols, generator=g, device="cuda"))
+    got = call([grad], out, 1, coefs, eps=1e-7)[0]
+    x = grad.view.double()
+    x = x / (torch.linalg.vector_norm(x) + 1e-7)
+    x = (x.t() if rows > cols else x).contiguous()
+    h = TWO if out == "f32" else HALF
+    m, n = x.shape
+    a, b, c = coefs
+    ax = x.abs()
+    dx = (h + 2 * U32) * ax + 2.0 ** -36  # (a denormal plane cuts off at 2^-25 times 2^-14, X's power of two)
+    A = x @ x.t().contiguous()
+    dA = dx @ ax.t().contiguous()
+    dA = dA + dA.t() + n * U32 * (ax @ ax.t().contiguous()) + (h + 2 * U32) * A.abs() + 2.0 ** -36
+    B = b * A + c * (A @ A)
+    dB = abs(b) * dA + abs(c) * (dA @ A.abs() + A.abs() @ dA + m * U32 * (A.abs() @ A.abs())) + (h + 4 * U32) * B.abs() + 2.0 ** -35
+    want = a * x + B @ x
+    tol = abs(a) * dx + dB @ ax + B.abs() @ dx + m * U32 * (B.abs() @ ax) + (DT[out][2] + 4 * U32) * want.abs()
+    if rows > cols:
+        want, tol = want.t(), tol.t()
+    close(got.view, want, tol * (1 + 2.0 ** -6))
+
+
+def steps_bound(x, steps, coefs, h):
+    """A bound on the Frobenius norm of the result's error.
+
+    A step is an odd function of X's singular values; its derivative, as a map of matrices, is at most the largest slope L of
+    that function on [-s, s], s the largest singular value.  A step's own roundings are those of X, A and B (each h of its norm
+    at most, entering through b, c and X) and of the sums."""
+    err = 0.0
+    a, b, c = (abs(t) for t in coefs)
+    m, n = x.shape
+    for _ in range(steps):
+        s = torch.linalg.matrix_norm(x, 2).item() * 1.02
+        grid = torch.linspace(0, s, 4001, dtype=torch.float64)
+        slope = (coefs[0] + 3 * coefs[1] * grid ** 2 + 5 * coefs[2] * grid ** 4).abs().max().item()
+        A = x @ x.t().contiguous()
+        B = coefs[1] * A + coefs[2] * (A @ A)
+        fro = lambda t: torch.linalg.matrix_norm(t).item()  # noqa: E731
+        sums = (n + 2 * m) * U32 * (b * fro(x) ** 2 * s + c * fro(A) ** 2 * s + fro(B) * fro(x))
+        dA = h * fro(A)
+        own = slope * h * fro(x) + (b + 2 * c * s * s) * dA * s + h * fro(B) * s + sums
+        err = slope * err + own
+        x = coefs[0] * x + B @ x
+    return err, x
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 40), (200, 700), (640, 130), (512, 512)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("coefs", [STEEP, CUBIC])
+def test_five_steps(rows, cols, out, coefs):
+    g = gen(3 * rows + cols)
+    grad = Guarded(rows, cols, torch.float32, value=torch.randn(rows, cols, generator=g, device="cuda") * 1e-4)
+    got = call([grad], out, 5, coefs, eps=1e-7, scale=2.0)[0].view.double()
+    x = grad.view.double()
+    x = x / (torch.linalg.vector_norm(x) + 1e-7)
+    x = (x.t() if rows > cols else x).contiguous()
+    err, want = steps_bound(x, 5, coefs, TWO if out == "f32" else HALF)
+    want = 2 * (want.t() if rows > cols else want)
+    off = torch.linalg.matrix_norm(got - want).item()
+    assert off <= 2 * err + DT[out][2] * torch.linalg.matrix_norm(want).item(), (off, err)
+    if coefs == STEEP and rows != cols:  # what it is for: every singular value near one
+        sv = torch.linalg.svdvals((got / 2).cpu())
+        assert 0.6 < sv.min() and sv.max() < 1.25
+
+
+def test_coefficients_of_each_step():
+    """The defaults, one triple for every step, and a triple of each: the same where they are the same, and in their order."""
+    g = gen(2)
+    grad = Guarded(70, 90, torch.float32, value=torch.randn(70, 90, generator=g, device="cuda"))
+    a, b, c = (call([grad], "f32", 3, k)[0].view for k in (None, STEEP, [STEEP] * 3))
+    assert torch.equal(a, b) and torch.equal(a, c)
+    got = call([grad], "f32", 2, [STEEP, CUBIC])[0].view.double()
+    want = formula(formula(grad.view, 1, STEEP) * 1.0, 0, CUBIC)
+    x = formula(grad.view, 1, STEEP)
+    want = 1.5 * x - 0.5 * (x @ x.t().contiguous()) @ x
+    assert torch.linalg.matrix_norm(got - want) <= 1e-5 * torch.linalg.matrix_norm(want)  # 22 bits, a dozen roundings raised by 4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_edges(dtype):
+    """Zeros give zeros (with no eps either), what is not finite gives NaN in its own matrix alone, and sizes do not matter."""
+    g = gen(9)
+    rows, cols = 70, 150
+    base = [torch.randn(rows, cols, generator=g, device="cuda") for _ in range(6)]
+    base[1] = torch.zeros(rows, cols, device="cuda")
+    base[2][3, 149] = math.nan
+    base[3][69, 0] = math.inf
+    base[4] *= 1e-30
+    base[5] *= 1e30
+    grads = [Guarded(rows, cols, DT[dtype][0], value=t) for t in base]
+    outs = [o.view for o in call(grads, dtype, 5, STEEP)]
+    assert not bool(outs[1].any())
+    assert bool(torch.isnan(outs[2]).all()) and bool(torch.isnan(outs[3]).all())
+    fine = [Guarded(rows, cols, DT[dtype][0], value=base[0 if i in (2, 3) else i]) for i in range(6)]
+    again = [o.view for o in call(fine, dtype, 5, STEEP)]
+    for i in (0, 1, 4, 5):
+        assert torch.equal(outs[i], again[i])
+    for i in (4, 5):
+        want = formula(grads[i].view, 5, STEEP)
+        off = torch.linalg.matrix_norm(outs[i].double() - want) / torch.linalg.matrix_norm(want)
+        assert off <= (3e-2 if dtype == "bf16" else 5e-5)  # as in test_five_steps: some 60 roundings' size, raised
+    zero = [Guarded(rows, cols, torch.float32, value=torch.zeros(rows, cols)) for _ in range(2)]
+    bufs = [Guarded(rows, cols, torch.float32, value=b) for b in (torch.zeros(rows, cols), base[0])]
+    o = call(zero, dtype, 5, STEEP, bufs, 0.0, True)
+    assert not bool(o[0].view.any()) and not bool(o[1].view.any()) and not bool(bufs[1].view.any())  # mu 0: nothing is kept
+
+
+def test_nothing_to_do():
+    prm = LC.orthogonalize_params(5)
+    LC.lc_orthogonalize(prm, [], [], 0, 0, stream=stream())
+    empty = LC.matrix(0, 0, 8, LC.LC_DT_F32)
+    LC.lc_orthogonalize(prm, [empty], [empty], 0, 0, stream=stream())
+    assert LC.lc_orthogonalize_workspace(0, 8, 8, LC.LC_DT_F32) == 0
+
+
+def test_columns_of_one_buffer():
+    """Matrices side by side in one array, results in another: the same bits as apart."""
+    g = gen(5)
+    wide = torch.randn(90, 3 * 40, generator=g, device="cuda")
+    out = torch.zeros_like(wide)
+    prm = LC.orthogonalize_params(5)
+    need = LC.lc_orthogonalize_workspace(3, 90, 40, LC.LC_DT_F32)
+    buf, ws, _ = space(need)
+    part = lambda t, i: LC.matrix(t.data_ptr() + 160 * i, 90, 40, LC.LC_DT_F32, 120)  # noqa: E731
+    LC.lc_orthogonalize(prm, [part(wide, i) for i in range(3)], [part(out, i) for i in range(3)], ws, need, stream=stream())
+    apart = call([Guarded(90, 40, torch.float32, value=wide[:, 40 * i:40 * i + 40]) for i in range(3)], "f32", 5, eps=1e-7)
+    for i, o in enumerate(apart):
+        assert torch.equal(out[:, 40 * i:40 * i + 40], o.view)
+
+
+def test_sixty_four_matrices():
+    grads = [whole(70, 40, 4, s, "f32") for s in range(64)]
+    outs = call(grads, "f32", 1, (1.0, 1.0, 0.0))
+    for g, o in zip(grads, outs):
+        x = g.view.double()
+        assert torch.equal(o.view.double(), (x + x @ (x.t().contiguous() @ x) / 256) / 16)
+
+
+def optimizer(seed, rows=200, cols=330, n=3):
+    """A momentum, its orthogonalised update and the step that takes it: (enqueue, results, what they need)."""
+    g = gen(seed)
+    grads = [torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(n)]
+    bufs = [torch.zeros(rows, cols, device="cuda") for _ in range(n)]
+    outs = [torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda") for _ in range(n)]
+    need = LC.lc_orthogonalize_workspace(n, rows, cols, LC.LC_DT_BF16)
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    prm = LC.orthogonalize_params(5, None, 0.95, True, 1e-7, 2.0)
+    M = lambda t: LC.matrix(t.data_ptr(), rows, cols, LC.LC_DT_BF16 if t.dtype == torch.bfloat16 else LC.LC_DT_F32)  # noqa: E731
+
+    def enqueue():
+        LC.lc_orthogonalize(prm, [M(t) for t in grads], [M(t) for t in outs], ws.data_ptr(), need, momenta=[M(t) for t in bufs],
+                            stream=stream())
+
+    return enqueue, outs, bufs, (grads, ws)
+
+
+def test_calls_in_a_graph():
+    """Replays go on from the momentum that the one before left, as eager calls do."""
+    a, b = optimizer(1), optimizer(1)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    a[0]()  # first, eagerly
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            a[0]()
+    b[0]()
+    for i in range(4):
+        torch.cuda.synchronize()
+        assert all(torch.equal(s, t) for s, t in zip(a[1] + a[2], b[1] + b[2])), i
+        for t in a[1] + b[1]:
+            t.fill_(3)
+        graph.replay()
+        b[0]()
+
+
+def test_calls_on_two_streams():
+    steps, want = [optimizer(s) for s in (1, 2)], [optimizer(s) for s in (1, 2)]
+    for _ in range(3):
+        for w in want:
+            w[0]()
+    streams = [torch.cuda.Stream() for _ in steps]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for st, s in zip(streams, steps):
+            with torch.cuda.stream(st):
+                s[0]()
+    torch.cuda.synchronize()
+    for s, w in zip(steps, want):
+        assert all(torch.equal(x, y) for x, y in zip(s[1] + s[2], w[1] + w[2]))
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 4 GB apart; and a matrix whose planes are larger than 4 GB, with one entry in some rows and columns (A is then the
+    identity on those rows, and X + A X is 2 X)."""
+    wide = torch.zeros(2, 1 << 30, device="cuda")
+    src, out = wide[:, :40], wide[:, 1000:1040]
+    src.copy_(whole(2, 40, 3, 1, "f32").view)
+    keep = src.clone()
+    need = LC.lc_orthogonalize_workspace(1, 2, 40, LC.LC_DT_F32)
+    buf, ws, _ = space(need)
+    prm = LC.orthogonalize_params(1, (1, 0, 0), eps=0.0, scale=8.0)
+    M = lambda t, r, c: LC.matrix(t.data_ptr(), r, c, LC.LC_DT_F32 if t.dtype == torch.float32 else LC.LC_DT_BF16, t.stride(0))  # noqa: E731
+    LC.lc_orthogonalize(prm, [M(src, 2, 40)], [M(out, 2, 40)], ws, need, stream=stream())
+    assert torch.equal(out, keep)
+    del wide, src, out
+    rows, cols = 50001, 46500
+    g = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    k = 4 ** 7
+    r = torch.arange(k, device="cuda") * 3 + (rows - 3 * k)
+    c = cols - 1 - torch.arange(k, device="cuda") * 2
+    g[r, c] = 1
+    out = torch.empty_like(g)
+    need = LC.lc_orthogonalize_workspace(1, rows, cols, LC.LC_DT_BF16)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    prm = LC.orthogonalize_params(1, (1.0, float(k), 0.0), eps=0.0, scale=128.0)
+    LC.lc_orthogonalize(prm, [M(g, rows, cols)], [M(out, rows, cols)], ws.data_ptr(), need, stream=stream())
+    g.mul_(2)
+    assert torch.equal(out, g)
