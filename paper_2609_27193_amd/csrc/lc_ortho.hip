@@ -18,7 +18,11 @@
 // norm, a bf16 result's rounding itself 1.7e-3; bf16 throughout 1.2e-2; two planes
 // 2.6e-7, fp32 throughout 1.7e-7.  Sums, norms and the momentum are fp32 or wider.
 //
-// Inside, sides are padded to multiples of 64 with zeros, which stay zeros.
+// Inside, sides are padded to multiples of 64 with zeros, which stay zeros, and a
+// plane lies in panels of 32 columns: a row's 64 bytes of a panel, the next row's
+// behind it.  What a step of a product takes of either operand is then whole
+// kilobytes of neighbours (4096^3 with tiles of 256, in rows as they are 124 us, in
+// panels 114; its upper half with tiles of 192 100 and 78).
 #include <algorithm>
 #include <cmath>
 
@@ -41,7 +45,8 @@ typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
 constexpr uint32_t kThreads = 256;  // four waves
 constexpr uint32_t kPad = 64;       // of both sides
-constexpr uint32_t kStep = 64;      // of the sum, in LDS at a time
+constexpr uint32_t kStep = 32;      // of the sum, in LDS at a time
+constexpr uint32_t kPanel = 32;     // columns
 constexpr uint32_t kNormBlocks = 256;  // of one matrix, at most
 
 // ---- the update and its norm -----------------------------------------------------------
@@ -102,35 +107,57 @@ __global__ __launch_bounds__(kThreads) void ortho_norm_kernel(OrthoIn a, double*
 
 // fp16 planes of eight neighbours: the value's, and of two the rest's times 2^11.
 constexpr float kRestUp = 2048.0f;
+template <int PLANES>
 __device__ __forceinline__ void store_planes8(uint64_t p, uint64_t plane, const float (&v)[8]) {
   u32x4 hi, lo;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const f16x2 h = {static_cast<_Float16>(v[e]), static_cast<_Float16>(v[e + 1])};
     hi[e / 2] = __builtin_bit_cast(uint32_t, h);
-    const f16x2 l = {static_cast<_Float16>((v[e] - static_cast<float>(h[0])) * kRestUp),
-                     static_cast<_Float16>((v[e + 1] - static_cast<float>(h[1])) * kRestUp)};
-    lo[e / 2] = __builtin_bit_cast(uint32_t, l);
+    if constexpr (PLANES == 2) {
+      const f16x2 l = {static_cast<_Float16>((v[e] - static_cast<float>(h[0])) * kRestUp),
+                       static_cast<_Float16>((v[e + 1] - static_cast<float>(h[1])) * kRestUp)};
+      lo[e / 2] = __builtin_bit_cast(uint32_t, l);
+    }
   }
   *(g_u32x4*)p = hi;
-  if (plane) *(g_u32x4*)(p + plane) = lo;
+  if constexpr (PLANES == 2) *(g_u32x4*)(p + plane) = lo;
 }
 typedef const __attribute__((address_space(1))) u32x4 gc_u32x4;
+template <int PLANES>
+struct Planes8 {
+  u32x4 v[PLANES];
+};
+template <int PLANES>
+__device__ __forceinline__ Planes8<PLANES> load_planes(uint64_t p, uint64_t plane) {
+  Planes8<PLANES> x;
+  x.v[0] = *(gc_u32x4*)p;
+  if constexpr (PLANES == 2) x.v[1] = *(gc_u32x4*)(p + plane);
+  return x;
+}
 // Two elements of a plane to fp32.
 __device__ __forceinline__ f32x2 halves(uint32_t w) {
   const f16x2 h = __builtin_bit_cast(f16x2, w);
   return f32x2{static_cast<float>(h[0]), static_cast<float>(h[1])};
 }
-__device__ __forceinline__ void load_planes8(uint64_t p, uint64_t plane, float (&v)[8]) {
-  const u32x4 hi = *(gc_u32x4*)p;
-  u32x4 lo = {0, 0, 0, 0};
-  if (plane) lo = *(gc_u32x4*)(p + plane);
+template <int PLANES>
+__device__ __forceinline__ void unpack_planes(const Planes8<PLANES>& x, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
-    const f32x2 h = halves(hi[e / 2]), l = halves(lo[e / 2]);
-    v[e] = __builtin_fmaf(l[0], 1.0f / kRestUp, h[0]);
-    v[e + 1] = __builtin_fmaf(l[1], 1.0f / kRestUp, h[1]);
+    const f32x2 h = halves(x.v[0][e / 2]);
+    v[e] = h[0];
+    v[e + 1] = h[1];
+    if constexpr (PLANES == 2) {
+      const f32x2 l = halves(x.v[1][e / 2]);
+      v[e] = __builtin_fmaf(l[0], 1.0f / kRestUp, v[e]);
+      v[e + 1] = __builtin_fmaf(l[1], 1.0f / kRestUp, v[e + 1]);
+    }
   }
+}
+
+// Element (row, col) of a plane whose panels are `panel` bytes apart.
+__device__ __forceinline__ uint64_t in_panels(uint64_t row, uint32_t col, uint64_t panel) {
+  return col / kPanel * panel + row * (kPanel * 2) + col % kPanel * 2;
 }
 
 // X of the group: u over its norm, m x n, padded.
@@ -140,7 +167,7 @@ struct OrthoX {
   double eps, power;        // what X is held times
 };
 // Blocks of 64 x 64 of a matrix: a tall one goes through LDS.
-template <int DT, bool TALL>
+template <int DT, bool TALL, int PLANES>
 __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX o, const double* sums, uint32_t n_sums) {
   __shared__ double red[kThreads / 64];
   __shared__ float tile[TALL ? 64 : 1][65];
@@ -167,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX 
 #pragma unroll
         for (int e = 0; e < 8; ++e) tile[lr][lc + e] = u[e];
       } else {
-        store_planes8(base + (static_cast<uint64_t>(row) * o.n + c) * 2, o.plane, u);
+        store_planes8<PLANES>(base + in_panels(row, c, o.m * (kPanel * 2)), o.plane, u);
       }
     }
     if constexpr (TALL) {
@@ -178,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX 
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[lr + e][lc];
-        store_planes8(base + (static_cast<uint64_t>(c0 + lc) * o.n + r0 + lr) * 2, o.plane, v);
+        store_planes8<PLANES>(base + in_panels(c0 + lc, r0 + lr, o.m * (kPanel * 2)), o.plane, v);
       }
       __syncthreads();
     }
@@ -193,7 +220,7 @@ struct OrthoProduct {
   uint64_t left, right, aux, out;              // of the group's first matrix
   uint64_t left_plane, right_plane, out_plane; // bytes to the second plane; 0: one plane (aux: as out)
   uint64_t left_next, right_next, out_next;    // bytes to the next matrix (aux: as out)
-  uint32_t left_pitch, right_pitch, out_pitch; // bytes from row to row (aux: as out)
+  uint32_t left_panel, right_panel, out_panel; // bytes from panel to panel (aux: as out)
   uint32_t rows, cols, k;                      // multiples of 64
   uint32_t ti, tj, tiles, count;               // tiles down, across and of a matrix; matrices
   uint32_t splits, split_k;                    // parts of the sum and its steps a part
@@ -204,7 +231,7 @@ struct OrthoProduct {
 struct OrthoOut {
   uint64_t data[kOrthoMost], stride[kOrthoMost];
   uint32_t m, n;  // of X, without its padding
-  int dtype, tall;
+  int tall;
 };
 
 __device__ __forceinline__ void ortho_place(const OrthoProduct& p, bool sym, uint32_t t, uint32_t& i, uint32_t& j) {
@@ -219,9 +246,24 @@ __device__ __forceinline__ void ortho_place(const OrthoProduct& p, bool sym, uin
     j = in_g / high;
     i = group * 8 + in_g % high;
   }
+  // the same for the whole block, which the square root hides
+  i = __builtin_amdgcn_readfirstlane(i);
+  j = __builtin_amdgcn_readfirstlane(j);
 }
 
-constexpr int kVmcnt0 = 0x0F70;
+constexpr int kMfma = 0x8, kVmemRead = 0x20, kLdsRead = 0x100;  // kinds of instructions, for their order
+
+// A barrier behind which all waves have what they read from LDS and all but the
+// newest N loads to LDS of each have landed.  A fence would wait for every load.
+template <uint32_t N>
+__device__ __forceinline__ void barrier_lds() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);  // vmcnt(N) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 // A lane's 16 bytes to LDS, the wave's 64 after each other.  The whole offset is in
 // the operand that the bounds check covers.
@@ -229,35 +271,35 @@ __device__ __forceinline__ void load_lds(tile_t t, uint8_t* to, uint32_t off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(t, (lds_void*)to, 16, off, 0, 0, 0);
 }
 
-// Eight neighbours of row i of D from column j on, in the user's type.
+// Eight neighbours of row i of D from column j on, in the result's type.
+template <int DT>
 __device__ __forceinline__ void ortho_out8(const OrthoOut& o, uint32_t z, uint64_t row, uint32_t col, int n, const float (&v)[8]) {
-  if (n <= 0) return;
-  const uint64_t at = row * o.stride[z] + col;
-  if (o.dtype == kBf16) store8<kBf16>(o.data[z] + 2 * at, v, n);
-  else store8<kF32>(o.data[z] + 4 * at, v, n);
+  if (n > 0) store8<DT>(o.data[z] + (row * o.stride[z] + col) * kEsz<DT>, v, n);
 }
 
 constexpr int kSym = 0, kMid = 1, kLast = 2;
 
-// T x T of D a block, four waves of T/2 x T/2, two LDS buffers of a step each that
-// the loads write by themselves.
+// T x T of D a block, four waves of T/2 x T/2.  A step of the sum is 32; the loads
+// write LDS by themselves, four steps on their way in turn, for one wave a SIMD has
+// nothing else to hide the way from HBM with (4096^3: with two steps of 64 160 us).
 //
-// LDS: a row of an operand's step is 128 bytes along the sum (L, and R of SYM), its
-// 16-byte pieces at c ^ row % 8; or, of R as it lies, T columns of one k, its 32-byte
-// slots moved up by k % 4, which spreads the four rows that a transposing read takes.
+// LDS: T rows of an operand's step (L, and R of SYM), of 64 bytes along the sum, whose
+// 16-byte pieces lie at c ^ row / 4 % 4, so that the 16 rows of a quarter read are in
+// different banks; of R as it lies, T / 32 panels of 32 rows of 64 bytes, of which half
+// a transposing read takes four rows, 256 bytes.
 // PLANES: of each operand.
 template <int MODE, int T, int PLANES>
-__global__ __launch_bounds__(kThreads, T == 256 ? 1 : 2) void ortho_product_kernel(OrthoProduct p, OrthoOut o) {
+__global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kernel(OrthoProduct p, OrthoOut o) {
   constexpr bool SYM = MODE == kSym;
   constexpr uint32_t NF = T / 64;             // 32-wide pieces of a wave's side
   constexpr uint32_t kOperand = T * kStep * 2;  // bytes
-  constexpr uint32_t kLoads = T / 32;         // of an operand, a thread
-  constexpr uint32_t kSlots = T / 16;         // of 32 bytes in a row of R as it lies
+  constexpr uint32_t kLoads = T / 64;         // of an operand, a thread
   constexpr uint32_t kOut = T / 2 + 4;        // floats from row to row on their way out
-  constexpr uint32_t kSlab = 32 * kOut * 4;
-  constexpr uint32_t kStage = 2 * kOperand > 2 * kSlab ? 2 * kOperand : 2 * kSlab;
-  __shared__ __align__(1024) uint8_t stage0[kStage];
-  __shared__ __align__(1024) uint8_t stage1[kStage];
+  static_assert(32 * kOut * 4 <= 2 * kOperand, "a wave's rows on their way out lie in one buffer");
+  __shared__ __align__(1024) uint8_t stage0[2 * kOperand];
+  __shared__ __align__(1024) uint8_t stage1[2 * kOperand];
+  __shared__ __align__(1024) uint8_t stage2[2 * kOperand];
+  __shared__ __align__(1024) uint8_t stage3[2 * kOperand];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t items = p.count * p.tiles * p.splits;
   for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
@@ -267,65 +309,67 @@ __global__ __launch_bounds__(kThreads, T == 256 ? 1 : 2) void ortho_product_kern
     ortho_place(p, SYM, tile % p.tiles, ti, tj);
     const uint32_t i0 = ti * T, j0 = tj * T;
     // the steps of this part
-    const uint32_t k_begin = split * p.split_k, k_all = p.k / kStep;
+    const uint32_t k_begin = split * p.split_k, k_all = p.k / kStep;  // split_k is even, as k_all is
     const uint32_t k_end = k_begin + p.split_k < k_all ? k_begin + p.split_k : k_all;
-    uint32_t pass = 0, next_k = 0, last_pass = 0;
-    const uint64_t left = p.left + z * p.left_next + static_cast<uint64_t>(i0) * p.left_pitch;
-    const uint64_t right = p.right + z * p.right_next + (SYM ? static_cast<uint64_t>(j0) * p.right_pitch : 2ull * j0);
+    const uint64_t left = p.left + z * p.left_next + i0 * (kPanel * 2ull);
+    const uint64_t right = p.right + z * p.right_next + (SYM ? j0 * (kPanel * 2ull) : static_cast<uint64_t>(j0 / kPanel) * p.right_panel);
     const uint32_t left_rows = p.rows - i0 < T ? p.rows - i0 : T, right_rows = p.cols - j0 < T ? p.cols - j0 : T;
-    const uint32_t left_at = (wave * 8 + lane / 8) * p.left_pitch + (lane % 8 ^ lane / 8) * 16;
-    uint32_t right_at[kLoads];
-#pragma unroll
-    for (uint32_t q = 0; q < kLoads; ++q) {
-      if constexpr (SYM) {
-        right_at[q] = (q * 32 + wave * 8 + lane / 8) * p.right_pitch + (lane % 8 ^ lane / 8) * 16;
-      } else {
-        const uint32_t piece = (q * 4 + wave) * 64 + lane, row = piece / (2 * kSlots), pos = piece % (2 * kSlots);
-        right_at[q] = row * p.right_pitch + ((pos / 2 + kSlots - row % 4) % kSlots * 2 + pos % 2) * 16;
-      }
-    }
+    // a load takes 16 rows of a panel
+    const uint32_t rows16 = wave * 1024 + lane / 4 * 64 + (lane % 4 ^ lane / 16) * 16;
+    const uint32_t right_at = SYM ? rows16 : wave / 2 * p.right_panel + wave % 2 * 1024 + lane * 16;
+    const uint32_t right_by = SYM ? 4096 : 2 * p.right_panel;  // to the thread's next load
     // Nothing is read behind an operand: rows and columns that are not there are
     // not stored, whatever LDS holds for them.
-    auto load = [&](uint8_t* stage) {
-      const bool on = pass < last_pass;
-      const uint64_t l = left + (pass == 0 ? p.left_plane : 0) + next_k * 128ull;
-      const uint64_t r = right + (pass == 1 ? p.right_plane : 0) + (SYM ? next_k * 128ull : next_k * 64ull * p.right_pitch);
-      const tile_t tl = make_tile(reinterpret_cast<const void*>(l), on ? left_rows * p.left_pitch - next_k * 128 : 0);
-      const tile_t tr = make_tile(reinterpret_cast<const void*>(r), !on ? 0 : SYM ? right_rows * p.right_pitch - next_k * 128
-                                                                                  : kStep * p.right_pitch - 2 * j0);
+    const int left_bytes = static_cast<int>(left_rows * (kPanel * 2));
+    const int right_bytes = static_cast<int>(SYM ? right_rows * (kPanel * 2) : right_rows / kPanel * p.right_panel);
+    const uint64_t left_step = p.left_panel, right_step = SYM ? p.right_panel : kStep * (kPanel * 2);
+    // `next` says where the next step comes from, a half step ahead of its loads: the
+    // scalar unit's work would hold up the products behind a barrier.
+    tile_t from_left, from_right;
+    uint64_t left_next = 0, right_next = 0;
+    int todo = 0, turn = 0;  // steps not yet under way; how many of them are left where the planes change
+    auto next = [&] {
+      from_left = make_tile(reinterpret_cast<const void*>(left_next), todo > 0 ? left_bytes : 0);
+      from_right = make_tile(reinterpret_cast<const void*>(right_next), todo > 0 ? right_bytes : 0);
+      left_next += left_step;
+      right_next += right_step;
+      --todo;
+      if (PLANES == 2 && todo == turn) {
+        left_next = left + k_begin * left_step;
+        right_next = right + p.right_plane + k_begin * right_step;
+      }
+    };
+    auto load_left = [&](uint8_t* stage) {
 #pragma unroll
       for (uint32_t q = 0; q < kLoads; ++q)
-        load_lds(tl, stage + (q * 4 + wave) * 1024, left_at + q * 32 * p.left_pitch);
+        load_lds(from_left, stage + (q * 4 + wave) * 1024, rows16 + q * 4096);
+    };
+    auto load_right = [&](uint8_t* stage) {
 #pragma unroll
-      for (uint32_t q = 0; q < kLoads; ++q) load_lds(tr, stage + kOperand + (q * 4 + wave) * 1024, right_at[q]);
-      if (++next_k == k_end) {
-        next_k = k_begin;
-        ++pass;
-      }
+      for (uint32_t q = 0; q < kLoads; ++q) load_lds(from_right, stage + kOperand + (q * 4 + wave) * 1024, right_at + q * right_by);
     };
     // operands of 16 of the sum
     const uint32_t wi = wave % 2 * (T / 2), wj = wave / 2 * (T / 2);
     f16x8 lf[2][NF], rf[2][NF];
-    const uint32_t x4 = lane % 16 / 4;
-    uint32_t tr_at[NF];
-#pragma unroll
-    for (uint32_t f = 0; f < NF; ++f)
-      tr_at[f] = kOperand + (lane / 32 * 8 + x4) * (T * 2) + (wj / 16 + 2 * f + lane / 16 % 2 + x4) % kSlots * 32 + lane % 4 * 8;
+    // of R as it lies: column lane % 32 of a panel, rows lane / 32 * 8 and on
+    const uint32_t tr_at = kOperand + wj * (kStep * 2) + (lane / 32 * 8 + lane % 16 / 4) * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
     auto fetch = [&](uint8_t* stage, uint32_t to, uint32_t sub) {
-      const uint32_t piece = ((2 * sub + lane / 32) ^ (lane % 8)) * 16;
-#pragma unroll
-      for (uint32_t f = 0; f < NF; ++f) {
+      const uint32_t piece = ((2 * sub + lane / 32) ^ (lane / 4 % 4)) * 16;
+      const auto right_of = [&](uint32_t f) {
         if constexpr (SYM) {
-          rf[to][f] = *(lds_f16x8*)(stage + kOperand + (wj + 32 * f + lane % 32) * 128 + piece);
+          rf[to][f] = *(lds_f16x8*)(stage + kOperand + (wj + 32 * f + lane % 32) * 64 + piece);
         } else {
-          uint8_t* const at = stage + tr_at[f] + sub * 16 * T * 2;
+          uint8_t* const at = stage + tr_at + f * (kPanel * kStep * 2) + sub * 1024;
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * T * 2));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 256));
           rf[to][f] = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
-      }
+      };
+      right_of(0);  // in the order in which the products want them
 #pragma unroll
-      for (uint32_t f = 0; f < NF; ++f) lf[to][f] = *(lds_f16x8*)(stage + (wi + 32 * f + lane % 32) * 128 + piece);
+      for (uint32_t f = 0; f < NF; ++f) lf[to][f] = *(lds_f16x8*)(stage + (wi + 32 * f + lane % 32) * 64 + piece);
+#pragma unroll
+      for (uint32_t f = 1; f < NF; ++f) right_of(f);
     };
     f32x16 acc[NF][NF];  // [j][i] pieces of 32: a lane holds four runs of 4 of j for one i
 #pragma unroll
@@ -340,42 +384,66 @@ __global__ __launch_bounds__(kThreads, T == 256 ? 1 : 2) void ortho_product_kern
 #pragma unroll
         for (uint32_t i = 0; i < NF; ++i) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(rf[of][j], lf[of][i], acc[j][i], 0, 0, 0);
     };
-    // One step out of `cur`: the next operands are read while the ones before them
-    // multiply, and the step behind the next goes into `cur` when all waves have it
-    // in registers.
-    auto step = [&](uint8_t* cur, uint8_t* nxt) {
+    // One step out of `cur`: the operands of each half are read while the half before
+    // it multiplies.  When all waves have the step in registers, the loads of the
+    // fourth behind it go into `cur`, L's in this step's second half, R's in the next
+    // one's first (into `old`): each takes the CU's address unit 16 clocks, and those
+    // of four waves in a row hold up the products behind them.
+    // The order lays reads and loads between the products, or the compiler reads an
+    // operand right before it waits for it.
+    constexpr int kProducts = NF * NF, kReads = (SYM ? 2 : 3) * NF, kPer = (kReads + kProducts - 1) / kProducts;
+    constexpr int kEvery = kProducts / static_cast<int>(kLoads);
+    auto order = [] {
+#pragma unroll
+      for (int t = 0; t < kProducts; ++t) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        if (t * kPer < kReads) __builtin_amdgcn_sched_group_barrier(kLdsRead, kPer, 0);
+        if (t % kEvery == kEvery - 1) __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto step = [&](uint8_t* old, uint8_t* cur, uint8_t* nxt) {
+      __builtin_amdgcn_sched_barrier(0);
       fetch(cur, 1, 1);
+      load_right(old);
+      next();
       multiply(0);
-      fetch(cur, 0, 2);
-      multiply(1);
-      fetch(cur, 1, 3);
-      multiply(0);
-      __builtin_amdgcn_s_waitcnt(kVmcnt0);
-      __syncthreads();
+      order();
+      barrier_lds<4 * kLoads>();  // the next step is there, the two behind it on their way
       fetch(nxt, 0, 0);
-      load(cur);
+      load_left(cur);
       multiply(1);
+      order();
     };
     // first the products of a second plane, of either side, then those of the first
 #pragma unroll 1
     for (uint32_t big = PLANES == 2 ? 0 : 1; big < 2; ++big) {
-      pass = big ? 2 : 0;
-      last_pass = big ? 3 : 2;
-      next_k = k_begin;
-      const uint32_t steps = (k_end - k_begin) * (last_pass - pass);
-      load(stage0);
-      load(stage1);
-      __builtin_amdgcn_s_waitcnt(kVmcnt0);
-      __syncthreads();
-      fetch(stage0, 0, 0);
-      for (uint32_t s = 0; s < steps / 2; ++s) {
-        step(stage0, stage1);
-        step(stage1, stage0);
+      const uint32_t steps = (k_end - k_begin) * (big ? 1 : 2);  // even
+      todo = static_cast<int>(steps);
+      turn = big ? -1 - todo : todo / 2;  // never, with the first planes
+      left_next = left + (big ? 0 : p.left_plane) + k_begin * left_step;
+      right_next = right + k_begin * right_step;
+      for (uint8_t* const stage : {stage0, stage1, stage2}) {
+        next();
+        load_left(stage);
+        load_right(stage);
       }
-      if (steps % 2) step(stage0, stage1);
-      __builtin_amdgcn_s_waitcnt(kVmcnt0);
-      __syncthreads();
+      next();
+      load_left(stage3);
+      barrier_lds<5 * kLoads>();
+      fetch(stage0, 0, 0);
+      for (uint32_t s = 0; s < steps / 4; ++s) {
+        step(stage3, stage0, stage1);
+        step(stage0, stage1, stage2);
+        step(stage1, stage2, stage3);
+        step(stage2, stage3, stage0);
+      }
+      if (steps % 4) {
+        step(stage3, stage0, stage1);
+        step(stage0, stage1, stage2);
+      }
       if (PLANES == 2 && !big) {
+        barrier_lds<0>();
 #pragma unroll
         for (uint32_t j = 0; j < NF; ++j)
 #pragma unroll
@@ -385,61 +453,90 @@ __global__ __launch_bounds__(kThreads, T == 256 ? 1 : 2) void ortho_product_kern
       }
     }
 
-    // out through LDS, 32 rows a wave at a time
-    lds_f32* const mine = (lds_f32*)((wave < 2 ? stage0 : stage1) + wave % 2 * kSlab);
-    constexpr uint32_t kGroups = T / 16;  // of eight columns in a wave's row
+    // out through LDS, 32 rows a wave at a time; the next rows of aux are on their way
+    // meanwhile, clamped to what is there: what is not is not stored
+    constexpr uint32_t kRounds = T / 32;  // of 16 rows of a panel
+    const uint32_t row0 = i0 + wi, col0 = j0 + wj;
     const uint64_t out = p.out + z * p.out_next, aux = p.aux + z * p.out_next;
+    const bool has_aux = p.aux && p.splits == 1;
+    Planes8<PLANES> x[2][kRounds];
+    auto load_aux = [&](uint32_t f) {
+#pragma unroll
+      for (uint32_t r = 0; r < kRounds; ++r) {
+        const uint32_t row = row0 + 32 * f + r % 2 * 16 + lane / 4, col = col0 + r / 2 * kPanel + lane % 4 * 8;
+        const uint64_t at = in_panels(row < p.rows ? row : p.rows - 1, col < p.cols ? col : p.cols - 8, p.out_panel);
+        x[f % 2][r] = load_planes<PLANES>(aux + at, p.out_plane);
+      }
+    };
+    if (has_aux) {
+      load_aux(0);
+      barrier_lds<kRounds * PLANES>();
+    } else {
+      barrier_lds<0>();
+    }
+    lds_f32* const mine = (lds_f32*)(wave < 2 ? (wave == 0 ? stage0 : stage1) : wave == 2 ? stage2 : stage3);
+    const bool turned = SYM ? ti != tj : MODE == kLast;
 #pragma unroll
     for (uint32_t f = 0; f < NF; ++f) {
+      if (has_aux && f + 1 < NF) load_aux(f + 1);
 #pragma unroll
       for (uint32_t j = 0; j < NF; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           *(lds_f32x4*)(mine + lane % 32 * kOut + 32 * j + 8 * r + lane / 32 * 4) =
               f32x4{acc[j][f][4 * r], acc[j][f][4 * r + 1], acc[j][f][4 * r + 2], acc[j][f][4 * r + 3]};
-      const uint32_t row0 = i0 + wi + 32 * f, col0 = j0 + wj;
       if (p.splits > 1) {
         float* const to = p.part + (static_cast<uint64_t>(tile) * p.splits + split) * (T * T) + (wi + 32 * f) * T + wj;
-        for (uint32_t g = lane; g < 32 * kGroups; g += 64) {
-          const uint32_t q = g / kGroups, c = g % kGroups * 8;
+#pragma unroll
+        for (uint32_t r = 0; r < kRounds; ++r) {
+          const uint32_t q = r % 2 * 16 + lane / 4, c = r / 2 * kPanel + lane % 4 * 8;
 #pragma unroll
           for (int h = 0; h < 2; ++h)
             *(f32x4*)(to + q * T + c + 4 * h) = *(lds_f32x4*)(mine + q * kOut + c + 4 * h);
         }
         continue;
       }
-      const bool turned = SYM ? ti != tj : MODE == kLast && o.tall;
-      for (uint32_t g = lane; g < 32 * kGroups; g += 64) {
-        const uint32_t q = g / kGroups, c = g % kGroups * 8, row = row0 + q, col = col0 + c;
-        float v[8], x[8];
+#pragma unroll
+      for (uint32_t r = 0; r < kRounds; ++r) {
+        const uint32_t q = r % 2 * 16 + lane / 4, c = r / 2 * kPanel + lane % 4 * 8, row = row0 + 32 * f + q, col = col0 + c;
+        float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + c + e] * p.f_acc;
-        if (row < p.rows && col < p.cols) {
-          const uint64_t at = static_cast<uint64_t>(row) * p.out_pitch + 2 * col;
-          if (p.aux) {
-            load_planes8(aux + at, p.out_plane, x);
+        if (has_aux) {
+          float y[8];
+          unpack_planes<PLANES>(x[f % 2][r], y);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(p.f_aux, x[e], v[e]);
-          }
-          if (MODE != kLast) store_planes8(out + at, p.out_plane, v);
-          else if (!o.tall && row < o.m) ortho_out8(o, z, row, col, static_cast<int>(o.n) - static_cast<int>(col), v);
+          for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(p.f_aux, y[e], v[e]);
         }
+        if (MODE != kLast && row < p.rows && col < p.cols)
+          store_planes8<PLANES>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
         if (turned) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) mine[q * kOut + c + e] = v[e];
         }
       }
-      if (turned) {  // column j of the slab: 32 neighbours of row j of the other side
-        for (uint32_t g = lane; g < 4 * (T / 2); g += 64) {
-          const uint32_t j = g % (T / 2), c = g / (T / 2) * 8, row = col0 + j, col = row0 + c;
-          float v[8];
+      if (!turned) continue;
+      // the caller's rows, or the other side of the diagonal: four lanes take 32 neighbours of a column of these rows
+      constexpr int kOutType = PLANES == 1 ? kBf16 : kF32;
+#pragma unroll 2
+      for (uint32_t r = 0; r < kRounds; ++r) {
+        constexpr uint32_t kGroups = T / 16;  // of eight columns in a wave's row
+        const uint32_t g = lane + 64 * r;
+        float v[8];
+        if (MODE == kLast && !o.tall) {
+          const uint32_t q = g / kGroups, c = g % kGroups * 8, row = row0 + 32 * f + q, col = col0 + c;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = mine[(c + e) * kOut + j];
-          if (MODE == kLast) {
-            if (row < o.n) ortho_out8(o, z, row, col, static_cast<int>(o.m) - static_cast<int>(col), v);
-          } else if (row < p.cols && col < p.rows) {
-            store_planes8(out + static_cast<uint64_t>(row) * p.out_pitch + 2 * col, p.out_plane, v);
-          }
+          for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + c + e];
+          if (row < o.m) ortho_out8<kOutType>(o, z, row, col, static_cast<int>(o.n) - static_cast<int>(col), v);
+          continue;
+        }
+        const uint32_t j = g / 4, c = g % 4 * 8, row = col0 + j, col = row0 + 32 * f + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = mine[(c + e) * kOut + j];
+        if (MODE == kLast) {
+          if (row < o.n) ortho_out8<kOutType>(o, z, row, col, static_cast<int>(o.m) - static_cast<int>(col), v);
+        } else if (row < p.cols && col < p.rows) {
+          store_planes8<PLANES>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
         }
       }
     }
@@ -447,47 +544,61 @@ __global__ __launch_bounds__(kThreads, T == 256 ? 1 : 2) void ortho_product_kern
   }
 }
 
-// The parts' sums of a symmetric product, in order, to both sides of the diagonal.
+// The parts' sums of a symmetric product, to both sides of the diagonal.  A block
+// takes 8 rows of a panel: 32 groups of eight columns, whose parts eight slices of
+// threads add in turn; the slices' sums are added in order.
+constexpr uint32_t kSlices = 8, kJoinRows = kThreads / kSlices / 4;
+template <int PLANES>
 __global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoProduct p, uint32_t side) {
-  __shared__ float sums[64][65];
-  const uint32_t per_tile = (side / 64) * (side / 64);
+  __shared__ float sums[kSlices][8][kThreads / kSlices];
+  __shared__ float out_rows[kJoinRows][kPanel + 1];
+  const uint32_t across = side / kPanel, per_tile = across * (side / kJoinRows);
   const uint32_t items = p.count * p.tiles * per_tile;
+  const uint32_t own = threadIdx.x % (kThreads / kSlices), slice = threadIdx.x / (kThreads / kSlices);
   for (uint32_t it = blockIdx.x; it < items; it += gridDim.x) {
     const uint32_t tile = it / per_tile, z = tile / p.tiles, sub = it % per_tile;
-    const uint32_t si = sub / (side / 64) * 64, sj = sub % (side / 64) * 64;
+    const uint32_t si = sub / across * kJoinRows, sj = sub % across * kPanel;
     uint32_t ti, tj;
     ortho_place(p, true, tile % p.tiles, ti, tj);
     const uint32_t i0 = ti * side + si, j0 = tj * side + sj;
+    const bool on = i0 < p.rows && j0 < p.cols;  // the same for the block
     const uint64_t out = p.out + z * p.out_next, aux = p.aux + z * p.out_next;
-    const float* const part = p.part + static_cast<uint64_t>(tile) * p.splits * side * side;
-    const bool on = i0 < p.rows && j0 < p.cols;
-    for (uint32_t g = threadIdx.x; on && g < 64 * 8; g += kThreads) {
-      const uint32_t q = g / 8, c = g % 8 * 8;
-      float v[8] = {}, x[8];
-      for (uint32_t s = 0; s < p.splits; ++s) {
-        unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(part + (static_cast<uint64_t>(s) * side + si + q) * side + sj + c)), x);
+    const uint32_t q = own / 4, c = own % 4 * 8;
+    float v[8] = {}, x[8];
+    if (on) {
+      const float* const part = p.part + (static_cast<uint64_t>(tile) * p.splits * side + si + q) * side + sj + c;
+#pragma unroll 4
+      for (uint32_t s = slice; s < p.splits; s += kSlices) {
+        unpack8<kF32>(load8_raw<kF32>(reinterpret_cast<uint64_t>(part + static_cast<uint64_t>(s) * side * side)), x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
       }
-      const uint64_t at = static_cast<uint64_t>(i0 + q) * p.out_pitch + 2 * (j0 + c);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[slice][e][own] = v[e];
+    __syncthreads();
+    if (on && slice == 0) {
+#pragma unroll
+      for (uint32_t s = 1; s < kSlices; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += sums[s][e][own];
+      const uint64_t at = in_panels(i0 + q, j0 + c, p.out_panel);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= p.f_acc;
       if (p.aux) {
-        load_planes8(aux + at, p.out_plane, x);
+        unpack_planes<PLANES>(load_planes<PLANES>(aux + at, p.out_plane), x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(p.f_aux, x[e], v[e]);
       }
-      store_planes8(out + at, p.out_plane, v);
+      store_planes8<PLANES>(out + at, p.out_plane, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sums[q][c + e] = v[e];
+      for (int e = 0; e < 8; ++e) out_rows[q][c + e] = v[e];
     }
     __syncthreads();
-    for (uint32_t g = threadIdx.x; on && ti != tj && g < 64 * 8; g += kThreads) {
-      const uint32_t j = g / 8, c = g % 8 * 8;
-      float v[8];
+    if (on && slice == 0 && ti != tj) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = sums[c + e][j];
-      store_planes8(out + static_cast<uint64_t>(j0 + j) * p.out_pitch + 2 * (i0 + c), p.out_plane, v);
+      for (int e = 0; e < 8; ++e) v[e] = out_rows[e][own];
+      store_planes8<PLANES>(out + in_panels(j0 + own, i0, p.out_panel), p.out_plane, v);
     }
     __syncthreads();
   }
@@ -500,25 +611,55 @@ uint64_t padded(uint64_t x) { return (x + kPad - 1) / kPad * kPad; }
 struct OrthoCut {
   uint32_t side, ti, tj, tiles, splits, split_k;
 };
-OrthoCut ortho_cut(uint64_t rows, uint64_t cols, uint64_t k, uint32_t count, bool sym, bool may_split) {
-  OrthoCut c{};
-  c.side = 64;
-  for (uint32_t side : {256u, 128u}) {
-    const uint64_t ti = (rows + side - 1) / side, tj = (cols + side - 1) / side;
-    if ((sym ? ti * (ti + 1) / 2 : ti * tj) * count >= (side == 256 ? 256u : 200u)) {
-      c.side = side;
-      break;
+// What a block of a side takes, measured (us): beside its steps, and a step of 32, of
+// 1 to per_cu blocks a CU; `lone`, a step of one on the whole chip.  The upper half and
+// the whole of n^3, tiles of 64 / 128 / 192 / 256: n = 1024 8, 11, 18, 29 and 8, 10, 16,
+// 25; 2048 20, 19, 29, 45 and 28, 21, 29, 43; 3000 58, 43, 42, 64 and 88, 65, 51, 65; 4096
+// 154, 90, 68, 88 and 222, 125, 127, 112.
+struct OrthoCost {
+  uint32_t side, per_cu;
+  double lone, base[4], step[4];
+};
+constexpr OrthoCost kOrthoCosts[] = {{64, 4, 0.114, {4.0, 4.5, 4.5, 5.5}, {0.125, 0.15, 0.26, 0.35}},
+                                     {128, 2, 0.144, {6.0, 9.6}, {0.21, 0.43}},
+                                     {192, 1, 0.25, {9.0}, {0.46}},
+                                     {256, 1, 0.44, {13.0}, {0.76}}};
+double ortho_us(const OrthoCost& c, uint64_t blocks, uint32_t steps) {
+  const uint64_t rounds = blocks / (256 * c.per_cu), rest = blocks % (256 * c.per_cu);
+  double us = rounds * (c.base[c.per_cu - 1] + steps * c.step[c.per_cu - 1]);
+  if (rest) {
+    const uint32_t b = static_cast<uint32_t>((rest + 255) / 256) - 1;
+    const double step = b == 0 ? c.lone + (c.step[0] - c.lone) * (rest / 256.0) : c.step[b];
+    us += (c.base[b] + steps * step) * (rounds && c.per_cu == 4 ? 0.6 : 1.0);  // small blocks begin beside the round before
+  }
+  return us;
+}
+// A symmetric product may be split over its sum, whose parts then go through memory
+// (4 TB/s there and back) and a join.
+OrthoCut ortho_cut(uint64_t rows, uint64_t cols, uint64_t k, uint32_t count, bool sym, int planes) {
+  const uint32_t pairs = static_cast<uint32_t>(k / (2 * kStep));  // of steps
+  OrthoCut best{};
+  double best_us = 1e30;
+  for (const OrthoCost& cost : kOrthoCosts) {
+    if (planes == 2 && cost.side == 256) continue;  // its sums leave no registers for a second plane's way
+    OrthoCut c{};
+    c.side = cost.side;
+    c.ti = static_cast<uint32_t>((rows + c.side - 1) / c.side);
+    c.tj = static_cast<uint32_t>((cols + c.side - 1) / c.side);
+    c.tiles = sym ? c.ti * (c.ti + 1) / 2 : c.ti * c.tj;
+    const uint64_t tiles = static_cast<uint64_t>(c.tiles) * count;
+    for (uint32_t splits = 1; splits == 1 || (sym && splits <= pairs && tiles * splits <= 256 * cost.per_cu); splits += 1 + splits / 16) {
+      c.split_k = (pairs + splits - 1) / splits * 2;
+      c.splits = (2 * pairs + c.split_k - 1) / c.split_k;
+      const double us = ortho_us(cost, tiles * c.splits, c.split_k * (planes == 2 ? 3 : 1)) +
+                        (c.splits > 1 ? 4.5 + tiles * c.splits * c.side * c.side * 8 / 4e6 : 0.0);
+      if (us < best_us) {
+        best_us = us;
+        best = c;
+      }
     }
   }
-  c.ti = static_cast<uint32_t>((rows + c.side - 1) / c.side);
-  c.tj = static_cast<uint32_t>((cols + c.side - 1) / c.side);
-  c.tiles = sym ? c.ti * (c.ti + 1) / 2 : c.ti * c.tj;
-  const uint32_t steps = static_cast<uint32_t>(k / kStep);
-  uint32_t splits = 1;
-  if (may_split && c.tiles * count < 256) splits = std::min(256 / (c.tiles * count), std::max(1u, steps / 4));
-  c.split_k = (steps + splits - 1) / splits;
-  c.splits = (steps + c.split_k - 1) / c.split_k;
-  return c;
+  return best;
 }
 uint64_t ortho_part_bytes(const OrthoCut& c, uint32_t count) {
   return c.splits > 1 ? static_cast<uint64_t>(c.tiles) * count * c.splits * c.side * c.side * 4 : 0;
@@ -544,9 +685,9 @@ OrthoPlan ortho_plan(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype
   // as many as keep the chip at work: a round of 256 tiles, four times
   const uint64_t tiles = ((p.m + 255) / 256) * ((p.m + 255) / 256);
   p.group = static_cast<uint32_t>(std::min<uint64_t>(count, std::max<uint64_t>(1, 1024 / tiles)));
-  p.gram = ortho_cut(p.m, p.m, p.n, p.group, true, true);
-  p.poly = ortho_cut(p.m, p.m, p.m, p.group, true, true);
-  p.mid = ortho_cut(p.m, p.n, p.m, p.group, false, false);
+  p.gram = ortho_cut(p.m, p.m, p.n, p.group, true, p.planes);
+  p.poly = ortho_cut(p.m, p.m, p.m, p.group, true, p.planes);
+  p.mid = ortho_cut(p.m, p.n, p.m, p.group, false, p.planes);
   p.sums = 0;
   p.x0 = kOrthoMost * kNormBlocks * 8;
   p.x1 = p.x0 + p.group * p.x_bytes;
@@ -599,7 +740,9 @@ constexpr double kSlack = 1.02;  // what roundings may add to a bound
 template <int MODE, int PLANES>
 hipError_t product_of(const OrthoProduct& p, const OrthoOut& o, uint32_t side, hipStream_t st) {
   const uint32_t grid = grid_for(static_cast<uint64_t>(p.count) * p.tiles * p.splits, kThreads);
-  if (side == 256) return launch_op(ortho_product_kernel<MODE, 256, PLANES>, grid, kThreads, st, p, o);
+  if constexpr (PLANES == 1)
+    if (side == 256) return launch_op(ortho_product_kernel<MODE, 256, PLANES>, grid, kThreads, st, p, o);
+  if (side == 192) return launch_op(ortho_product_kernel<MODE, 192, PLANES>, grid, kThreads, st, p, o);
   if (side == 128) return launch_op(ortho_product_kernel<MODE, 128, PLANES>, grid, kThreads, st, p, o);
   return launch_op(ortho_product_kernel<MODE, 64, PLANES>, grid, kThreads, st, p, o);
 }
@@ -607,8 +750,13 @@ template <int MODE>
 hipError_t product(const OrthoProduct& p, const OrthoOut& o, uint32_t side, hipStream_t st) {
   const hipError_t e = p.left_plane ? product_of<MODE, 2>(p, o, side, st) : product_of<MODE, 1>(p, o, side, st);
   if (e != hipSuccess || p.splits == 1) return e;
-  const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * (side / 64) * (side / 64);
-  return launch_op(ortho_join_kernel, grid_for(items, kThreads), kThreads, st, p, side);
+  const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * (side / kPanel) * (side / kJoinRows);
+  return launch_op(p.left_plane ? ortho_join_kernel<2> : ortho_join_kernel<1>, grid_for(items, kThreads), kThreads, st, p, side);
+}
+
+template <int DT, int PLANES>
+hipError_t load_x(const OrthoIn& in, const OrthoX& x, bool tall, dim3 grid, const double* sums, uint32_t n_sums, hipStream_t st) {
+  return launch_op(tall ? ortho_load_kernel<DT, true, PLANES> : ortho_load_kernel<DT, false, PLANES>, grid, kThreads, st, in, x, sums, n_sums);
 }
 
 void set_cut(OrthoProduct& p, const OrthoCut& c) {
@@ -641,7 +789,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
   const uint64_t ws = reinterpret_cast<uint64_t>(a.ws);
   double* const sums = reinterpret_cast<double*>(ws + plan.sums);
   float* const part = reinterpret_cast<float*>(ws + plan.part);
-  const uint32_t x_pitch = static_cast<uint32_t>(plan.n * 2), a_pitch = static_cast<uint32_t>(plan.m * 2);
+  const uint32_t panel = static_cast<uint32_t>(plan.m * (kPanel * 2));  // of X and of A and B: all have m rows
   const uint64_t x_plane = plan.planes == 2 ? plan.m * plan.n * 2 : 0, a_plane = plan.planes == 2 ? plan.m * plan.m * 2 : 0;
   for (uint32_t z0 = 0; z0 < a.count; z0 += plan.group) {
     const uint32_t count = std::min(plan.group, a.count - z0);
@@ -661,7 +809,6 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
     in.nesterov = a.nesterov;
     out.m = static_cast<uint32_t>(std::min(a.rows, a.cols));
     out.n = static_cast<uint32_t>(std::max(a.rows, a.cols));
-    out.dtype = a.out_dtype;
     out.tall = plan.tall;
     const uint64_t groups = a.rows * ((a.cols + 7) / 8);
     uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>(kNormBlocks, (groups + kThreads - 1) / kThreads));
@@ -673,8 +820,8 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
     uint64_t x = ws + plan.x0, other = ws + plan.x1;
     const OrthoX ox{x, x_plane, plan.x_bytes, static_cast<uint32_t>(plan.m), static_cast<uint32_t>(plan.n), a.eps, std::ldexp(1.0, ex)};
     const dim3 load_grid(grid_for((plan.m / 64) * (plan.n / 64), kThreads), count);
-    if (a.dtype == kBf16) e = launch_op(plan.tall ? ortho_load_kernel<kBf16, true> : ortho_load_kernel<kBf16, false>, load_grid, kThreads, st, in, ox, sums, blocks);
-    else e = launch_op(plan.tall ? ortho_load_kernel<kF32, true> : ortho_load_kernel<kF32, false>, load_grid, kThreads, st, in, ox, sums, blocks);
+    if (a.dtype == kBf16) e = plan.planes == 2 ? load_x<kBf16, 2>(in, ox, plan.tall, load_grid, sums, blocks, st) : load_x<kBf16, 1>(in, ox, plan.tall, load_grid, sums, blocks, st);
+    else e = plan.planes == 2 ? load_x<kF32, 2>(in, ox, plan.tall, load_grid, sums, blocks, st) : load_x<kF32, 1>(in, ox, plan.tall, load_grid, sums, blocks, st);
     if (e != hipSuccess) return e;
     for (uint32_t s = 0; s < a.steps; ++s) {
       const double* const k = a.coefs + 3 * s;
@@ -684,11 +831,10 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
       p.left = p.right = x;
       p.left_plane = p.right_plane = x_plane;
       p.left_next = p.right_next = plan.x_bytes;
-      p.left_pitch = p.right_pitch = x_pitch;
+      p.left_panel = p.right_panel = p.out_panel = panel;
       p.out = ws + plan.a;
       p.out_plane = a_plane;
       p.out_next = plan.a_bytes;
-      p.out_pitch = a_pitch;
       p.rows = p.cols = static_cast<uint32_t>(plan.m);
       p.k = static_cast<uint32_t>(plan.n);
       p.count = count;
@@ -704,7 +850,6 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
         p.left = p.right = p.aux = ws + plan.a;
         p.left_plane = p.right_plane = a_plane;
         p.left_next = p.right_next = plan.a_bytes;
-        p.left_pitch = p.right_pitch = a_pitch;
         p.out = ws + plan.b;
         p.k = static_cast<uint32_t>(plan.m);
         p.f_acc = static_cast<float>(std::ldexp(k[2], eb - 2 * ea));
@@ -722,15 +867,12 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
       p.left = left;  // X <- a X + B X
       p.left_plane = a_plane;
       p.left_next = plan.a_bytes;
-      p.left_pitch = a_pitch;
       p.right = p.aux = x;
       p.right_plane = x_plane;
       p.right_next = plan.x_bytes;
-      p.right_pitch = x_pitch;
       p.out = other;
       p.out_plane = x_plane;
       p.out_next = plan.x_bytes;
-      p.out_pitch = x_pitch;
       p.cols = static_cast<uint32_t>(plan.n);
       p.k = static_cast<uint32_t>(plan.m);
       p.f_acc = static_cast<float>(std::ldexp(by * scale, eo - el - ex));
