@@ -301,7 +301,8 @@ hipError_t launch_adamw(const DeviceTables& t, const InlineGrads& grads, int gra
                         const AdamScalars& sc, hipStream_t st);
 hipError_t launch_sgd(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
                       const SgdScalars& sc, hipStream_t st);
+// ortho_share: of the elements, those with an orthogonalised update.
 hipError_t launch_muon(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
-                       const MuonScalars& sc, hipStream_t st);
+                       const MuonScalars& sc, double ortho_share, hipStream_t st);
 
 }  // namespace lc

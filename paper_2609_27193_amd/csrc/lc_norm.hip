@@ -414,12 +414,12 @@ hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t st) {
 
 uint64_t norm_bwd_workspace(uint64_t rows, uint64_t dim) {
   // whether a call is light goes by its kind and types
-  const uint64_t a = norm_parts(rows, dim, true).parts, b = norm_parts(rows, dim, false).parts;
+  const uint64_t a = norm_parts(rows, dim, kNormLight).parts, b = norm_parts(rows, dim, kNormHeavy).parts;
   return (a > b ? a : b) * 2 * dim * 4;
 }
 
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t st) {
-  const NormParts p = norm_parts(a.rows, a.dim, !a.layer && a.dtype == kBf16);
+  const NormParts p = norm_parts(a.rows, a.dim, !a.layer && a.dtype == kBf16 ? kNormLight : kNormHeavy);
   if (a.rows > 0 && (a.part || a.dx.data)) {
     const hipError_t e = a.dtype == kBf16 ? norm_bwd_kind<kBf16>(a, p, st) : norm_bwd_kind<kF32>(a, p, st);
     if (e != hipSuccess) return e;

@@ -100,13 +100,18 @@ constexpr bool norm_has_shape(uint64_t dim) { return dim >= 8 && dim <= kNormLon
   else if (dim <= 8192) F(512, 2); \
   else F(1024, 2)
 
-// As many blocks as are resident at once, for more only add parts (16384 x
-// 4096 layer norm in bf16, 12 waves a CU 69 us, 16 81; RMS norm, which holds no
-// sums of db, 66 and 65).
-__host__ inline NormParts norm_parts(uint64_t rows, uint64_t dim, bool light) {
+// As many blocks as are resident at once, for more only add parts: waves a CU by the
+// groups of eight that a thread has.
+struct NormWaves {
+  uint32_t of1, of2, of3;
+};
+// (16384 x 4096 layer norm in bf16, 12 waves a CU 69 us, 16 81; RMS norm, which holds
+// no sums of db, 66 and 65.)
+constexpr NormWaves kNormLight = {20, 16, 12}, kNormHeavy = {20, 12, 8};
+__host__ inline NormParts norm_parts(uint64_t rows, uint64_t dim, const NormWaves& w) {
   uint32_t tpr = kLongThreads, waves = 16;
   if (norm_has_shape(dim)) {
-#define LC_NORM_SHAPE(TPR, NV) tpr = TPR, waves = NV == 1 ? 20 : NV == 2 ? (light ? 16 : 12) : light ? 12 : 8
+#define LC_NORM_SHAPE(TPR, NV) tpr = TPR, waves = NV == 1 ? w.of1 : NV == 2 ? w.of2 : w.of3
     LC_NORM_SHAPES(LC_NORM_SHAPE);
 #undef LC_NORM_SHAPE
   }
@@ -114,7 +119,7 @@ __host__ inline NormParts norm_parts(uint64_t rows, uint64_t dim, bool light) {
   p.rpb = tpr < 256 ? 256 / tpr : 1;
   const uint32_t block_waves = tpr < 256 ? 4 : tpr / 64;
   const uint64_t items = (rows + p.rpb - 1) / p.rpb;
-  const auto blocks_of = [&](uint32_t w) -> uint64_t { return 256 * (w > block_waves ? w / block_waves : 1); };
+  const auto blocks_of = [&](uint32_t n) -> uint64_t { return 256 * (n > block_waves ? n / block_waves : 1); };
   // up to four rows a block the parts weigh more (1024 x 4096 RMS norm in bf16, 16
   // waves a CU 18.0 us of kernels, 8 14.6)
   const uint64_t most = blocks_of(waves > 8 && items <= 4 * blocks_of(8) ? 8 : waves);

@@ -365,15 +365,22 @@ __global__ __launch_bounds__((kOptThreads<WDT, MASTER>)) void optim_kernel(
 // 335, of 13000 937 / 918; 90% full: 6000 of 26000 776 / 846).
 constexpr uint32_t kOptBytesPerCU = 100 * 1024;
 
+// The mixed step goes by the mean over its elements: of 1.2 B parameters, four in five
+// of them orthogonalised (bf16, master; 62 KB in the mean), us at 1 / 2 / 3 / 4 blocks
+// per CU: 3296 / 3105 / 3221 / 3245.
+template <int OPT, int WDT, int GDT, bool MASTER>
+constexpr uint32_t kOptTile = kChunkBytes / (WDT == 1 ? 2 : 4) *
+                              ((MASTER ? 8 + (WDT == 1 ? 2 : 4) : WDT == 1 ? 4 : 8) + (OPT == kAdamW ? 16 : 0) + (GDT == 1 ? 2 : 4));
+
 template <int OPT, int WDT, int GDT, bool MASTER, typename SC>
-void launch_optim_t(const DeviceTables& t, const InlineGrads& ig, const SC& sc, hipStream_t st) {
+void launch_optim_t(const DeviceTables& t, const InlineGrads& ig, const SC& sc, double ortho_share, hipStream_t st) {
   const uint32_t g = grid_for(t.n_chunks, kOptThreads<WDT, MASTER>);
   constexpr uint32_t CE = kChunkBytes / (WDT == 1 ? 2 : 4);
-  constexpr uint32_t wsz = WDT == 1 ? 2 : 4;
-  constexpr uint32_t tile = CE * ((MASTER ? 8 + wsz : 2 * wsz) + (OPT == kSGD ? 0 : 16) + (GDT == 1 ? 2 : 4));
-  constexpr uint32_t fit = (kOptBytesPerCU + tile / 2) / tile;
-  constexpr uint32_t blocks = LC_OPT_BLOCKS_PER_CU ? LC_OPT_BLOCKS_PER_CU
-                              : tile >= kOptBytesPerCU ? 1 : fit < 2 ? 2 : fit;
+  const uint32_t tile = OPT == kMuon ? static_cast<uint32_t>(ortho_share * kOptTile<kSGD, WDT, GDT, MASTER> +
+                                                             (1.0 - ortho_share) * kOptTile<kAdamW, WDT, GDT, MASTER>)
+                                     : kOptTile<OPT, WDT, GDT, MASTER>;
+  const uint32_t fit = (kOptBytesPerCU + tile / 2) / tile;
+  const uint32_t blocks = LC_OPT_BLOCKS_PER_CU ? LC_OPT_BLOCKS_PER_CU : tile >= kOptBytesPerCU ? 1 : fit < 2 ? 2 : fit;
   const bool full = t.total_numel * 8 >= static_cast<uint64_t>(t.n_chunks) * CE * 7;
   const uint32_t lds = full ? occupancy_lds(blocks) : 0;
   if (g == t.n_chunks)
@@ -386,14 +393,14 @@ void launch_optim_t(const DeviceTables& t, const InlineGrads& ig, const SC& sc, 
 
 template <int OPT, typename SC>
 void launch_optim(const DeviceTables& t, const InlineGrads& ig, int grad_dtype, int has_master, const SC& sc,
-                  hipStream_t st) {
+                  hipStream_t st, double ortho_share = 0.0) {
   const bool gb = grad_dtype == 1;
   if (t.dtype == 1) {
-    if (has_master) { if (gb) launch_optim_t<OPT, 1, 1, true>(t, ig, sc, st); else launch_optim_t<OPT, 1, 2, true>(t, ig, sc, st); }
-    else { if (gb) launch_optim_t<OPT, 1, 1, false>(t, ig, sc, st); else launch_optim_t<OPT, 1, 2, false>(t, ig, sc, st); }
+    if (has_master) { if (gb) launch_optim_t<OPT, 1, 1, true>(t, ig, sc, ortho_share, st); else launch_optim_t<OPT, 1, 2, true>(t, ig, sc, ortho_share, st); }
+    else { if (gb) launch_optim_t<OPT, 1, 1, false>(t, ig, sc, ortho_share, st); else launch_optim_t<OPT, 1, 2, false>(t, ig, sc, ortho_share, st); }
   } else {
-    if (has_master) { if (gb) launch_optim_t<OPT, 2, 1, true>(t, ig, sc, st); else launch_optim_t<OPT, 2, 2, true>(t, ig, sc, st); }
-    else { if (gb) launch_optim_t<OPT, 2, 1, false>(t, ig, sc, st); else launch_optim_t<OPT, 2, 2, false>(t, ig, sc, st); }
+    if (has_master) { if (gb) launch_optim_t<OPT, 2, 1, true>(t, ig, sc, ortho_share, st); else launch_optim_t<OPT, 2, 2, true>(t, ig, sc, ortho_share, st); }
+    else { if (gb) launch_optim_t<OPT, 2, 1, false>(t, ig, sc, ortho_share, st); else launch_optim_t<OPT, 2, 2, false>(t, ig, sc, ortho_share, st); }
   }
 }
 
@@ -406,8 +413,8 @@ hipError_t launch_adamw(const DeviceTables& t, const InlineGrads& grads, int gra
 }
 
 hipError_t launch_muon(const DeviceTables& t, const InlineGrads& grads, int grad_dtype, int has_master,
-                       const MuonScalars& sc, hipStream_t st) {
-  launch_optim<kMuon>(t, grads, grad_dtype, has_master, sc, st);
+                       const MuonScalars& sc, double ortho_share, hipStream_t st) {
+  launch_optim<kMuon>(t, grads, grad_dtype, has_master, sc, st, ortho_share);
   return hipGetLastError();
 }
 

@@ -420,6 +420,12 @@ hipError_t res_norm_fwd_kind(const ResNormFwd& a, hipStream_t st) {
   return a.layer ? res_norm_fwd_of<DT, RT, true>(a, st) : res_norm_fwd_of<DT, RT, false>(a, st);
 }
 
+// Waves a CU, by the groups of eight that a thread has: three or four streams in and
+// one or two out are enough of two blocks (us at 8 / 12 / 16 waves: 16384 x 4096 in
+// bf16 91 / 94 / 95, 8192 x 5120 with an fp32 stream from kept rows 101 / 115).  The
+// next row's loads in registers meanwhile: 92 and 103.
+constexpr NormWaves kResWaves = {16, 8, 8};  // fewer than the workspace reckons with
+
 template <int DT, int RT, bool LAYER, bool KEPT>
 hipError_t res_norm_bwd_of(const ResNormBwd& a, const NormParts& p, hipStream_t st) {
   const uint32_t dim = a.dim;
@@ -446,7 +452,7 @@ hipError_t launch_res_norm_fwd(const ResNormFwd& a, hipStream_t st) {
 }
 
 hipError_t launch_res_norm_bwd(const ResNormBwd& a, hipStream_t st) {
-  const NormParts p = norm_parts(a.rows, a.dim, !a.layer && a.dtype == kBf16);
+  const NormParts p = norm_parts(a.rows, a.dim, kResWaves);
   if (a.rows > 0 && (a.part || a.dx.data || a.dres.data)) {
     const hipError_t e = a.dtype == kF32         ? res_norm_bwd_kind<kF32, kF32>(a, p, st)
                          : a.res_dtype == kBf16 ? res_norm_bwd_kind<kBf16, kBf16>(a, p, st)

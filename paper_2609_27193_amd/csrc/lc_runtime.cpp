@@ -1083,7 +1083,13 @@ lc_status lc_muon_step_score(lc_ctx* c, int64_t step, const void* const* grads, 
   sc.adamw = adamw_scalars(&p->adamw);
   sc.ortho.lr = static_cast<float>(p->ortho_lr);
   sc.ortho.decay = static_cast<float>(1.0 - p->ortho_lr * p->ortho_weight_decay);
-  LC_HIP(c, launch_muon(c->dt, c->inline_grads, grad_dtype, c->L.has_master ? 1 : 0, sc, c->stream));
+  double ortho = 0.0, all = 0.0;
+  for (size_t i = 0; i < c->L.opt_segs.size(); ++i) {
+    const double n = static_cast<double>(c->L.opt_segs[i].numel);
+    all += n;
+    ortho += ortho_mask[i] ? n : 0.0;
+  }
+  LC_HIP(c, launch_muon(c->dt, c->inline_grads, grad_dtype, c->L.has_master ? 1 : 0, sc, ortho / all, c->stream));
   return optimizer_end(c, step);
 }
 
