@@ -462,10 +462,11 @@ lc_status lc_destroy(lc_ctx *c);
 
 /* ---- Training operators -----------------------------------------------------
  * What a training step computes around the weights of a layout: the embedding
- * and its gradient, layer norm and RMS norm with their gradients, activations
- * kept in 8 bits, and a linear layer's weight gradient from them.  Their
- * gradients are what lc_adamw_step_score and lc_sgd_step_score take, in the
- * same types (LC_DT_BF16, LC_DT_F32).
+ * and its gradient, layer norm and RMS norm with their gradients, also with a
+ * residual's addition before them, activations kept in 8 bits, a linear layer's
+ * weight gradient from them, and the orthogonalised update of a matrix from its
+ * gradient.  Their gradients are what lc_adamw_step_score, lc_sgd_step_score and
+ * lc_muon_step_score take, in the same types (LC_DT_BF16, LC_DT_F32).
  *
  * These calls need no context.  Every array is device memory of the caller's;
  * a call writes the arrays that it returns and the workspace it is given, and
@@ -640,10 +641,12 @@ typedef struct {
  * with more rows than columns, X^T in X's place.  Without momenta (NULL) u = g.  The
  * gradients are of one dtype, the momenta fp32 (the exp_avg of their segments, so
  * that records hold them; strides as in memory), the results of one dtype: with
- * LC_DT_BF16 the steps hold X, A and their products' operands to 11 bits, about what
- * a gradient in bf16 holds of itself, with LC_DT_F32 to 22 bits, in three times the
- * products.  Errors are relative to the largest singular value, and the steps raise
- * the small ones by up to `a` each.  Coefficients that let a singular value grow
+ * LC_DT_BF16 and sides of 384 and more the steps hold X, A and their products'
+ * operands to 11 bits, about what a gradient in bf16 holds of itself, otherwise to 22
+ * bits, in three times the products.  Errors are relative to the largest singular
+ * value, and the steps raise the small ones by up to `a` each: with the coefficients
+ * above a result in bf16 is off by 2.0e-3 of its norm, 1.7e-3 of it the rounding of
+ * the result itself, one in fp32 by 1e-6 to 2e-6.  Coefficients that let a singular value grow
  * beyond 2^30 are refused.  A matrix of zeros gives zeros; one that holds an infinity
  * or a NaN gives NaN throughout (its momentum holds them where they were), and the
  * matrices beside it are as ever.  The results are what lc_muon_step_score takes.

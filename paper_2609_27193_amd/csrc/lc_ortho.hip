@@ -10,13 +10,14 @@
 // X, A and B are held in fp16, times a power of two that keeps their largest
 // possible element, which is bounded by the largest singular value that the steps'
 // polynomials allow, at 2^15 or less: 11 bits of every element, where bf16 at the
-// same rate keeps 8.  A result in fp32 takes each as the sum of two such planes, 22
-// bits, and a product as three (the fourth is below the last bit).  An error of one
-// rounding (2^-12 of an element) is spread over all singular directions; the
-// smaller ones, which the steps raise by up to `a` each, carry it along: 256 x 1024
-// of normal elements, five steps of 3.4445, -4.775, 2.0315: 1.4e-3 of the result's
-// norm, a bf16 result's rounding itself 1.7e-3; bf16 throughout 1.2e-2; two planes
-// 2.6e-7, fp32 throughout 1.7e-7.  Sums, norms and the momentum are fp32 or wider.
+// same rate keeps 8.  A result in fp32, and any of few rows (kOnePlane), takes each as
+// the sum of two such planes, 22 bits, and a product as three (the fourth is below
+// the last bit).  An error of one rounding (2^-12 of an element) is spread over all
+// singular directions; the smaller ones, which the steps raise by up to `a` each,
+// carry it along: 256 x 1024 of normal elements, five steps of 3.4445, -4.775, 2.0315:
+// 1.4e-3 of the result's norm, a bf16 result's rounding itself 1.7e-3; bf16
+// throughout 1.2e-2; two planes 2.6e-7, fp32 throughout 1.7e-7.  Sums, norms and the
+// momentum are fp32 or wider.
 //
 // Inside, sides are padded to multiples of 64 with zeros, which stay zeros, and a
 // plane lies in panels of 32 columns: a row's 64 bytes of a panel, the next row's
@@ -47,7 +48,7 @@ constexpr uint32_t kThreads = 256;  // four waves
 constexpr uint32_t kPad = 64;       // of both sides
 constexpr uint32_t kStep = 32;      // of the sum, in LDS at a time
 constexpr uint32_t kPanel = 32;     // columns
-constexpr uint32_t kNormBlocks = 256;  // of one matrix, at most
+constexpr uint32_t kNormBlocks = 1024;  // of one matrix, at most: every block of the next kernel adds their sums
 
 // ---- the update and its norm -----------------------------------------------------------
 // Matrix z of the group: where its gradient and momentum are.
@@ -85,15 +86,17 @@ __device__ __forceinline__ double block_sum(double v, double (&red)[kThreads / 6
 }
 
 // The new momentum, and the squares of u summed in 64 bits: a gradient's elements
-// may be as small as their squares are no fp32 numbers.
+// may be as small as their squares are no fp32 numbers.  Bound by memory: 4096 x 4096
+// of bf16 and its momentum 33 us at 1024 blocks, 5.1 TB/s, 41 at 512 and 63 at 256;
+// twice 4096 x 14336 222, 209 and 232.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void ortho_norm_kernel(OrthoIn a, double* sums) {
   __shared__ double red[kThreads / 64];
   const uint32_t z = blockIdx.y, groups = (a.cols + 7) / 8;
-  const uint64_t items = static_cast<uint64_t>(a.rows) * groups;
+  const uint32_t items = a.rows * groups;  // 2^29 at most
   double s = 0;
-  for (uint64_t i = blockIdx.x * kThreads + threadIdx.x; i < items; i += gridDim.x * kThreads) {
-    const uint32_t row = static_cast<uint32_t>(i / groups), c = static_cast<uint32_t>(i % groups) * 8;
+  for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < items; i += gridDim.x * kThreads) {
+    const uint32_t row = i / groups, c = i % groups * 8;
     const int n = static_cast<int>(a.cols - c);
     float u[8], b[8];
     update8<DT, true>(a, z, row, c, n, u, b);
@@ -231,7 +234,7 @@ struct OrthoProduct {
 struct OrthoOut {
   uint64_t data[kOrthoMost], stride[kOrthoMost];
   uint32_t m, n;  // of X, without its padding
-  int tall;
+  int tall, dtype;
 };
 
 __device__ __forceinline__ void ortho_place(const OrthoProduct& p, bool sym, uint32_t t, uint32_t& i, uint32_t& j) {
@@ -272,9 +275,12 @@ __device__ __forceinline__ void load_lds(tile_t t, uint8_t* to, uint32_t off) {
 }
 
 // Eight neighbours of row i of D from column j on, in the result's type.
-template <int DT>
+template <int PLANES>
 __device__ __forceinline__ void ortho_out8(const OrthoOut& o, uint32_t z, uint64_t row, uint32_t col, int n, const float (&v)[8]) {
-  if (n > 0) store8<DT>(o.data[z] + (row * o.stride[z] + col) * kEsz<DT>, v, n);
+  if (n <= 0) return;
+  const uint64_t at = row * o.stride[z] + col;
+  if (PLANES == 1 || o.dtype == kBf16) store8<kBf16>(o.data[z] + at * 2, v, n);
+  else store8<kF32>(o.data[z] + at * 4, v, n);
 }
 
 constexpr int kSym = 0, kMid = 1, kLast = 2;
@@ -517,7 +523,6 @@ __global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kern
       }
       if (!turned) continue;
       // the caller's rows, or the other side of the diagonal: four lanes take 32 neighbours of a column of these rows
-      constexpr int kOutType = PLANES == 1 ? kBf16 : kF32;
 #pragma unroll 2
       for (uint32_t r = 0; r < kRounds; ++r) {
         constexpr uint32_t kGroups = T / 16;  // of eight columns in a wave's row
@@ -527,14 +532,14 @@ __global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kern
           const uint32_t q = g / kGroups, c = g % kGroups * 8, row = row0 + 32 * f + q, col = col0 + c;
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + c + e];
-          if (row < o.m) ortho_out8<kOutType>(o, z, row, col, static_cast<int>(o.n) - static_cast<int>(col), v);
+          if (row < o.m) ortho_out8<PLANES>(o, z, row, col, static_cast<int>(o.n) - static_cast<int>(col), v);
           continue;
         }
         const uint32_t j = g / 4, c = g % 4 * 8, row = col0 + j, col = row0 + 32 * f + c;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = mine[(c + e) * kOut + j];
         if (MODE == kLast) {
-          if (row < o.n) ortho_out8<kOutType>(o, z, row, col, static_cast<int>(o.m) - static_cast<int>(col), v);
+          if (row < o.n) ortho_out8<PLANES>(o, z, row, col, static_cast<int>(o.m) - static_cast<int>(col), v);
         } else if (row < p.cols && col < p.rows) {
           store_planes8<PLANES>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
         }
@@ -665,6 +670,13 @@ uint64_t ortho_part_bytes(const OrthoCut& c, uint32_t count) {
   return c.splits > 1 ? static_cast<uint64_t>(c.tiles) * count * c.splits * c.side * c.side * 4 : 0;
 }
 
+// A bf16 result of a shorter side of this and more comes from one plane.  Below, where
+// fewer singular directions share a rounding, one plane shows beside the result's
+// own rounding (1.7e-3): 16 x 16 2.1 to 4.1e-3, 128 x 1024 2.4e-3, 256 x 1024 2.1e-3; from
+// 384 to 4096 1.9 to 2.0e-3.  Two take 127 us for 88 (256 x 1024), 109 for 75 (four of
+// 256 x 256), 812 for 390 (four of 383 x 16000).
+constexpr uint64_t kOnePlane = 384;
+
 // Matrices at once and their place in the workspace.
 struct OrthoPlan {
   uint64_t m, n;  // padded
@@ -679,7 +691,7 @@ OrthoPlan ortho_plan(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype
   p.tall = rows > cols;
   p.m = padded(p.tall ? cols : rows);
   p.n = padded(p.tall ? rows : cols);
-  p.planes = out_dtype == kF32 ? 2 : 1;
+  p.planes = out_dtype == kF32 || std::min(rows, cols) < kOnePlane ? 2 : 1;
   p.x_bytes = p.m * p.n * 2 * p.planes;
   p.a_bytes = p.m * p.m * 2 * p.planes;
   // as many as keep the chip at work: a round of 256 tiles, four times
@@ -810,6 +822,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
     out.m = static_cast<uint32_t>(std::min(a.rows, a.cols));
     out.n = static_cast<uint32_t>(std::max(a.rows, a.cols));
     out.tall = plan.tall;
+    out.dtype = a.out_dtype;
     const uint64_t groups = a.rows * ((a.cols + 7) / 8);
     uint32_t blocks = static_cast<uint32_t>(std::min<uint64_t>(kNormBlocks, (groups + kThreads - 1) / kThreads));
     if (LC_MAX_GRID_BLOCKS > 0 && blocks > LC_MAX_GRID_BLOCKS) blocks = LC_MAX_GRID_BLOCKS;

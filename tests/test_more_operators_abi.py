@@ -162,7 +162,8 @@ def test_ortho_shapes_and_types():
 def test_ortho_workspace():
     need = LC.lc_orthogonalize_workspace(2, 4, 8, B)
     assert need > 0 and need % 16 == 0
-    assert LC.lc_orthogonalize_workspace(2, 4, 8, F) > need
+    assert LC.lc_orthogonalize_workspace(2, 4, 8, F) == need  # few rows: two planes for either result
+    assert LC.lc_orthogonalize_workspace(2, 400, 800, F) > LC.lc_orthogonalize_workspace(2, 400, 800, B)
     for bad in [(0, 4, 8, B), (65, 4, 8, B), (2, 0, 8, B), (2, 4, 0, B), (2, 65537, 8, B), (2, 4, 65537, B), (2, 4, 8, 3)]:
         assert LC.lc_orthogonalize_workspace(*bad) == 0
     assert LC.lc_orthogonalize_workspace(3, 700, 90, F) == LC.lc_orthogonalize_workspace(3, 90, 700, F)

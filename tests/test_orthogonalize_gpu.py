@@ -45,7 +45,8 @@ def formula(u, steps, coefs, eps=0.0, scale=1.0):
     return (x.t() if tall else x) * scale
 
 
-SHAPES = [(1, 1), (1, 7), (9, 1), (3, 5), (63, 65), (64, 64), (65, 200), (130, 129), (200, 1000), (1000, 96), (257, 513), (700, 650)]
+SHAPES = [(1, 1), (1, 7), (9, 1), (3, 5), (63, 65), (64, 64), (65, 200), (130, 129), (200, 1000), (1000, 96), (257, 513), (700, 650),
+          (384, 385), (383, 4000), (1029, 390)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
@@ -123,7 +124,8 @@ def test_whole_numbers_come_out_exactly(rows, cols, log4, n, coefs, pad, off):
 
 
 @pytest.mark.parametrize("rows,cols,log4,n", [(64, 256, 5, 3), (700, 90, 5, 2), (300, 300, 5, 2), (1300, 1200, 6, 1), (40, 9000, 6, 2),
-                                              (4100, 4096, 6, 5)])
+                                              (4100, 4096, 6, 5), (384, 9000, 6, 2), (450, 385, 5, 3), (1100, 500, 6, 1), (390, 390, 5, 9),
+                                              (600, 2100, 6, 2)])
 def test_whole_numbers_in_one_plane(rows, cols, log4, n):
     """Thin matrices, whose A, and mostly A A, stays below 2^11: a bf16 result is then the exact one, rounded once."""
     grads = [whole(rows, cols, log4, 50 + s, "bf16") for s in range(n)]
@@ -143,7 +145,8 @@ def test_whole_numbers_in_one_plane(rows, cols, log4, n):
             assert torch.equal(o.view, want.float().to(torch.bfloat16))  # a sum of whole numbers below 2^24: exact in fp32
 
 
-@pytest.mark.parametrize("rows,cols", [(3, 5), (64, 64), (65, 300), (400, 129), (520, 520), (96, 5000)])
+@pytest.mark.parametrize("rows,cols", [(3, 5), (64, 64), (65, 300), (400, 129), (520, 520), (96, 5000), (385, 391), (1000, 390),
+                                       (390, 1003)])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("coefs", [STEEP, CUBIC])
 def test_one_step_an_element_at_a_time(rows, cols, out, coefs):
@@ -195,7 +198,7 @@ def steps_bound(x, steps, coefs, h):
     return err, x
 
 
-@pytest.mark.parametrize("rows,cols", [(40, 40), (200, 700), (640, 130), (512, 512)])
+@pytest.mark.parametrize("rows,cols", [(40, 40), (200, 700), (640, 130), (512, 512), (450, 700), (3000, 400)])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("coefs", [STEEP, CUBIC])
 def test_five_steps(rows, cols, out, coefs):
@@ -287,7 +290,7 @@ def test_sixty_four_matrices():
         assert torch.equal(o.view.double(), (x + x @ (x.t().contiguous() @ x) / 256) / 16)
 
 
-def optimizer(seed, rows=200, cols=330, n=3):
+def optimizer(seed, rows=430, cols=390, n=3):
     """A momentum, its orthogonalised update and the step that takes it: (enqueue, results, what they need)."""
     g = gen(seed)
     grads = [torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(n)]
