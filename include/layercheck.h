@@ -627,7 +627,8 @@ typedef struct {
   int32_t nesterov;    /* 0 or 1                                                   */
   double momentum;     /* mu, in [0, 1); not looked at without momenta             */
   double eps;          /* added to the norm, finite and >= 0 (e.g. 1e-7)           */
-  double scale;        /* of the result, finite (e.g. 0.2 sqrt(max(rows, cols)))   */
+  double scale;        /* of the result, 0 or 2^-64 to 2^64 in magnitude
+                          (e.g. 0.2 sqrt(max(rows, cols)))                         */
   const double *coefs; /* host [steps][3]: a, b, c of each step; NULL: 3.4445,
                           -4.7750, 2.0315 for every one                            */
 } lc_orthogonalize_params;
@@ -644,14 +645,15 @@ typedef struct {
  * LC_DT_BF16 and sides of 384 and more the steps hold X, A and their products'
  * operands to 11 bits, about what a gradient in bf16 holds of itself, otherwise to 22
  * bits, in three times the products.  Errors are relative to the largest singular
- * value, and the steps raise the small ones by up to `a` each: with the coefficients
- * above a result in bf16 is off by 2.0e-3 of its norm, 1.7e-3 of it the rounding of
- * the result itself, one in fp32 by 1e-6 to 2e-6.  Coefficients that let a singular value grow
- * beyond 2^30 are refused.  A matrix of zeros gives zeros; one that holds an infinity
- * or a NaN gives NaN throughout (its momentum holds them where they were), and the
- * matrices beside it are as ever.  The results are what lc_muon_step_score takes.
- * The workspace is that of the matrices which are worked on at once, and goes by the
- * results' dtype. */
+ * value that |X| <= 1 allows (a matrix that eps far outweighs loses bits), and the
+ * steps raise the small ones by up to `a` each: with the coefficients above a result
+ * in bf16 is off by 2.0e-3 of its norm, 1.7e-3 of it the rounding of the result itself,
+ * one in fp32 by 1e-6 to 2e-6.  Coefficients that let the largest singular value grow
+ * beyond 2^30 or fall below 2^-30 are refused.  A matrix of zeros gives zeros; one that
+ * holds an infinity or a NaN gives NaN throughout (its momentum holds them where they
+ * were), and the matrices beside it are as ever.  The results are what
+ * lc_muon_step_score takes.  The workspace is that of the matrices which are worked
+ * on at once, and goes by the results' dtype. */
 uint64_t lc_orthogonalize_workspace(uint32_t n_matrices, uint64_t rows, uint64_t cols, int32_t out_dtype);
 lc_status lc_orthogonalize(const lc_orthogonalize_params *params, uint32_t n_matrices, const lc_matrix *grads,
                            const lc_matrix *momenta, const lc_matrix *out, void *workspace, uint64_t workspace_bytes,

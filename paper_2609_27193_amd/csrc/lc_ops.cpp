@@ -584,12 +584,14 @@ lc_status check_ortho(const lc_orthogonalize_params* p, double (&coefs)[3 * kOrt
   LC_CHECK(check_flag("nesterov", p->nesterov));
   if (!(p->momentum >= 0.0 && p->momentum < 1.0)) return fail(LC_ERR_INVALID_ARG, "momentum must lie in [0, 1)");
   if (!(p->eps >= 0.0) || !std::isfinite(p->eps)) return fail(LC_ERR_INVALID_ARG, "eps must be finite and >= 0");
-  if (!std::isfinite(static_cast<float>(p->scale))) return fail(LC_ERR_INVALID_ARG, "scale must be finite");
+  const double size = std::fabs(p->scale);  // with the steps' powers of two a factor of it is a normal fp32 number
+  if (!(size == 0 || (size >= 0x1p-64 && size <= 0x1p64)))
+    return fail(LC_ERR_INVALID_ARG, "scale must be zero or between 2^-64 and 2^64");
   for (uint32_t i = 0; i < 3 * p->steps; ++i) {
     coefs[i] = p->coefs ? p->coefs[i] : kOrthoDefault[i % 3];
     if (!std::isfinite(coefs[i])) return fail(LC_ERR_INVALID_ARG, "coefs must be finite");
   }
-  if (!ortho_in_range(p->steps, coefs)) return fail(LC_ERR_INVALID_ARG, "coefs make a singular value larger than 2^30");
+  if (!ortho_in_range(p->steps, coefs)) return fail(LC_ERR_INVALID_ARG, "coefs make the largest singular value exceed 2^30 or fall below 2^-30");
   return LC_OK;
 }
 

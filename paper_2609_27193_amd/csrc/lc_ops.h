@@ -122,7 +122,7 @@ hipError_t launch_wgrad(const Wgrad& a, hipStream_t st);
 // Momentum and Newton-Schulz steps of matrices of one shape.
 constexpr uint32_t kOrthoMost = 64;             // matrices a call
 constexpr uint64_t kOrthoLongest = 1 << 16;     // of a side
-constexpr double kOrthoLargest = 1.0 * (1 << 30);  // that the steps may make a singular value
+constexpr double kOrthoLargest = 1.0 * (1 << 30);  // that the steps may make the largest singular value; its inverse the least
 struct Ortho {
   const Rows* grads;
   const Rows* momenta;  // null: none

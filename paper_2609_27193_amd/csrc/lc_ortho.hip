@@ -787,6 +787,7 @@ bool ortho_in_range(uint32_t steps, const double* coefs) {
     const double* const k = coefs + 3 * s;
     const double q = x * x * kSlack;
     x = ortho_bound(x, k) * kSlack;
+    if (x != 0 && x < 1.0 / kOrthoLargest) return false;
     if (!(x < kOrthoLargest) || !(ortho_bound_b(q, k[1], k[2]) < kOrthoLargest) || !(q < kOrthoLargest)) return false;
   }
   return true;

@@ -130,8 +130,9 @@ def test_ortho_params():
     P = LC.orthogonalize_params
     for bad, says in [(P(0, None), "steps"), (P(33, None), "steps"), (P(5, momentum=1.0), "momentum"), (P(5, momentum=-0.1), "momentum"),
                       (P(5, momentum=math.nan), "momentum"), (P(5, eps=-1.0), "eps"), (P(5, eps=math.inf), "eps"),
-                      (P(5, scale=math.nan), "scale"), (P(5, scale=1e39), "scale"), (P(5, (1, math.nan, 0)), "coefs"),
-                      (P(5, (1, math.inf, 0)), "coefs"), (P(5, (40.0, 0, 0)), "singular"), (P(3, [(1, 0, 0), (1, 0, 0), (1, 2e9, 0)]), "singular")]:
+                      (P(5, scale=math.nan), "scale"), (P(5, scale=2.0 ** 65), "scale"), (P(5, scale=-(2.0 ** -65)), "scale"), (P(5, scale=math.inf), "scale"), (P(5, (1, math.nan, 0)), "coefs"),
+                      (P(5, (1, math.inf, 0)), "coefs"), (P(5, (40.0, 0, 0)), "singular"), (P(5, (2.0 ** -7, 0, 0)), "singular"),
+                      (P(3, [(1, 0, 0), (1, 0, 0), (1, 2e9, 0)]), "singular")]:
         refused(ortho, prm=bad, says=says)
     flag = P(5)
     flag.nesterov = 2

@@ -259,6 +259,15 @@ def test_edges(dtype):
     assert not bool(o[0].view.any()) and not bool(o[1].view.any()) and not bool(bufs[1].view.any())  # mu 0: nothing is kept
 
 
+@pytest.mark.parametrize("rows,cols", [(30, 70), (400, 500)])
+def test_scales_at_their_limits(rows, cols):
+    """A power of two more or less leaves every bit of an fp32 result's mantissa; zero gives zeros."""
+    grad = Guarded(rows, cols, torch.float32, value=torch.randn(rows, cols, generator=gen(4), device="cuda"))
+    one = call([grad], "f32")[0].view
+    for scale in (2.0 ** -64, -(2.0 ** 64), 0.0):
+        assert torch.equal(call([grad], "f32", scale=scale)[0].view, one * scale)
+
+
 def test_nothing_to_do():
     prm = LC.orthogonalize_params(5)
     LC.lc_orthogonalize(prm, [], [], 0, 0, stream=stream())
