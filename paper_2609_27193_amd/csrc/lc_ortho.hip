@@ -268,10 +268,12 @@ __device__ __forceinline__ void barrier_lds() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// A lane's 16 bytes to LDS, the wave's 64 after each other.  The whole offset is in
-// the operand that the bounds check covers.
+// A lane's 16 bytes to LDS, the wave's 64 after each other: descriptor, place, bytes,
+// offset, scalar offset and two more.  The whole offset is in the operand that the
+// bounds check covers.
+#define LC_BUFFER_LOAD_LDS __builtin_amdgcn_raw_ptr_buffer_load_lds
 __device__ __forceinline__ void load_lds(tile_t t, uint8_t* to, uint32_t off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(t, (lds_void*)to, 16, off, 0, 0, 0);
+  LC_BUFFER_LOAD_LDS(t, (lds_void*)to, 16, off, 0, 0, 0);
 }
 
 // Eight neighbours of row i of D from column j on, in the result's type.
@@ -293,20 +295,29 @@ constexpr int kSym = 0, kMid = 1, kLast = 2;
 // 16-byte pieces lie at c ^ row / 4 % 4, so that the 16 rows of a quarter read are in
 // different banks; of R as it lies, T / 32 panels of 32 rows of 64 bytes, of which half
 // a transposing read takes four rows, 256 bytes.
-// PLANES: of each operand.
-template <int MODE, int T, int PLANES>
-__global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kernel(OrthoProduct p, OrthoOut o) {
+// PLANES: of each operand.  GROUPS: 3 gives each of two planes' products four waves
+// and LDS of their own, for few tiles, whose steps wait for their loads (five steps in
+// fp32, all of 1024^3 232 us with one group and 190 with three, 512^3 152 and 137, six of
+// 1027 x 509 232 and 208; 1500^3, where the larger tiles fill the chip, 423 and 506).
+template <int MODE, int T, int PLANES, int GROUPS>
+__global__ __launch_bounds__(kThreads * GROUPS, GROUPS > 1 ? GROUPS : T >= 192 ? 1 : 2) void ortho_product_kernel(OrthoProduct p, OrthoOut o) {
+  static_assert(GROUPS == 1 || (GROUPS == 3 && PLANES == 2 && T == 64), "a group's sums lie in its buffers on their way");
   constexpr bool SYM = MODE == kSym;
   constexpr uint32_t NF = T / 64;             // 32-wide pieces of a wave's side
   constexpr uint32_t kOperand = T * kStep * 2;  // bytes
   constexpr uint32_t kLoads = T / 64;         // of an operand, a thread
   constexpr uint32_t kOut = T / 2 + 4;        // floats from row to row on their way out
   static_assert(32 * kOut * 4 <= 2 * kOperand, "a wave's rows on their way out lie in one buffer");
-  __shared__ __align__(1024) uint8_t stage0[2 * kOperand];
-  __shared__ __align__(1024) uint8_t stage1[2 * kOperand];
-  __shared__ __align__(1024) uint8_t stage2[2 * kOperand];
-  __shared__ __align__(1024) uint8_t stage3[2 * kOperand];
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ __align__(1024) uint8_t all0[GROUPS * 2 * kOperand];
+  __shared__ __align__(1024) uint8_t all1[GROUPS * 2 * kOperand];
+  __shared__ __align__(1024) uint8_t all2[GROUPS * 2 * kOperand];
+  __shared__ __align__(1024) uint8_t all3[GROUPS * 2 * kOperand];
+  const uint32_t group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  uint8_t* const stage0 = all0 + group * 2 * kOperand;
+  uint8_t* const stage1 = all1 + group * 2 * kOperand;
+  uint8_t* const stage2 = all2 + group * 2 * kOperand;
+  uint8_t* const stage3 = all3 + group * 2 * kOperand;
+  const uint32_t tid = threadIdx.x % kThreads, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t items = p.count * p.tiles * p.splits;
   for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
     const uint32_t item = items <= gridDim.x ? remap_xcd(b, items) : b;
@@ -423,12 +434,12 @@ __global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kern
     };
     // first the products of a second plane, of either side, then those of the first
 #pragma unroll 1
-    for (uint32_t big = PLANES == 2 ? 0 : 1; big < 2; ++big) {
+    for (uint32_t big = PLANES == 2 && GROUPS == 1 ? 0 : 1; big < 2; ++big) {
       const uint32_t steps = (k_end - k_begin) * (big ? 1 : 2);  // even
       todo = static_cast<int>(steps);
       turn = big ? -1 - todo : todo / 2;  // never, with the first planes
-      left_next = left + (big ? 0 : p.left_plane) + k_begin * left_step;
-      right_next = right + k_begin * right_step;
+      left_next = left + ((GROUPS == 1 ? big : group) == 0 && PLANES == 2 ? p.left_plane : 0) + k_begin * left_step;
+      right_next = right + (GROUPS > 1 && group == 1 ? p.right_plane : 0) + k_begin * right_step;
       for (uint8_t* const stage : {stage0, stage1, stage2}) {
         next();
         load_left(stage);
@@ -464,7 +475,7 @@ __global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kern
     constexpr uint32_t kRounds = T / 32;  // of 16 rows of a panel
     const uint32_t row0 = i0 + wi, col0 = j0 + wj;
     const uint64_t out = p.out + z * p.out_next, aux = p.aux + z * p.out_next;
-    const bool has_aux = p.aux && p.splits == 1;
+    const bool has_aux = p.aux && p.splits == 1 && group == GROUPS - 1;
     Planes8<PLANES> x[2][kRounds];
     auto load_aux = [&](uint32_t f) {
 #pragma unroll
@@ -479,6 +490,26 @@ __global__ __launch_bounds__(kThreads, T >= 192 ? 1 : 2) void ortho_product_kern
       barrier_lds<kRounds * PLANES>();
     } else {
       barrier_lds<0>();
+    }
+    if constexpr (GROUPS > 1) {  // the last group adds the others' sums
+      constexpr uint32_t kTheirs = 2 * kOperand;
+      if (group < GROUPS - 1) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(lds_f32x4*)((q < 2 ? (q == 0 ? stage0 : stage1) : q == 2 ? stage2 : stage3) + tid * 16) =
+              f32x4{acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
+        barrier_lds<0>();
+        __syncthreads();  // with the last group, behind the item
+        continue;
+      }
+      barrier_lds<kRounds * PLANES>();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint8_t* const at = (q < 2 ? (q == 0 ? all0 : all1) : q == 2 ? all2 : all3) + tid * 16;
+        const f32x4 u = *(lds_f32x4*)at, v = *(lds_f32x4*)(at + kTheirs);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[0][0][4 * q + e] = __builtin_fmaf(u[e] + v[e], 1.0f / kRestUp, acc[0][0][4 * q + e]);
+      }
     }
     lds_f32* const mine = (lds_f32*)(wave < 2 ? (wave == 0 ? stage0 : stage1) : wave == 2 ? stage2 : stage3);
     const bool turned = SYM ? ti != tj : MODE == kLast;
@@ -614,21 +645,22 @@ uint64_t padded(uint64_t x) { return (x + kPad - 1) / kPad * kPad; }
 
 // How the products of a shape are cut.
 struct OrthoCut {
-  uint32_t side, ti, tj, tiles, splits, split_k;
+  uint32_t side, groups, ti, tj, tiles, splits, split_k;
 };
 // What a block of a side takes, measured (us): beside its steps, and a step of 32, of
-// 1 to per_cu blocks a CU; `lone`, a step of one on the whole chip.  The upper half and
-// the whole of n^3, tiles of 64 / 128 / 192 / 256: n = 1024 8, 11, 18, 29 and 8, 10, 16,
-// 25; 2048 20, 19, 29, 45 and 28, 21, 29, 43; 3000 58, 43, 42, 64 and 88, 65, 51, 65; 4096
-// 154, 90, 68, 88 and 222, 125, 127, 112.
+// 1 to per_cu blocks a CU; `lone`, a step of one on the whole chip.  A step of three
+// groups is one of each.  The upper half and the whole of n^3, tiles of 64 / 128 / 192 /
+// 256: n = 1024 8, 11, 18, 29 and 8, 10, 16, 25; 2048 20, 19, 29, 45 and 28, 21, 29, 43;
+// 3000 58, 43, 42, 64 and 88, 65, 51, 65; 4096 154, 90, 68, 88 and 222, 125, 127, 112.
 struct OrthoCost {
-  uint32_t side, per_cu;
+  uint32_t side, groups, per_cu;
   double lone, base[4], step[4];
 };
-constexpr OrthoCost kOrthoCosts[] = {{64, 4, 0.114, {4.0, 4.5, 4.5, 5.5}, {0.125, 0.15, 0.26, 0.35}},
-                                     {128, 2, 0.144, {6.0, 9.6}, {0.21, 0.43}},
-                                     {192, 1, 0.25, {9.0}, {0.46}},
-                                     {256, 1, 0.44, {13.0}, {0.76}}};
+constexpr OrthoCost kOrthoCosts[] = {{64, 1, 4, 0.114, {4.0, 4.5, 4.5, 5.5}, {0.125, 0.15, 0.26, 0.35}},
+                                     {64, 3, 1, 0.2, {5.0}, {0.19}},
+                                     {128, 1, 2, 0.144, {6.0, 9.6}, {0.21, 0.43}},
+                                     {192, 1, 1, 0.25, {9.0}, {0.46}},
+                                     {256, 1, 1, 0.44, {13.0}, {0.76}}};
 double ortho_us(const OrthoCost& c, uint64_t blocks, uint32_t steps) {
   const uint64_t rounds = blocks / (256 * c.per_cu), rest = blocks % (256 * c.per_cu);
   double us = rounds * (c.base[c.per_cu - 1] + steps * c.step[c.per_cu - 1]);
@@ -646,9 +678,11 @@ OrthoCut ortho_cut(uint64_t rows, uint64_t cols, uint64_t k, uint32_t count, boo
   OrthoCut best{};
   double best_us = 1e30;
   for (const OrthoCost& cost : kOrthoCosts) {
+    if (planes == 1 && cost.groups > 1) continue;
     if (planes == 2 && cost.side == 256) continue;  // its sums leave no registers for a second plane's way
     OrthoCut c{};
     c.side = cost.side;
+    c.groups = cost.groups;
     c.ti = static_cast<uint32_t>((rows + c.side - 1) / c.side);
     c.tj = static_cast<uint32_t>((cols + c.side - 1) / c.side);
     c.tiles = sym ? c.ti * (c.ti + 1) / 2 : c.ti * c.tj;
@@ -656,7 +690,7 @@ OrthoCut ortho_cut(uint64_t rows, uint64_t cols, uint64_t k, uint32_t count, boo
     for (uint32_t splits = 1; splits == 1 || (sym && splits <= pairs && tiles * splits <= 256 * cost.per_cu); splits += 1 + splits / 16) {
       c.split_k = (pairs + splits - 1) / splits * 2;
       c.splits = (2 * pairs + c.split_k - 1) / c.split_k;
-      const double us = ortho_us(cost, tiles * c.splits, c.split_k * (planes == 2 ? 3 : 1)) +
+      const double us = ortho_us(cost, tiles * c.splits, c.split_k * (planes == 2 && c.groups == 1 ? 3 : 1)) +
                         (c.splits > 1 ? 4.5 + tiles * c.splits * c.side * c.side * 8 / 4e6 : 0.0);
       if (us < best_us) {
         best_us = us;
@@ -749,34 +783,37 @@ double ortho_bound_b(double top, double b, double c) {
 }
 constexpr double kSlack = 1.02;  // what roundings may add to a bound
 
+template <int MODE, int T, int PLANES, int GROUPS = 1>
+hipError_t product_as(const OrthoProduct& p, const OrthoOut& o, hipStream_t st) {
+  const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * p.splits;
+  return launch_op(ortho_product_kernel<MODE, T, PLANES, GROUPS>, grid_for(items, kThreads * GROUPS), kThreads * GROUPS, st, p, o);
+}
 template <int MODE, int PLANES>
-hipError_t product_of(const OrthoProduct& p, const OrthoOut& o, uint32_t side, hipStream_t st) {
-  const uint32_t grid = grid_for(static_cast<uint64_t>(p.count) * p.tiles * p.splits, kThreads);
+hipError_t product_of(const OrthoProduct& p, const OrthoOut& o, const OrthoCut& c, hipStream_t st) {
   if constexpr (PLANES == 1)
-    if (side == 256) return launch_op(ortho_product_kernel<MODE, 256, PLANES>, grid, kThreads, st, p, o);
-  if (side == 192) return launch_op(ortho_product_kernel<MODE, 192, PLANES>, grid, kThreads, st, p, o);
-  if (side == 128) return launch_op(ortho_product_kernel<MODE, 128, PLANES>, grid, kThreads, st, p, o);
-  return launch_op(ortho_product_kernel<MODE, 64, PLANES>, grid, kThreads, st, p, o);
+    if (c.side == 256) return product_as<MODE, 256, PLANES>(p, o, st);
+  if constexpr (PLANES == 2)
+    if (c.groups == 3) return product_as<MODE, 64, PLANES, 3>(p, o, st);
+  if (c.side == 192) return product_as<MODE, 192, PLANES>(p, o, st);
+  if (c.side == 128) return product_as<MODE, 128, PLANES>(p, o, st);
+  return product_as<MODE, 64, PLANES>(p, o, st);
 }
 template <int MODE>
-hipError_t product(const OrthoProduct& p, const OrthoOut& o, uint32_t side, hipStream_t st) {
-  const hipError_t e = p.left_plane ? product_of<MODE, 2>(p, o, side, st) : product_of<MODE, 1>(p, o, side, st);
-  if (e != hipSuccess || p.splits == 1) return e;
-  const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * (side / kPanel) * (side / kJoinRows);
-  return launch_op(p.left_plane ? ortho_join_kernel<2> : ortho_join_kernel<1>, grid_for(items, kThreads), kThreads, st, p, side);
-}
-
-template <int DT, int PLANES>
-hipError_t load_x(const OrthoIn& in, const OrthoX& x, bool tall, dim3 grid, const double* sums, uint32_t n_sums, hipStream_t st) {
-  return launch_op(tall ? ortho_load_kernel<DT, true, PLANES> : ortho_load_kernel<DT, false, PLANES>, grid, kThreads, st, in, x, sums, n_sums);
-}
-
-void set_cut(OrthoProduct& p, const OrthoCut& c) {
+hipError_t product(OrthoProduct& p, const OrthoOut& o, const OrthoCut& c, hipStream_t st) {
   p.ti = c.ti;
   p.tj = c.tj;
   p.tiles = c.tiles;
   p.splits = c.splits;
   p.split_k = c.split_k;
+  const hipError_t e = p.left_plane ? product_of<MODE, 2>(p, o, c, st) : product_of<MODE, 1>(p, o, c, st);
+  if (e != hipSuccess || p.splits == 1) return e;
+  const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * (c.side / kPanel) * (c.side / kJoinRows);
+  return launch_op(p.left_plane ? ortho_join_kernel<2> : ortho_join_kernel<1>, grid_for(items, kThreads), kThreads, st, p, c.side);
+}
+
+template <int DT, int PLANES>
+hipError_t load_x(const OrthoIn& in, const OrthoX& x, bool tall, dim3 grid, const double* sums, uint32_t n_sums, hipStream_t st) {
+  return launch_op(tall ? ortho_load_kernel<DT, true, PLANES> : ortho_load_kernel<DT, false, PLANES>, grid, kThreads, st, in, x, sums, n_sums);
 }
 
 }  // namespace
@@ -854,8 +891,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
       p.count = count;
       p.part = part;
       p.f_acc = static_cast<float>(std::ldexp(1.0, ea - 2 * ex));
-      set_cut(p, plan.gram);
-      if ((e = product<kSym>(p, out, plan.gram.side, st)) != hipSuccess) return e;
+      if ((e = product<kSym>(p, out, plan.gram, st)) != hipSuccess) return e;
       uint64_t left = p.out;
       int el = ea;
       double by = k[1];  // of A X; B = b A needs no product of its own
@@ -868,8 +904,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
         p.k = static_cast<uint32_t>(plan.m);
         p.f_acc = static_cast<float>(std::ldexp(k[2], eb - 2 * ea));
         p.f_aux = static_cast<float>(std::ldexp(k[1], eb - ea));
-        set_cut(p, plan.poly);
-        if ((e = product<kSym>(p, out, plan.poly.side, st)) != hipSuccess) return e;
+        if ((e = product<kSym>(p, out, plan.poly, st)) != hipSuccess) return e;
         left = p.out;
         el = eb;
         by = 1.0;
@@ -891,8 +926,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
       p.k = static_cast<uint32_t>(plan.m);
       p.f_acc = static_cast<float>(std::ldexp(by * scale, eo - el - ex));
       p.f_aux = static_cast<float>(std::ldexp(k[0] * scale, eo - ex));
-      set_cut(p, plan.mid);
-      e = last ? product<kLast>(p, out, plan.mid.side, st) : product<kMid>(p, out, plan.mid.side, st);
+      e = last ? product<kLast>(p, out, plan.mid, st) : product<kMid>(p, out, plan.mid, st);
       if (e != hipSuccess) return e;
       std::swap(x, other);
       ex = eo;

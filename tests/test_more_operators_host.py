@@ -115,6 +115,20 @@ def test_checks_of_arguments_under_host_sanitizers():
     assert "ERROR: AddressSanitizer" not in tail and "runtime error:" not in tail, tail
 
 
+def test_loads_to_lds_have_their_offset_where_bounds_are_checked():
+    """As test_buffer_bounds.py, of the loads whose scalar offset is the fifth argument."""
+    from tests.test_buffer_bounds import CSRC, arguments
+    found = 0
+    for path in sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".h"))):
+        text = open(path).read()
+        assert text.count("buffer_load_lds") == text.count("#define LC_BUFFER_LOAD_LDS __builtin_amdgcn_raw_ptr_buffer_load_lds"), path
+        for at in (i + len("LC_BUFFER_LOAD_LDS(") for i in range(len(text)) if text.startswith("LC_BUFFER_LOAD_LDS(", i)):
+            args = arguments(text, at)
+            assert len(args) == 7 and args[4:6] == ["0", "0"], (os.path.basename(path), args)
+            found += 1
+    assert found == 1
+
+
 def test_workspace_of_any_shape():
     """Holds X twice and A twice in 16 bits, or in two planes of them, both sides padded to 64, for the matrices at once; a matrix needs the same
     turned; more of them never need less, nor two planes less than one."""
