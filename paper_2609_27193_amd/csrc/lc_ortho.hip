@@ -14,8 +14,8 @@
 // the sum of two such planes, 22 bits, and a product as three (the fourth is below
 // the last bit).  An error of one rounding (2^-12 of an element) is spread over all
 // singular directions; the smaller ones, which the steps raise by up to `a` each,
-// carry it along: 256 x 1024 of normal elements, five steps of 3.4445, -4.775, 2.0315:
-// 1.4e-3 of the result's norm, a bf16 result's rounding itself 1.7e-3; bf16
+// carry it along: 256 x 1024 of normal elements, five steps of 3.4445, -4.775, 2.0315, in
+// one plane 1.4e-3 of the result's norm, a bf16 result's rounding itself 1.7e-3; bf16
 // throughout 1.2e-2; two planes 2.6e-7, fp32 throughout 1.7e-7.  Sums, norms and the
 // momentum are fp32 or wider.
 //
