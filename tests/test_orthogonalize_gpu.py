@@ -146,7 +146,7 @@ def test_whole_numbers_in_one_plane(rows, cols, log4, n):
 
 
 @pytest.mark.parametrize("rows,cols", [(3, 5), (64, 64), (65, 300), (400, 129), (520, 520), (96, 5000), (385, 391), (1000, 390),
-                                       (390, 1003)])
+                                       (390, 1003), (1, 65536), (65536, 2), (65, 65535), (65536, 400)])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("coefs", [STEEP, CUBIC])
 def test_one_step_an_element_at_a_time(rows, cols, out, coefs):
