@@ -642,11 +642,10 @@ typedef struct {
  * with more rows than columns, X^T in X's place.  Without momenta (NULL) u = g.  The
  * gradients are of one dtype, the momenta fp32 (the exp_avg of their segments, so
  * that records hold them; strides as in memory), the results of one dtype: with
- * LC_DT_BF16 and sides of 384 and more the steps hold X, A and their products'
- * operands to 11 bits, about what a gradient in bf16 holds of itself, otherwise to 22
- * bits, in three times the products.  Errors are relative to the largest singular
- * value that |X| <= 1 allows (a matrix that eps far outweighs loses bits), and the
- * steps raise the small ones by up to `a` each: with the coefficients above a result
+ * LC_DT_BF16 and sides of 384 and more the steps hold X to 22 bits, A and their
+ * products' operands to 11, otherwise all to 22 bits, in three times the products.
+ * Errors are relative to the largest singular value that |X| <= 1 allows (a matrix
+ * that eps far outweighs loses bits): with the coefficients above a result
  * in bf16 is off by 2.0e-3 of its norm, 1.7e-3 of it the rounding of the result itself,
  * one in fp32 by 1e-6 to 2e-6.  Coefficients that let the largest singular value grow
  * beyond 2^30 or fall below 2^-30 are refused.  A matrix of zeros gives zeros; one that

@@ -10,14 +10,24 @@
 // X, A and B are held in fp16, times a power of two that keeps their largest
 // possible element, which is bounded by the largest singular value that the steps'
 // polynomials allow, at 2^15 or less: 11 bits of every element, where bf16 at the
-// same rate keeps 8.  A result in fp32, and any of few rows (kOnePlane), takes each as
-// the sum of two such planes, 22 bits, and a product as three (the fourth is below
-// the last bit).  An error of one rounding (2^-12 of an element) is spread over all
-// singular directions; the smaller ones, which the steps raise by up to `a` each,
-// carry it along: 256 x 1024 of normal elements, five steps of 3.4445, -4.775, 2.0315, in
-// one plane 1.4e-3 of the result's norm, a bf16 result's rounding itself 1.7e-3; bf16
-// throughout 1.2e-2; two planes 2.6e-7, fp32 throughout 1.7e-7.  Sums, norms and the
-// momentum are fp32 or wider.
+// same rate keeps 8.  X is the sum of two such planes, 22 bits.  A result in fp32, and
+// any of few rows (kOnePlane), takes A and B as two planes as well and a product as
+// three (the fourth is below the last bit); the others hold one plane of A and B and
+// multiply the first planes alone, and X's second enters through a X.
+//
+// An error of X itself lies in all singular directions, and a X carries it on: the
+// steps raise the small ones by up to `a` each, a^5 = 480 in five.  An error E of A or
+// B stands to the left of X, (a + B + E) X: it turns and stretches what X holds, by
+// |E| over the least |a + b s^2 + c s^4| (0.64 with the default coefficients), and adds nothing
+// to directions that X has little of; nor does what B misses of X's second plane, as
+// B is s^2 there.  So the error does not depend on how far the singular values are
+// apart.  Five steps of 3.4445, -4.775, 2.0315, bf16 results, off by of their norm: 512 x 1024
+// of normal elements 2.3e-3, of rank 64 1.8e-3, of rank 4 1.7e-3, of which the
+// result's own rounding is 1.7e-3 (with X in one plane 2.1e-3, 2.2e-2 and 7.2e-2).  Where
+// all singular values are alike, a rounding falls the same way on each and comes out
+// as a common factor, 4.5e-3 in all of 384 x 384.  X's second plane costs memory: 4096 x 4096
+// 1311 -> 1367 us, two of 14336 x 4096 7.02 -> 7.36 ms, two of 400 x 20000 338 -> 410 us.
+// Sums, norms and the momentum are fp32 or wider.
 //
 // Inside, sides are padded to multiples of 64 with zeros, which stay zeros, and a
 // plane lies in panels of 32 columns: a row's 64 bytes of a panel, the next row's
@@ -165,12 +175,12 @@ __device__ __forceinline__ uint64_t in_panels(uint64_t row, uint32_t col, uint64
 
 // X of the group: u over its norm, m x n, padded.
 struct OrthoX {
-  uint64_t x, plane, next;  // the first matrix's first plane; bytes to the second plane (0: none), to the next matrix
+  uint64_t x, plane, next;  // the first matrix's first plane; bytes to the second plane, to the next matrix
   uint32_t m, n;            // padded
   double eps, power;        // what X is held times
 };
 // Blocks of 64 x 64 of a matrix: a tall one goes through LDS.
-template <int DT, bool TALL, int PLANES>
+template <int DT, bool TALL>
 __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX o, const double* sums, uint32_t n_sums) {
   __shared__ double red[kThreads / 64];
   __shared__ float tile[TALL ? 64 : 1][65];
@@ -197,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX 
 #pragma unroll
         for (int e = 0; e < 8; ++e) tile[lr][lc + e] = u[e];
       } else {
-        store_planes8<PLANES>(base + in_panels(row, c, o.m * (kPanel * 2)), o.plane, u);
+        store_planes8<2>(base + in_panels(row, c, o.m * (kPanel * 2)), o.plane, u);
       }
     }
     if constexpr (TALL) {
@@ -208,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX 
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[lr + e][lc];
-        store_planes8<PLANES>(base + in_panels(c0 + lc, r0 + lr, o.m * (kPanel * 2)), o.plane, v);
+        store_planes8<2>(base + in_panels(c0 + lc, r0 + lr, o.m * (kPanel * 2)), o.plane, v);
       }
       __syncthreads();
     }
@@ -221,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoIn a, OrthoX 
 // computes the tiles on and above the diagonal; else R' = R.
 struct OrthoProduct {
   uint64_t left, right, aux, out;              // of the group's first matrix
-  uint64_t left_plane, right_plane, out_plane; // bytes to the second plane; 0: one plane (aux: as out)
+  uint64_t left_plane, right_plane, out_plane; // bytes to the second plane (aux: as out); of one plane not looked at
   uint64_t left_next, right_next, out_next;    // bytes to the next matrix (aux: as out)
   uint32_t left_panel, right_panel, out_panel; // bytes from panel to panel (aux: as out)
   uint32_t rows, cols, k;                      // multiples of 64
@@ -295,14 +305,15 @@ constexpr int kSym = 0, kMid = 1, kLast = 2;
 // 16-byte pieces lie at c ^ row / 4 % 4, so that the 16 rows of a quarter read are in
 // different banks; of R as it lies, T / 32 panels of 32 rows of 64 bytes, of which half
 // a transposing read takes four rows, 256 bytes.
-// PLANES: of each operand.  GROUPS: 3 gives each of two planes' products four waves
-// and LDS of their own, for few tiles, whose steps wait for their loads (five steps in
+// PLANES: of each operand; where the result is X, it and aux have two in any case.
+// GROUPS: 3 gives each of two planes' products four waves and LDS of their own, for few tiles, whose steps wait for their loads (five steps in
 // fp32, all of 1024^3 232 us with one group and 190 with three, 512^3 152 and 137, six of
 // 1027 x 509 232 and 208; 1500^3, where the larger tiles fill the chip, 423 and 506).
 template <int MODE, int T, int PLANES, int GROUPS>
 __global__ __launch_bounds__(kThreads * GROUPS, GROUPS > 1 ? GROUPS : T >= 192 ? 1 : 2) void ortho_product_kernel(OrthoProduct p, OrthoOut o) {
   static_assert(GROUPS == 1 || (GROUPS == 3 && PLANES == 2 && T == 64), "a group's sums lie in its buffers on their way");
   constexpr bool SYM = MODE == kSym;
+  constexpr int HELD = SYM ? PLANES : 2;      // planes of aux and of the result
   constexpr uint32_t NF = T / 64;             // 32-wide pieces of a wave's side
   constexpr uint32_t kOperand = T * kStep * 2;  // bytes
   constexpr uint32_t kLoads = T / 64;         // of an operand, a thread
@@ -476,18 +487,18 @@ __global__ __launch_bounds__(kThreads * GROUPS, GROUPS > 1 ? GROUPS : T >= 192 ?
     const uint32_t row0 = i0 + wi, col0 = j0 + wj;
     const uint64_t out = p.out + z * p.out_next, aux = p.aux + z * p.out_next;
     const bool has_aux = p.aux && p.splits == 1 && group == GROUPS - 1;
-    Planes8<PLANES> x[2][kRounds];
+    Planes8<HELD> x[2][kRounds];
     auto load_aux = [&](uint32_t f) {
 #pragma unroll
       for (uint32_t r = 0; r < kRounds; ++r) {
         const uint32_t row = row0 + 32 * f + r % 2 * 16 + lane / 4, col = col0 + r / 2 * kPanel + lane % 4 * 8;
         const uint64_t at = in_panels(row < p.rows ? row : p.rows - 1, col < p.cols ? col : p.cols - 8, p.out_panel);
-        x[f % 2][r] = load_planes<PLANES>(aux + at, p.out_plane);
+        x[f % 2][r] = load_planes<HELD>(aux + at, p.out_plane);
       }
     };
     if (has_aux) {
       load_aux(0);
-      barrier_lds<kRounds * PLANES>();
+      barrier_lds<kRounds * HELD>();
     } else {
       barrier_lds<0>();
     }
@@ -502,7 +513,7 @@ __global__ __launch_bounds__(kThreads * GROUPS, GROUPS > 1 ? GROUPS : T >= 192 ?
         __syncthreads();  // with the last group, behind the item
         continue;
       }
-      barrier_lds<kRounds * PLANES>();
+      barrier_lds<kRounds * HELD>();
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const uint8_t* const at = (q < 2 ? (q == 0 ? all0 : all1) : q == 2 ? all2 : all3) + tid * 16;
@@ -541,12 +552,12 @@ __global__ __launch_bounds__(kThreads * GROUPS, GROUPS > 1 ? GROUPS : T >= 192 ?
         for (int e = 0; e < 8; ++e) v[e] = mine[q * kOut + c + e] * p.f_acc;
         if (has_aux) {
           float y[8];
-          unpack_planes<PLANES>(x[f % 2][r], y);
+          unpack_planes<HELD>(x[f % 2][r], y);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(p.f_aux, y[e], v[e]);
         }
         if (MODE != kLast && row < p.rows && col < p.cols)
-          store_planes8<PLANES>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
+          store_planes8<HELD>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
         if (turned) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) mine[q * kOut + c + e] = v[e];
@@ -572,7 +583,7 @@ __global__ __launch_bounds__(kThreads * GROUPS, GROUPS > 1 ? GROUPS : T >= 192 ?
         if (MODE == kLast) {
           if (row < o.n) ortho_out8<PLANES>(o, z, row, col, static_cast<int>(o.m) - static_cast<int>(col), v);
         } else if (row < p.cols && col < p.rows) {
-          store_planes8<PLANES>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
+          store_planes8<HELD>(out + in_panels(row, col, p.out_panel), p.out_plane, v);
         }
       }
     }
@@ -704,11 +715,13 @@ uint64_t ortho_part_bytes(const OrthoCut& c, uint32_t count) {
   return c.splits > 1 ? static_cast<uint64_t>(c.tiles) * count * c.splits * c.side * c.side * 4 : 0;
 }
 
-// A bf16 result of a shorter side of this and more comes from one plane.  Below, where
-// fewer singular directions share a rounding, one plane shows beside the result's
-// own rounding (1.7e-3): 16 x 16 2.1 to 4.1e-3, 128 x 1024 2.4e-3, 256 x 1024 2.1e-3; from
-// 384 to 4096 1.9 to 2.0e-3.  Two take 127 us for 88 (256 x 1024), 109 for 75 (four of
-// 256 x 256), 812 for 390 (four of 383 x 16000).
+// A bf16 result of a shorter side of this and more takes A, B and the products from
+// one plane and is off by 2.0e-3 (4096) to 2.7e-3 (384 x 16000) of its norm for normal elements,
+// 1.7e-3 of it its own rounding.  Below, one plane would give 2.3e-3 (128 x 1024) to 3.1e-3
+// (16 x 16) and save launches' time above all, 98 us for 134 (256 x 1024), 86 for 116
+// (four of 256 x 256), at most 528 for 809 (four of 383 x 16000); two give 1.7e-3.  Above, the
+// products are the time, and two planes take three times as many (2048 x 2048 668 us
+// for 296, 4096 x 4096 3808 for 1358).
 constexpr uint64_t kOnePlane = 384;
 
 // Matrices at once and their place in the workspace.
@@ -716,7 +729,7 @@ struct OrthoPlan {
   uint64_t m, n;  // padded
   bool tall;
   uint32_t planes, group;
-  uint64_t x_bytes, a_bytes;  // of one matrix, all planes
+  uint64_t x_bytes, a_bytes;  // of one matrix, all planes; X has two
   uint64_t sums, x0, x1, a, b, part, bytes;  // offsets, and the whole
   OrthoCut gram, poly, mid;
 };
@@ -726,7 +739,7 @@ OrthoPlan ortho_plan(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype
   p.m = padded(p.tall ? cols : rows);
   p.n = padded(p.tall ? rows : cols);
   p.planes = out_dtype == kF32 || std::min(rows, cols) < kOnePlane ? 2 : 1;
-  p.x_bytes = p.m * p.n * 2 * p.planes;
+  p.x_bytes = p.m * p.n * 4;
   p.a_bytes = p.m * p.m * 2 * p.planes;
   // as many as keep the chip at work: a round of 256 tiles, four times
   const uint64_t tiles = ((p.m + 255) / 256) * ((p.m + 255) / 256);
@@ -799,21 +812,21 @@ hipError_t product_of(const OrthoProduct& p, const OrthoOut& o, const OrthoCut& 
   return product_as<MODE, 64, PLANES>(p, o, st);
 }
 template <int MODE>
-hipError_t product(OrthoProduct& p, const OrthoOut& o, const OrthoCut& c, hipStream_t st) {
+hipError_t product(OrthoProduct& p, const OrthoOut& o, const OrthoCut& c, uint32_t planes, hipStream_t st) {
   p.ti = c.ti;
   p.tj = c.tj;
   p.tiles = c.tiles;
   p.splits = c.splits;
   p.split_k = c.split_k;
-  const hipError_t e = p.left_plane ? product_of<MODE, 2>(p, o, c, st) : product_of<MODE, 1>(p, o, c, st);
+  const hipError_t e = planes == 2 ? product_of<MODE, 2>(p, o, c, st) : product_of<MODE, 1>(p, o, c, st);
   if (e != hipSuccess || p.splits == 1) return e;
   const uint64_t items = static_cast<uint64_t>(p.count) * p.tiles * (c.side / kPanel) * (c.side / kJoinRows);
-  return launch_op(p.left_plane ? ortho_join_kernel<2> : ortho_join_kernel<1>, grid_for(items, kThreads), kThreads, st, p, c.side);
+  return launch_op(planes == 2 ? ortho_join_kernel<2> : ortho_join_kernel<1>, grid_for(items, kThreads), kThreads, st, p, c.side);
 }
 
-template <int DT, int PLANES>
+template <int DT>
 hipError_t load_x(const OrthoIn& in, const OrthoX& x, bool tall, dim3 grid, const double* sums, uint32_t n_sums, hipStream_t st) {
-  return launch_op(tall ? ortho_load_kernel<DT, true, PLANES> : ortho_load_kernel<DT, false, PLANES>, grid, kThreads, st, in, x, sums, n_sums);
+  return launch_op(tall ? ortho_load_kernel<DT, true> : ortho_load_kernel<DT, false>, grid, kThreads, st, in, x, sums, n_sums);
 }
 
 }  // namespace
@@ -840,7 +853,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
   double* const sums = reinterpret_cast<double*>(ws + plan.sums);
   float* const part = reinterpret_cast<float*>(ws + plan.part);
   const uint32_t panel = static_cast<uint32_t>(plan.m * (kPanel * 2));  // of X and of A and B: all have m rows
-  const uint64_t x_plane = plan.planes == 2 ? plan.m * plan.n * 2 : 0, a_plane = plan.planes == 2 ? plan.m * plan.m * 2 : 0;
+  const uint64_t x_plane = plan.m * plan.n * 2, a_plane = plan.m * plan.m * 2;
   for (uint32_t z0 = 0; z0 < a.count; z0 += plan.group) {
     const uint32_t count = std::min(plan.group, a.count - z0);
     OrthoIn in{};
@@ -871,8 +884,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
     uint64_t x = ws + plan.x0, other = ws + plan.x1;
     const OrthoX ox{x, x_plane, plan.x_bytes, static_cast<uint32_t>(plan.m), static_cast<uint32_t>(plan.n), a.eps, std::ldexp(1.0, ex)};
     const dim3 load_grid(grid_for((plan.m / 64) * (plan.n / 64), kThreads), count);
-    if (a.dtype == kBf16) e = plan.planes == 2 ? load_x<kBf16, 2>(in, ox, plan.tall, load_grid, sums, blocks, st) : load_x<kBf16, 1>(in, ox, plan.tall, load_grid, sums, blocks, st);
-    else e = plan.planes == 2 ? load_x<kF32, 2>(in, ox, plan.tall, load_grid, sums, blocks, st) : load_x<kF32, 1>(in, ox, plan.tall, load_grid, sums, blocks, st);
+    e = a.dtype == kBf16 ? load_x<kBf16>(in, ox, plan.tall, load_grid, sums, blocks, st) : load_x<kF32>(in, ox, plan.tall, load_grid, sums, blocks, st);
     if (e != hipSuccess) return e;
     for (uint32_t s = 0; s < a.steps; ++s) {
       const double* const k = a.coefs + 3 * s;
@@ -891,7 +903,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
       p.count = count;
       p.part = part;
       p.f_acc = static_cast<float>(std::ldexp(1.0, ea - 2 * ex));
-      if ((e = product<kSym>(p, out, plan.gram, st)) != hipSuccess) return e;
+      if ((e = product<kSym>(p, out, plan.gram, plan.planes, st)) != hipSuccess) return e;
       uint64_t left = p.out;
       int el = ea;
       double by = k[1];  // of A X; B = b A needs no product of its own
@@ -904,7 +916,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
         p.k = static_cast<uint32_t>(plan.m);
         p.f_acc = static_cast<float>(std::ldexp(k[2], eb - 2 * ea));
         p.f_aux = static_cast<float>(std::ldexp(k[1], eb - ea));
-        if ((e = product<kSym>(p, out, plan.poly, st)) != hipSuccess) return e;
+        if ((e = product<kSym>(p, out, plan.poly, plan.planes, st)) != hipSuccess) return e;
         left = p.out;
         el = eb;
         by = 1.0;
@@ -926,7 +938,7 @@ hipError_t launch_ortho(const Ortho& a, hipStream_t st) {
       p.k = static_cast<uint32_t>(plan.m);
       p.f_acc = static_cast<float>(std::ldexp(by * scale, eo - el - ex));
       p.f_aux = static_cast<float>(std::ldexp(k[0] * scale, eo - ex));
-      e = last ? product<kLast>(p, out, plan.mid, st) : product<kMid>(p, out, plan.mid, st);
+      e = last ? product<kLast>(p, out, plan.mid, plan.planes, st) : product<kMid>(p, out, plan.mid, plan.planes, st);
       if (e != hipSuccess) return e;
       std::swap(x, other);
       ex = eo;
