@@ -645,10 +645,15 @@ typedef struct {
  * LC_DT_BF16 and sides of 384 and more the steps hold X to 22 bits, A and their
  * products' operands to 11, otherwise all to 22 bits, in three times the products.
  * Errors are relative to the largest singular value that |X| <= 1 allows (a matrix
- * that eps far outweighs loses bits): with the coefficients above a result
- * in bf16 is off by 2.0e-3 of its norm, 1.7e-3 of it the rounding of the result itself,
- * one in fp32 by 1e-6 to 2e-6.  Coefficients that let the largest singular value grow
- * beyond 2^30 or fall below 2^-30 are refused.  A matrix of zeros gives zeros; one that
+ * that eps far outweighs loses bits).  After five steps of the coefficients above a
+ * result in bf16 is off by 1.7e-3 to 2.7e-3 of its norm, 1.7e-3 of it the rounding of
+ * the result itself, whatever its singular values are; where they are all alike, by up
+ * to 5e-3.  One in fp32 is off by 1e-6 to 2e-6 if its elements are normal noise, and by
+ * up to 2e-4 if few singular values carry the norm (4096 x 4096 of rank 1), for the
+ * steps raise what lies in the other directions by up to a^5 = 480 (the formula in fp32
+ * throughout: 1e-6 to 1e-5, and 5e-4).
+ * Coefficients that let the largest singular value grow beyond 2^30 or fall below
+ * 2^-30 are refused.  A matrix of zeros gives zeros; one that
  * holds an infinity or a NaN gives NaN throughout (its momentum holds them where they
  * were), and the matrices beside it are as ever.  The results are what
  * lc_muon_step_score takes.  The workspace is that of the matrices which are worked
