@@ -768,18 +768,18 @@ double largest(double x, double a, double b, double c) { return std::fabs(x * (a
 // The largest |a s + b s^3 + c s^5| of s in [0, top].
 double ortho_bound(double top, const double* k) {
   double best = largest(top, k[0], k[1], k[2]);
-  // its slope is a + 3 b q + 5 c q^2, q = s^2
-  const double a = 5 * k[2], b = 3 * k[1], c = k[0];
+  const double m = std::max({std::fabs(k[0]), std::fabs(k[1]), std::fabs(k[2])});
+  if (m == 0) return 0;
+  // its slope is a + 3 b q + 5 c q^2, q = s^2, over m, lest d overflows.  -b and the root of
+  // d are added where both have one sign: their difference would lose the smaller
+  // root, which the other gives as it divides c / a.
+  const double a = 5 * (k[2] / m), b = 3 * (k[1] / m), c = k[0] / m, d = b * b - 4 * a * c;
   double roots[2];
   int n = 0;
-  if (a != 0) {
-    const double d = b * b - 4 * a * c;
-    if (d >= 0) {
-      roots[n++] = (-b + std::sqrt(d)) / (2 * a);
-      roots[n++] = (-b - std::sqrt(d)) / (2 * a);
-    }
-  } else if (b != 0) {
-    roots[n++] = -c / b;
+  if (d >= 0) {
+    const double t = -0.5 * (b + std::copysign(std::sqrt(d), b));
+    if (a != 0) roots[n++] = t / a;
+    if (t != 0) roots[n++] = c / t;
   }
   for (int i = 0; i < n; ++i)
     if (roots[i] > 0 && roots[i] < top * top) best = std::max(best, largest(std::sqrt(roots[i]), k[0], k[1], k[2]));

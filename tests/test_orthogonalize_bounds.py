@@ -1,0 +1,35 @@
+"""The bound on the largest singular value that the orthogonalised update reckons with, from which calls it refuses (CPU: no call
+here enqueues anything).  X is held times a power of two that the bound allows: one that is too small lets fp16 overflow."""
+import numpy as np
+import pytest
+
+from paper_2609_27193_amd import layercheck as LC
+from tests.test_more_operators_abi import ortho
+from tests.test_operators_abi import refused
+
+
+def largest(coefs):
+    """What the steps let it grow to, by a dense scan of each polynomial: they start from 1, and a step adds 2% for roundings."""
+    top = 1.0
+    for a, b, c in coefs:
+        s = np.linspace(0.0, top, 200001)
+        top = 1.02 * np.abs(s * (a + s * s * (b + s * s * c))).max()
+    return top
+
+
+BOUNDS = [[(3.4445, -4.775, 2.0315)] * 5, [(1.5, -0.5, 0.0)] * 9, [(2.0, -1.5, 0.5)] * 4, [(0.0, 3.0, -2.0)], [(1.0, 0.0, -1.0)] * 2,
+          [(-1.0, 0.0, 0.0)], [(1.6, -2.0, 0.7)] * 3, [(0.0, 0.0, 1.0)], [(1e-3, -2e-3, 1e-3)]]
+# c of what is left of a subtraction, or of a fit: the steps end near the polynomial's zero, with its largest value inside
+BOUNDS += [[(1.698, 0.0, 0.0), (1.5, -0.5, c)] for c in (1e-18, -1e-18, 1e-12, -1e-12, 1e-9, 1e-6, 5e-324, 1e-300, 0.0)]
+BOUNDS += [[(0.98, 0.0, 0.0), (1.0, b, -1.0)] for b in (1e-18, -1e-18, 1e-9, 0.0)]
+BOUNDS += [[(0.98, 0.0, 0.0), (a, 1.0, -1.0)] for a in (1e-18, -1e-18, 1e-9, 0.0)]
+
+
+@pytest.mark.parametrize("coefs", BOUNDS)
+def test_ortho_bound_is_the_largest_value_of_the_steps(coefs):
+    """One step more, of a factor alone, that brings the bound just below or above the most and the least that are taken."""
+    for edge, inside in ((2.0 ** 30, 0.999), (2.0 ** -30, 1.001)):
+        k = edge / (1.02 * largest(coefs))
+        refused(ortho, prm=LC.orthogonalize_params(len(coefs) + 1, coefs + [(k * inside, 0.0, 0.0)]), size=0, says="workspace",
+                code=LC.LC_ERR_CAPACITY)  # the coefficients are taken
+        refused(ortho, prm=LC.orthogonalize_params(len(coefs) + 1, coefs + [(k / inside, 0.0, 0.0)]), size=0, says="singular")

@@ -46,7 +46,7 @@ def matrix(rows, cols, kind, seed=0):
 
 def held(x, planes):
     """x in 11 bits or 22: an fp16 number near 2^15 and the rest, 2^11 times as large, in another."""
-    power = 2.0 ** (14 - torch.floor(torch.log2(x.abs().max())))
+    power = 2.0 ** (14 - torch.floor(torch.log2(x.abs().max()))) if bool(x.any()) else 1.0
     hi = (x * power).half().double()
     return (hi if planes == 1 else hi + ((x * power - hi) * 2048).half().double() / 2048) / power
 
@@ -82,3 +82,20 @@ def test_few_large_singular_values(rows, cols, kind, out, coefs):
     off = distance(got, want)
     print(f"{rows} x {cols} {kind} {out}: {off:.2e}, bound {bound:.2e}")
     assert off <= bound
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 64), (70, 300), (500, 400)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("tiny", [1e-18, -1e-18, 1e-12])
+def test_a_tiny_coefficient(rows, cols, out, tiny):
+    """s = 1.698 s, then 1.5 s - 0.5 s^3 + tiny s^5, which has its largest value of 1 inside and ends near its zero, then s: what a step
+    holds must not overflow."""
+    coefs = [(1.698, 0.0, 0.0), (1.5, -0.5, tiny), (1.0, 0.0, 0.0)]
+    u = matrix(rows, cols, "normal")
+    got = call([Guarded(rows, cols, torch.float32, value=u)], out, len(coefs), coefs)[0].view
+    want = steps(u.double(), coefs)
+    planes = 1 if out == "bf16" and min(rows, cols) >= ONE_PLANE else 2
+    bound = 1.5 * distance(steps(u.double(), coefs, held, planes), want) + 2 * distance(steps(u, coefs), want)
+    if out == "bf16":
+        bound += 1.1 * distance(want.bfloat16(), want)
+    assert distance(got, want) <= bound
