@@ -657,7 +657,8 @@ typedef struct {
  * holds an infinity or a NaN gives NaN throughout (its momentum holds them where they
  * were), and the matrices beside it are as ever.  The results are what
  * lc_muon_step_score takes.  The workspace is that of the matrices which are worked
- * on at once, and goes by the results' dtype. */
+ * on at once, of whose X, A and B it holds 4 GiB at most, or one matrix's, and goes by
+ * the results' dtype. */
 uint64_t lc_orthogonalize_workspace(uint32_t n_matrices, uint64_t rows, uint64_t cols, int32_t out_dtype);
 lc_status lc_orthogonalize(const lc_orthogonalize_params *params, uint32_t n_matrices, const lc_matrix *grads,
                            const lc_matrix *momenta, const lc_matrix *out, void *workspace, uint64_t workspace_bytes,

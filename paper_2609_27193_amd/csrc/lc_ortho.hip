@@ -682,6 +682,13 @@ double ortho_us(const OrthoCost& c, uint64_t blocks, uint32_t steps) {
   }
   return us;
 }
+constexpr uint64_t kMostPartBytes = 256ull * 256 * 256 * 4;  // of a round of blocks
+constexpr bool within_most_parts() {
+  for (const OrthoCost& c : kOrthoCosts)
+    if (256ull * c.per_cu * c.side * c.side * 4 > kMostPartBytes) return false;
+  return true;
+}
+static_assert(within_most_parts(), "parts are of one round at most");
 // A symmetric product may be split over its sum, whose parts then go through memory
 // (4 TB/s there and back) and a join.
 OrthoCut ortho_cut(uint64_t rows, uint64_t cols, uint64_t k, uint32_t count, bool sym, int planes) {
@@ -724,6 +731,13 @@ uint64_t ortho_part_bytes(const OrthoCut& c, uint32_t count) {
 // for 296, 4096 x 4096 3808 for 1358).
 constexpr uint64_t kOnePlane = 384;
 
+// Of X, A and B of the matrices at once, more than which only a single one takes.  Of
+// such long ones fewer keep the chip at work as well: 64 of 256 x 65536 (bf16, five
+// steps) in three turns 26.2 ms, in one, of 8 GiB, 26.6; 24 of 512 x 65536 (fp32, three) in two
+// 19.0 and in one 19.0; eight of 4096 x 65536 (bf16, two) each alone 53.8, four at once 56.8.
+// Even turns: 17 of 2048 x 2048 3.62 ms, as 16 and 1 3.79.
+constexpr uint64_t kOrthoSpace = 4ull << 30;
+
 // Matrices at once and their place in the workspace.
 struct OrthoPlan {
   uint64_t m, n;  // padded
@@ -741,19 +755,24 @@ OrthoPlan ortho_plan(uint32_t count, uint64_t rows, uint64_t cols, int out_dtype
   p.planes = out_dtype == kF32 || std::min(rows, cols) < kOnePlane ? 2 : 1;
   p.x_bytes = p.m * p.n * 4;
   p.a_bytes = p.m * p.m * 2 * p.planes;
-  // as many as keep the chip at work: a round of 256 tiles, four times
+  // as many as keep the chip at work, a round of 256 tiles four times, unless they are so
+  // long that fewer do and more would only take memory
   const uint64_t tiles = ((p.m + 255) / 256) * ((p.m + 255) / 256);
-  p.group = static_cast<uint32_t>(std::min<uint64_t>(count, std::max<uint64_t>(1, 1024 / tiles)));
+  const uint64_t most = std::max<uint64_t>(1, std::min(1024 / tiles, kOrthoSpace / (2 * (p.x_bytes + p.a_bytes))));
+  const uint32_t places = static_cast<uint32_t>(std::min<uint64_t>(count, most));
+  const uint32_t turns = (count + places - 1) / places;
+  p.group = (count + turns - 1) / turns;  // 17 as 9 and 8, not as 16 and 1
   p.gram = ortho_cut(p.m, p.m, p.n, p.group, true, p.planes);
   p.poly = ortho_cut(p.m, p.m, p.m, p.group, true, p.planes);
   p.mid = ortho_cut(p.m, p.n, p.m, p.group, false, p.planes);
   p.sums = 0;
   p.x0 = kOrthoMost * kNormBlocks * 8;
-  p.x1 = p.x0 + p.group * p.x_bytes;
-  p.a = p.x1 + p.group * p.x_bytes;
-  p.b = p.a + p.group * p.a_bytes;
-  p.part = p.b + p.group * p.a_bytes;
-  p.bytes = p.part + std::max(ortho_part_bytes(p.gram, p.group), ortho_part_bytes(p.poly, p.group));
+  p.x1 = p.x0 + places * p.x_bytes;
+  p.a = p.x1 + places * p.x_bytes;
+  p.b = p.a + places * p.a_bytes;
+  p.part = p.b + places * p.a_bytes;
+  // of several turns room for any parts, lest 17 need less than 16
+  p.bytes = p.part + (turns > 1 ? kMostPartBytes : std::max(ortho_part_bytes(p.gram, p.group), ortho_part_bytes(p.poly, p.group)));
   return p;
 }
 

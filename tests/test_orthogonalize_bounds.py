@@ -33,3 +33,19 @@ def test_ortho_bound_is_the_largest_value_of_the_steps(coefs):
         refused(ortho, prm=LC.orthogonalize_params(len(coefs) + 1, coefs + [(k * inside, 0.0, 0.0)]), size=0, says="workspace",
                 code=LC.LC_ERR_CAPACITY)  # the coefficients are taken
         refused(ortho, prm=LC.orthogonalize_params(len(coefs) + 1, coefs + [(k / inside, 0.0, 0.0)]), size=0, says="singular")
+
+
+GIB = 1 << 30
+
+
+@pytest.mark.parametrize("rows,cols", [(256, 65536), (65536, 512), (1024, 65536), (2000, 60000), (300, 40000), (4096, 65536)])
+@pytest.mark.parametrize("dtype", [LC.LC_DT_BF16, LC.LC_DT_F32], ids=["bf16", "f32"])
+def test_workspace_of_many_long_matrices(rows, cols, dtype):
+    """X goes from one buffer to another, each of 4 bytes an element in padded sides, beside A and B of 4 or 2: as many matrices as
+    take 4 GiB of these are worked on at once, or one; the rest of the workspace are sums and parts of sums."""
+    m, n = (-(-x // 64) * 64 for x in sorted((rows, cols)))
+    each = 8 * m * n + 8 * m * m
+    alone = LC.lc_orthogonalize_workspace(1, rows, cols, dtype)
+    needs = [LC.lc_orthogonalize_workspace(count, rows, cols, dtype) for count in (1, 2, 5, 8, 15, 16, 17, 40, 64)]
+    assert max(needs) <= max(4 * GIB, each) + 256 * (1 << 20)
+    assert needs == sorted(needs) and needs[0] == alone

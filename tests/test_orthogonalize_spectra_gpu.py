@@ -14,7 +14,7 @@ import pytest
 import torch
 
 from tests.test_operators_gpu import Guarded, gen
-from tests.test_orthogonalize_gpu import CUBIC, STEEP, call
+from tests.test_orthogonalize_gpu import CUBIC, STEEP, call, whole
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +99,18 @@ def test_a_tiny_coefficient(rows, cols, out, tiny):
     if out == "bf16":
         bound += 1.1 * distance(want.bfloat16(), want)
     assert distance(got, want) <= bound
+
+
+@pytest.mark.parametrize("rows,cols,n,dtype", [(2050, 1900, 17, "bf16"), (1000, 60000, 9, "f32"), (4000, 3970, 5, "bf16")])
+def test_matrices_in_turns(rows, cols, n, dtype):
+    """More matrices than are worked on at once, in turns of 9 and 8, of 5 and 4, of 3 and 2: whole numbers come out exactly."""
+    grads = [whole(rows, cols, 6, s, dtype) for s in range(n)]
+    outs = call(grads, dtype, 1, (1.0, 1.0, 0.0))
+    for g, o in zip(grads, outs):
+        x = g.view.double()
+        x = (x.t() if rows > cols else x).contiguous()
+        gram = x @ x.t().contiguous()
+        assert gram.abs().max() <= 2048  # eleven bits
+        want = (x + gram @ x / 4.0 ** 6) / 2.0 ** 6
+        want = want.t() if rows > cols else want
+        assert torch.equal(o.view, want.float().to(o.view.dtype))
