@@ -625,7 +625,7 @@ lc_status lc_linear_wgrad(const lc_matrix *dy, const lc_saved_act *saved, const 
 typedef struct {
   uint32_t steps;      /* Newton-Schulz steps, 1 to 32                             */
   int32_t nesterov;    /* 0 or 1                                                   */
-  double momentum;     /* mu, in [0, 1); not looked at without momenta             */
+  double momentum;     /* mu, in [0, 1) in any call; without momenta of no effect  */
   double eps;          /* added to the norm, finite and >= 0 (e.g. 1e-7)           */
   double scale;        /* of the result, 0 or 2^-64 to 2^64 in magnitude
                           (e.g. 0.2 sqrt(max(rows, cols)))                         */

@@ -1,11 +1,15 @@
 """The bound on the largest singular value that the orthogonalised update reckons with, from which calls it refuses (CPU: no call
 here enqueues anything).  X is held times a power of two that the bound allows: one that is too small lets fp16 overflow."""
+import os
+
 import numpy as np
 import pytest
 
 from paper_2609_27193_amd import layercheck as LC
 from tests.test_more_operators_abi import ortho
 from tests.test_operators_abi import refused
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "layercheck.h")
 
 
 def largest(coefs):
@@ -49,3 +53,12 @@ def test_workspace_of_many_long_matrices(rows, cols, dtype):
     needs = [LC.lc_orthogonalize_workspace(count, rows, cols, dtype) for count in (1, 2, 5, 8, 15, 16, 17, 40, 64)]
     assert max(needs) <= max(4 * GIB, each) + 256 * (1 << 20)
     assert needs == sorted(needs) and needs[0] == alone
+
+
+def test_momentum_is_checked_without_momenta_too():
+    """As the header says: it lies in [0, 1) in any call."""
+    for bad in (1.0, -0.1, np.nan):
+        refused(ortho, prm=LC.orthogonalize_params(5, momentum=bad), says="momentum")
+    for good in (0.0, 0.95):
+        refused(ortho, prm=LC.orthogonalize_params(5, momentum=good), size=0, says="workspace", code=LC.LC_ERR_CAPACITY)
+    assert "mu, in [0, 1) in any call" in open(HEADER).read()

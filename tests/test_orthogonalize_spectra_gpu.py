@@ -114,3 +114,10 @@ def test_matrices_in_turns(rows, cols, n, dtype):
         want = (x + gram @ x / 4.0 ** 6) / 2.0 ** 6
         want = want.t() if rows > cols else want
         assert torch.equal(o.view, want.float().to(o.view.dtype))
+
+
+def test_a_momentum_without_momenta_has_no_effect():
+    grad = Guarded(60, 90, torch.float32, value=matrix(60, 90, "normal"))
+    plain = call([grad], "f32", momentum=0.0)[0].view
+    for nesterov in (False, True):
+        assert torch.equal(call([grad], "f32", momentum=0.95, nesterov=nesterov)[0].view, plain)
