@@ -653,12 +653,12 @@ typedef struct {
  * steps raise what lies in the other directions by up to a^5 = 480 (the formula in fp32
  * throughout: 1e-6 to 1e-5, and 5e-4).
  * Coefficients that let the largest singular value grow beyond 2^30 or fall below
- * 2^-30 are refused.  A matrix of zeros gives zeros; one that
- * holds an infinity or a NaN gives NaN throughout (its momentum holds them where they
- * were), and the matrices beside it are as ever.  The results are what
- * lc_muon_step_score takes.  The workspace is that of the matrices which are worked
- * on at once, of whose X, A and B it holds 4 GiB at most, or one matrix's, and goes by
- * the results' dtype. */
+ * 2^-30 are refused (from 1 on, with half a percent a step for roundings).  A matrix of
+ * zeros gives zeros; one that holds an infinity or a NaN gives NaN throughout (its
+ * momentum holds them where they were), and the matrices beside it are as ever.  The
+ * results are what lc_muon_step_score takes.  The workspace is that of the matrices
+ * which are worked on at once, of whose X, A and B it holds 4 GiB at most, or one
+ * matrix's, and goes by the results' dtype. */
 uint64_t lc_orthogonalize_workspace(uint32_t n_matrices, uint64_t rows, uint64_t cols, int32_t out_dtype);
 lc_status lc_orthogonalize(const lc_orthogonalize_params *params, uint32_t n_matrices, const lc_matrix *grads,
                            const lc_matrix *momenta, const lc_matrix *out, void *workspace, uint64_t workspace_bytes,

@@ -12,12 +12,15 @@ from tests.test_operators_abi import refused
 HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "layercheck.h")
 
 
+ROUNDINGS = 1.005
+
+
 def largest(coefs):
-    """What the steps let it grow to, by a dense scan of each polynomial: they start from 1, and a step adds 2% for roundings."""
+    """What the steps let it grow to, by a dense scan of each polynomial: they start from 1, and a step adds 0.5% for roundings."""
     top = 1.0
     for a, b, c in coefs:
         s = np.linspace(0.0, top, 200001)
-        top = 1.02 * np.abs(s * (a + s * s * (b + s * s * c))).max()
+        top = ROUNDINGS * np.abs(s * (a + s * s * (b + s * s * c))).max()
     return top
 
 
@@ -33,10 +36,22 @@ BOUNDS += [[(0.98, 0.0, 0.0), (a, 1.0, -1.0)] for a in (1e-18, -1e-18, 1e-9, 0.0
 def test_ortho_bound_is_the_largest_value_of_the_steps(coefs):
     """One step more, of a factor alone, that brings the bound just below or above the most and the least that are taken."""
     for edge, inside in ((2.0 ** 30, 0.999), (2.0 ** -30, 1.001)):
-        k = edge / (1.02 * largest(coefs))
+        k = edge / (ROUNDINGS * largest(coefs))
         refused(ortho, prm=LC.orthogonalize_params(len(coefs) + 1, coefs + [(k * inside, 0.0, 0.0)]), size=0, says="workspace",
                 code=LC.LC_ERR_CAPACITY)  # the coefficients are taken
         refused(ortho, prm=LC.orthogonalize_params(len(coefs) + 1, coefs + [(k / inside, 0.0, 0.0)]), size=0, says="singular")
+
+
+# Each step's polynomial turns upwards right behind the range that the one before leaves: 1.99, 1.97, 1.87, 1.56, 1.13, 1.
+SHARP = [(8.2, -22.9, 16.5), (4.07, -2.87, 0.522), (3.92, -2.83, 0.53), (3.29, -2.42, 0.49), (2.28, -1.62, 0.40), (1.87, -1.23, 0.36),
+         (1.875, -1.25, 0.375)]
+
+
+def test_steps_that_need_their_range_are_taken():
+    """The largest singular value stays below 2 in exact arithmetic; what is added for roundings must not run away with it."""
+    assert largest(SHARP) < 1.1
+    for n in range(1, len(SHARP) + 1):
+        refused(ortho, prm=LC.orthogonalize_params(n, SHARP[:n]), size=0, says="workspace", code=LC.LC_ERR_CAPACITY)
 
 
 GIB = 1 << 30

@@ -14,6 +14,7 @@ import pytest
 import torch
 
 from tests.test_operators_gpu import Guarded, gen
+from tests.test_orthogonalize_bounds import SHARP
 from tests.test_orthogonalize_gpu import CUBIC, STEEP, call, whole
 
 pytestmark = pytest.mark.gpu
@@ -65,13 +66,7 @@ def distance(x, want):
     return (torch.linalg.matrix_norm(x.double() - want) / torch.linalg.matrix_norm(want)).item()
 
 
-SIDES = [(16, 16), (40, 300), (383, 512), (384, 384), (512, 1024), (1500, 400), (1100, 1090)]
-
-
-@pytest.mark.parametrize("rows,cols", SIDES)
-@pytest.mark.parametrize("kind,out", [(k, o) for o in ("bf16", "f32") for k in KINDS if (k, o) != ("identity", "f32")])
-@pytest.mark.parametrize("coefs", [[STEEP] * 5, [CUBIC] * 5, [(2.0, -1.5, 0.5)] * 8], ids=["steep", "cubic", "quintic"])
-def test_few_large_singular_values(rows, cols, kind, out, coefs):
+def check(rows, cols, kind, out, coefs):
     u = matrix(rows, cols, kind)
     got = call([Guarded(rows, cols, torch.float32, value=u)], out, len(coefs), coefs)[0].view
     want = steps(u.double(), coefs)
@@ -84,6 +79,16 @@ def test_few_large_singular_values(rows, cols, kind, out, coefs):
     assert off <= bound
 
 
+SIDES = [(16, 16), (40, 300), (383, 512), (384, 384), (512, 1024), (1500, 400), (1100, 1090)]
+
+
+@pytest.mark.parametrize("rows,cols", SIDES)
+@pytest.mark.parametrize("kind,out", [(k, o) for o in ("bf16", "f32") for k in KINDS if (k, o) != ("identity", "f32")])
+@pytest.mark.parametrize("coefs", [[STEEP] * 5, [CUBIC] * 5, [(2.0, -1.5, 0.5)] * 8], ids=["steep", "cubic", "quintic"])
+def test_few_large_singular_values(rows, cols, kind, out, coefs):
+    check(rows, cols, kind, out, coefs)
+
+
 @pytest.mark.parametrize("rows,cols", [(64, 64), (70, 300), (500, 400)])
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("tiny", [1e-18, -1e-18, 1e-12])
@@ -91,14 +96,16 @@ def test_a_tiny_coefficient(rows, cols, out, tiny):
     """s = 1.698 s, then 1.5 s - 0.5 s^3 + tiny s^5, which has its largest value of 1 inside and ends near its zero, then s: what a step
     holds must not overflow."""
     coefs = [(1.698, 0.0, 0.0), (1.5, -0.5, tiny), (1.0, 0.0, 0.0)]
-    u = matrix(rows, cols, "normal")
-    got = call([Guarded(rows, cols, torch.float32, value=u)], out, len(coefs), coefs)[0].view
-    want = steps(u.double(), coefs)
-    planes = 1 if out == "bf16" and min(rows, cols) >= ONE_PLANE else 2
-    bound = 1.5 * distance(steps(u.double(), coefs, held, planes), want) + 2 * distance(steps(u, coefs), want)
-    if out == "bf16":
-        bound += 1.1 * distance(want.bfloat16(), want)
-    assert distance(got, want) <= bound
+    check(rows, cols, "normal", out, coefs)
+
+
+@pytest.mark.parametrize("rows,cols", [(90, 70), (384, 512)])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_steps_that_need_their_range(rows, cols, kind, out):
+    """Polynomials that turn upwards right behind the range that the step before leaves."""
+    if (kind, out) != ("identity", "f32"):
+        check(rows, cols, kind, out, SHARP)
 
 
 @pytest.mark.parametrize("rows,cols,n,dtype", [(2050, 1900, 17, "bf16"), (1000, 60000, 9, "f32"), (4000, 3970, 5, "bf16")])
