@@ -32,8 +32,9 @@
 // Inside, sides are padded to multiples of 64 with zeros, which stay zeros, and a
 // plane lies in panels of 32 columns: a row's 64 bytes of a panel, the next row's
 // behind it.  What a step of a product takes of either operand is then whole
-// kilobytes of neighbours (4096^3 with tiles of 256, in rows as they are 124 us, in
-// panels 114; its upper half with tiles of 192 100 and 78).
+// kilobytes of neighbours (4096^3 with tiles of 256, X in one plane, in rows as they
+// are 124 us, in panels 114, with both of its planes 124; its upper half with tiles of
+// 192 100 and 78).
 #include <algorithm>
 #include <cmath>
 
@@ -660,8 +661,8 @@ struct OrthoCut {
 };
 // What a block of a side takes, measured (us): beside its steps, and a step of 32, of
 // 1 to per_cu blocks a CU; `lone`, a step of one on the whole chip.  A step of three
-// groups is one of each.  The upper half and the whole of n^3, tiles of 64 / 128 / 192 /
-// 256: n = 1024 8, 11, 18, 29 and 8, 10, 16, 25; 2048 20, 19, 29, 45 and 28, 21, 29, 43;
+// groups is one of each.  The upper half and the whole of n^3 (without X's second plane,
+// which any side writes alike), tiles of 64 / 128 / 192 / 256: n = 1024 8, 11, 18, 29 and 8, 10, 16, 25; 2048 20, 19, 29, 45 and 28, 21, 29, 43;
 // 3000 58, 43, 42, 64 and 88, 65, 51, 65; 4096 154, 90, 68, 88 and 222, 125, 127, 112.
 struct OrthoCost {
   uint32_t side, groups, per_cu;

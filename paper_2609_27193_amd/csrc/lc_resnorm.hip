@@ -121,7 +121,8 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void res_norm_fwd_kernel(ResNorm
 }
 
 // Rows of any length (fewer than 8 columns, or beyond kNormLongest): both addends
-// are read again for each of the steps.
+// are read again for each of the steps.  4096 x 20000 in bf16 137 us, layer norm 160 (96 at
+// the copy's rate); 65536 x 7 520 us, for a block takes each row.
 template <int DT, int RT, bool LAYER>
 __global__ __launch_bounds__(kLongThreads) void res_norm_fwd_long_kernel(ResNormFwd a) {
   __shared__ float2 red[2][kLongThreads / 64];
@@ -341,7 +342,8 @@ __global__ __launch_bounds__(kNormThreads<TPR>) void res_norm_bwd_kernel(ResNorm
 }
 
 // Rows of any length, as above: a block's partial sums stay in its part of the
-// workspace, each element with the thread that it belongs to.
+// workspace, each element with the thread that it belongs to.  4096 x 20000 in bf16 254 us,
+// layer norm 348 (96 at the copy's rate); 65536 x 7 873 us.
 template <int DT, int RT, bool LAYER, bool KEPT>
 __global__ __launch_bounds__(kLongThreads) void res_norm_bwd_long_kernel(ResNormBwd a, uint32_t parts) {
   __shared__ float2 red[2][kLongThreads / 64];
