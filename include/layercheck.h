@@ -651,7 +651,8 @@ typedef struct {
  * to 5e-3.  One in fp32 is off by 1e-6 to 2e-6 if its elements are normal noise, and by
  * up to 2e-4 if few singular values carry the norm (4096 x 4096 of rank 1), for the
  * steps raise what lies in the other directions by up to a^5 = 480 (the formula in fp32
- * throughout: 1e-6 to 1e-5, and 5e-4).
+ * throughout: 1e-6 to 1e-5, and 5e-4).  A step that takes a singular value near zero, by
+ * terms that cancel, leaves it their last bits' error, which later steps may raise.
  * Coefficients that let the largest singular value grow beyond 2^30 or fall below
  * 2^-30 are refused (from 1 on, with half a percent a step for roundings).  A matrix of
  * zeros gives zeros; one that holds an infinity or a NaN gives NaN throughout (its
